@@ -50,7 +50,8 @@ enum {
 /* Bits of the sticky device status word. */
 enum {
   FLUX_DEV_KV_OVERFLOW = 1,   /* flux_kv_append dropped rows that did not fit `capacity` */
-  FLUX_DEV_BAD_LENGTH = 2     /* a kv_len / cu_seqlens value was inconsistent and was clamped */
+  FLUX_DEV_BAD_LENGTH = 2,    /* a kv_len / cu_seqlens value was inconsistent and was clamped */
+  FLUX_DEV_BAD_PAGE = 4       /* a page or slot number of a paged cache lies outside its pool and was left out */
 };
 
 typedef struct flux_ctx flux_ctx;   /* opaque; owns ONLY its device workspace */
@@ -274,6 +275,81 @@ int flux_kv_compact_ring(flux_ctx* ctx, const flux_kv_cache* src, const flux_kv_
  * ring must have been filled with n_sink and window rounded up to multiples of b. */
 int flux_attn_decode_ring(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const flux_kv_cache* ring,
                           void* out, void* stream);
+
+/* ---- Paged 8-bit KV caches: the same attention over a cache of half the bytes, whose sequences share one pool of pages.
+ *
+ * A PAGE holds FLUX_PAGE_TOKENS = 64 positions of a sequence (the block of App. C.3) for all KV heads of a layer, as e4m3 codes
+ * (sign, 4 exponent bits, 3 fraction bits, bias 7, no infinity; the codes 0x7F and 0xFF are NaN) with one fp32 scale per page,
+ * KV head and K or V: the value of a code is code * scale.  The block table says which pages a sequence has; it and the lengths
+ * are the same for all layers, so a step plans its pages once (flux_page_plan) and then runs flux_kv_append_paged and
+ * an attention call per layer, each on the layer's own pool. */
+#define FLUX_PAGE_TOKENS 64
+#define FLUX_MAX_PAGED_BATCH 4096   /* sequences of a flux_page_plan or flux_page_release call */
+
+/* Which pages the sequences have, and which are free.  Page `table[b * table_pages + i]` holds positions 64 i .. 64 i + 63 of
+ * sequence b; a sequence has ceil(kv_len[b] / 64) pages, and table entries behind them are not read.  A page may stand in the
+ * tables of several sequences (a shared prefix) as long as nobody appends to it or releases it. */
+typedef struct {
+  int32_t* table;           /* dev int32 [batch, table_pages] */
+  int32_t* kv_len;          /* dev int32 [batch]: valid positions per sequence */
+  int32_t* free_pages;      /* dev int32 [n_pages]: the free pages are entries 0 .. n_free - 1 (not used by attention: may be NULL there) */
+  int32_t* n_free;          /* dev int32 [1] (the same) */
+  int32_t batch, table_pages;   /* table_pages <= 2^24 */
+  int32_t n_pages;          /* pages of every layer's pool, at most 2^24: page numbers are 0 .. n_pages - 1 */
+} flux_page_table;
+
+/* One LAYER's pool, caller-owned: the code of (page p, KV head h, position t of the page, d) of K is byte
+ * p*stride_p + h*stride_h + t*stride_t + d of k, same strides for V; strides are multiples of 16 bytes, head_dim <= stride_t <=
+ * 2^20, and k and v are 16-byte aligned. */
+typedef struct {
+  void* k;                  /* dev e4m3 */
+  void* v;                  /* dev e4m3 */
+  float* k_scale;           /* dev fp32 [n_pages, n_kv_heads] */
+  float* v_scale;           /* dev fp32 [n_pages, n_kv_heads] */
+  int64_t stride_p, stride_h, stride_t;   /* in bytes */
+  int32_t n_pages;
+} flux_paged_kv;
+
+/* Pages and slots for the new tokens of a step.  Sequence b gets the rows cu_new[b] .. cu_new[b+1]-1 (dev int32 [batch+1], cut
+ * at total_new, the number of rows, host) at positions kv_len[b] .., and the ceil((kv_len[b] + rows) / 64) - ceil(kv_len[b] / 64)
+ * pages it lacks for them: the i-th page needed, counted by sequence and then by position, is free_pages[n_free - 1 - i].
+ * Writes those table entries, slots[t] = 64 * page + position % 64 for every row t (dev int32 [total_new]; -1: the row has no
+ * place), then kv_len[b] += rows that have one and n_free -= pages taken.  Where the free pages do not suffice, or table_pages
+ * does not, the last rows of the sequences that come too late get none and FLUX_DEV_KV_OVERFLOW is raised.  Numbers outside the
+ * pool raise FLUX_DEV_BAD_PAGE: a sequence whose last, partly filled page has one gets no new rows; a free page that has one is
+ * taken, but stands as -1 in the table and gives its rows no place (they count in kv_len[b]).
+ * batch <= FLUX_MAX_PAGED_BATCH, batch * table_pages < 2^31. */
+int flux_page_plan(flux_ctx* ctx, const flux_page_table* pt, const int32_t* cu_new, int total_new, int32_t* slots, void* stream);
+
+/* Cut every sequence to its first keep_len[b] positions (dev int32 [batch]; 0: the request is done; kv_len[b] or more: nothing
+ * changes; fewer: rejected tokens are taken back) and return the pages behind them, so that the next flux_page_plan takes the
+ * page of the first sequence's first returned place first (a plan is taken back exactly).  Returned table entries become -1.
+ * batch <= FLUX_MAX_PAGED_BATCH, batch * table_pages < 2^31.  Pages that stand in several tables must not be returned.  If the list of free pages would grow past n_pages, or an entry
+ * lies outside the pool, FLUX_DEV_BAD_PAGE is raised and the page is not listed. */
+int flux_page_release(flux_ctx* ctx, const flux_page_table* pt, const int32_t* keep_len, void* stream);
+
+/* Quantise new K/V rows of one layer into their slots.  k_new, v_new: dev bf16 [total_new, n_kv_heads, head_dim]; slots: dev
+ * int32 [total_new] as flux_page_plan writes them (rows of one page lie next to each other, in the order of their positions;
+ * no two rows have the same slot); rows with a negative slot, which stand before or behind those of a page, are left out.  The scale of a (page, head) is 2^e with the smallest
+ * e >= -100 for which no value of its block exceeds 448 * 2^e, the largest code; a page that holds rows already (slot % 64 of its
+ * first new row is not 0) keeps its scale unless a new row needs a larger one: then the codes it holds are rounded to that.
+ * Powers of two cost a code of 4 exponent bits nothing (values below 2^-14 of the block's largest one at most) and make that
+ * second rounding exact but for such values.  Rounding is to nearest even.  Values that are not finite are
+ * stored as NaN and do not count towards the scale; an attention result over such a row is NaN (prefill: also of earlier queries that share a tile of 64 keys
+ * with it).  A slot outside the pool raises FLUX_DEV_BAD_PAGE and its row is left out. */
+int flux_kv_append_paged(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int head_dim, const void* k_new, const void* v_new,
+                         const int32_t* slots, int total_new, void* stream);
+
+/* flux_attn_decode over a paged 8-bit cache: one query per sequence at position kv_len[b] - 1, mode bytes, SA rule, outputs and
+ * determinism as there; keys and values are code * scale (any finite scale >= 0).  max_kv_len: host upper bound on kv_len[b],
+ * at most 64 * table_pages (which is always valid); pages of a longer list are left out, the oldest kept, and FLUX_DEV_BAD_LENGTH
+ * is raised.  Where all sequences are SA, 64 * (ceil(n_sink / 64) + ceil(window / 64) + 1) is enough (n_sink and window rounded
+ * up to multiples of sa_block).  The workspace that flux_workspace_needed names for these arguments is enough.
+ * batch * n_kv_heads * ceil(group / 16) * (ceil(max_kv_len / 64) + 16) must be below 2^31 (FLUX_EINVAL).
+ * What lies behind kv_len[b] in a page is never used.  A table entry outside the pool counts as a page that is not there, and
+ * raises FLUX_DEV_BAD_PAGE; rows without any key are zero. */
+int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, int max_kv_len, const flux_paged_kv* kv,
+                           const flux_page_table* pt, const uint8_t* mode, void* out, void* stream);
 
 #ifdef __cplusplus
 }

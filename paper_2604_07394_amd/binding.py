@@ -22,13 +22,15 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 FLUX_OK, FLUX_EINVAL, FLUX_ECAPACITY, FLUX_EWORKSPACE, FLUX_EHIP, FLUX_ENOMEM = 0, -1, -2, -3, -4, -5
-FLUX_DEV_KV_OVERFLOW, FLUX_DEV_BAD_LENGTH = 1, 2
+FLUX_DEV_KV_OVERFLOW, FLUX_DEV_BAD_LENGTH, FLUX_DEV_BAD_PAGE = 1, 2, 4
 FA, SA = 1, 0
 
 EXPORTS = ["flux_create", "flux_destroy", "flux_strerror", "flux_workspace_needed", "flux_last_device_status",
            "flux_router", "flux_kv_append", "flux_attn_prefill", "flux_attn_decode",
            "flux_kv_append_ring", "flux_kv_compact_ring", "flux_attn_decode_ring", "flux_attn_decode_static",
-           "flux_attn_prefill_blocksparse", "flux_xa_select", "flux_attn_decode_append"]
+           "flux_attn_prefill_blocksparse", "flux_xa_select", "flux_attn_decode_append",
+           "flux_page_plan", "flux_page_release", "flux_kv_append_paged", "flux_attn_decode_paged"]
+PAGE_TOKENS, MAX_PAGED_BATCH = 64, 4096
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024 + 256
 
 
@@ -44,8 +46,20 @@ class FluxKVCache(C.Structure):
                 ("kv_len", C.c_void_p), ("batch", C.c_int32), ("capacity", C.c_int32)]
 
 
+class FluxPageTable(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("kv_len", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p),
+                ("batch", C.c_int32), ("table_pages", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class FluxPagedKV(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("stride_p", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64), ("n_pages", C.c_int32)]
+
+
 _pack_cache = struct.Struct("@PPqqqPii").pack                # the bytes of a FluxKVCache
 assert struct.calcsize("@PPqqqPii") == C.sizeof(FluxKVCache)
+_pack_pages, _pack_paged_kv = struct.Struct("@PPPPiii0P").pack, struct.Struct("@PPPPqqqi0q").pack
+assert struct.calcsize("@PPPPiii0P") == C.sizeof(FluxPageTable) and struct.calcsize("@PPPPqqqi0q") == C.sizeof(FluxPagedKV)
 
 _lib.flux_create.argtypes = [C.POINTER(C.c_void_p), C.c_int, C.c_size_t]
 _lib.flux_create.restype = C.c_int
@@ -91,6 +105,17 @@ _lib.flux_kv_compact_ring.restype = C.c_int
 _lib.flux_attn_decode_ring.argtypes = [C.c_void_p, C.POINTER(FluxAttnCfg), C.c_void_p, C.c_void_p,
                                        C.c_void_p, C.c_void_p]
 _lib.flux_attn_decode_ring.restype = C.c_int
+
+_lib.flux_page_plan.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
+_lib.flux_page_plan.restype = C.c_int
+_lib.flux_page_release.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.flux_page_release.restype = C.c_int
+_lib.flux_kv_append_paged.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                      C.c_void_p]
+_lib.flux_kv_append_paged.restype = C.c_int
+_lib.flux_attn_decode_paged.argtypes = [C.c_void_p, C.POINTER(FluxAttnCfg), C.c_void_p, C.c_int, C.c_void_p, C.c_void_p,
+                                        C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.flux_attn_decode_paged.restype = C.c_int
 
 
 class FluxError(RuntimeError):
@@ -186,6 +211,59 @@ def _cache_arg(cache):
     return _pack_cache(k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], cache.kv_len.data_ptr(), b, cap)
 
 
+@dataclass
+class PageTable:
+    """Which pages the sequences of a batch have, for all layers: table int32 [B, table_pages], kv_len int32 [B], and the free
+    pages, free_pages int32 [n_pages] (entries 0 .. n_free - 1) and n_free int32 [1]."""
+    table: torch.Tensor
+    kv_len: torch.Tensor
+    free_pages: torch.Tensor
+    n_free: torch.Tensor
+
+    @classmethod
+    def empty(cls, batch, n_pages, table_pages, device="cuda"):
+        """No sequence has a page; pages are given out from number 0 on."""
+        def i32(x):
+            return torch.tensor(x, dtype=torch.int32, device=device)
+        return cls(torch.full((batch, table_pages), -1, dtype=torch.int32, device=device), torch.zeros(batch, dtype=torch.int32, device=device),
+                   torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device), i32([n_pages]))
+
+
+@dataclass
+class PagedKV:
+    """One layer's pool of pages: k, v [n_pages, Hkv, 64, D] e4m3 codes (torch.float8_e4m3fn or uint8; any strides of multiples of
+    16 with D contiguous), k_scale, v_scale fp32 [n_pages, Hkv].  Plain device memory; all reads and writes happen in the library."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, head_dim, device="cuda"):
+        k = torch.empty(n_pages, n_kv_heads, PAGE_TOKENS, head_dim, dtype=torch.float8_e4m3fn, device=device)
+        s = torch.empty(n_pages, n_kv_heads, dtype=torch.float32, device=device)
+        return cls(k, torch.empty_like(k), s, torch.empty_like(s))
+
+
+def _pages_arg(pt):
+    if type(pt) is not PageTable:
+        return C.byref(pt)
+    t = pt.table
+    b, wide = t.shape
+    assert t.is_contiguous() and pt.kv_len.shape[0] == b
+    return _pack_pages(t.data_ptr(), pt.kv_len.data_ptr(), pt.free_pages.data_ptr(), pt.n_free.data_ptr(), b, wide, pt.free_pages.shape[0])
+
+
+def _paged_kv_arg(kv):
+    if type(kv) is not PagedKV:
+        return C.byref(kv)
+    k, v = kv.k, kv.v
+    strides, (n, h, tokens, _) = k.stride(), k.shape
+    assert tokens == PAGE_TOKENS and strides == v.stride() and strides[3] == 1 and k.element_size() == 1 and v.shape == k.shape
+    assert kv.k_scale.shape == (n, h) == kv.v_scale.shape and kv.k_scale.is_contiguous() and kv.v_scale.is_contiguous()
+    return _pack_paged_kv(k.data_ptr(), v.data_ptr(), kv.k_scale.data_ptr(), kv.v_scale.data_ptr(), strides[0], strides[1], strides[2], n)
+
+
 def flux_router(ctx, x, cu_seqlens, batch, hidden, pool, w1, b1, w2, b2, inner, mode_out, logits_out=None,
                 stream=None) -> None:
     _check(_lib.flux_router(ctx, _ptr(x), _ptr(cu_seqlens), batch, hidden, pool, _ptr(w1), _ptr(b1), _ptr(w2),
@@ -243,3 +321,21 @@ def flux_kv_compact_ring(ctx, src, dst, n_kv_heads, head_dim, n_sink, window, st
 
 def flux_attn_decode_ring(ctx, cfg, q, ring, out, stream=None) -> None:
     _check(_lib.flux_attn_decode_ring(ctx, C.byref(cfg), _ptr(q), _cache_arg(ring), _ptr(out), _stream(stream)))
+
+
+def flux_page_plan(ctx, pt, cu_new, total_new, slots, stream=None) -> None:
+    _check(_lib.flux_page_plan(ctx, _pages_arg(pt), _ptr(cu_new), total_new, _ptr(slots), _stream(stream)))
+
+
+def flux_page_release(ctx, pt, keep_len, stream=None) -> None:
+    _check(_lib.flux_page_release(ctx, _pages_arg(pt), _ptr(keep_len), _stream(stream)))
+
+
+def flux_kv_append_paged(ctx, kv, n_kv_heads, head_dim, k_new, v_new, slots, total_new, stream=None) -> None:
+    _check(_lib.flux_kv_append_paged(ctx, _paged_kv_arg(kv), n_kv_heads, head_dim, _ptr(k_new), _ptr(v_new), _ptr(slots), total_new,
+                                     _stream(stream)))
+
+
+def flux_attn_decode_paged(ctx, cfg, q, max_kv_len, kv, pt, mode, out, stream=None) -> None:
+    _check(_lib.flux_attn_decode_paged(ctx, C.byref(cfg), _ptr(q), max_kv_len, _paged_kv_arg(kv), _pages_arg(pt), _ptr(mode), _ptr(out),
+                                       _stream(stream)))

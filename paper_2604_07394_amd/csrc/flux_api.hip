@@ -8,7 +8,7 @@
 #include <mutex>
 #include <new>
 
-#include "flux_internal.h"
+#include "paged.h"
 
 using namespace flux;
 
@@ -77,6 +77,37 @@ int check_cache(const flux_kv_cache* kc, int head_dim) {
   if ((kc->stride_t | kc->stride_h | kc->stride_b) & 7) return FLUX_EINVAL;
   if (kc->stride_t > (1 << 22)) return FLUX_EINVAL;        // 32-bit byte offsets inside a 64-row tile
   return FLUX_OK;
+}
+
+int check_page_table(const flux_page_table* pt, bool plans) {
+  if (!pt || !pt->table || !pt->kv_len) return FLUX_EINVAL;
+  if (pt->batch <= 0 || pt->table_pages <= 0 || pt->n_pages <= 0) return FLUX_EINVAL;
+  if (pt->table_pages > (1 << 24) || pt->n_pages > (1 << 24)) return FLUX_EINVAL;   // positions, slots and page counts in 32 bits
+  if (!plans) return FLUX_OK;
+  if (!pt->free_pages || !pt->n_free || pt->batch > FLUX_MAX_PAGED_BATCH) return FLUX_EINVAL;
+  return (long long)pt->batch * pt->table_pages <= 0x7FFFFFFFll ? FLUX_OK : FLUX_EINVAL;
+}
+
+int check_paged_kv(const flux_paged_kv* kv, int head_dim) {
+  if (!kv || !kv->k || !kv->v || !kv->k_scale || !kv->v_scale) return FLUX_EINVAL;
+  if (kv->n_pages <= 0 || kv->n_pages > (1 << 24)) return FLUX_EINVAL;
+  if (!aligned16(kv->k) || !aligned16(kv->v)) return FLUX_EINVAL;
+  if (kv->stride_t < head_dim || kv->stride_h < 0 || kv->stride_p < 0) return FLUX_EINVAL;
+  if ((kv->stride_t | kv->stride_h | kv->stride_p) & 15) return FLUX_EINVAL;
+  return kv->stride_t <= (1 << 20) ? FLUX_OK : FLUX_EINVAL;   // 32-bit byte offsets inside a page
+}
+
+// What the attention calls over a paged cache share.
+int check_paged_attention(const flux_attn_cfg* cfg, const void* q, int max_kv_len, const flux_paged_kv* kv, const flux_page_table* pt, const void* out) {
+  int rc = check_cfg(cfg);
+  if (rc != FLUX_OK) return rc;
+  rc = check_paged_kv(kv, cfg->head_dim);
+  if (rc != FLUX_OK) return rc;
+  rc = check_page_table(pt, false);
+  if (rc != FLUX_OK) return rc;
+  if (pt->n_pages > kv->n_pages || max_kv_len < 0) return FLUX_EINVAL;
+  if (max_kv_len > pt->table_pages * kPageTokens) return FLUX_ECAPACITY;
+  return aligned16(q) && aligned16(out) ? FLUX_OK : FLUX_EINVAL;
 }
 
 }  // namespace
@@ -392,6 +423,54 @@ int flux_attn_decode_ring(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q
   if (ctx->c.device >= 0 && decode_partials_bytes(*cfg, p) > ctx->c.partials_bytes) return FLUX_EWORKSPACE;
   if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
   const hipError_t e = launch_decode(ctx->c, *cfg, q, n_keys, *ring, nullptr, 1, nullptr, nullptr, out, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+// ---- paged 8-bit caches
+
+int flux_page_plan(flux_ctx* ctx, const flux_page_table* pt, const int32_t* cu_new, int total_new, int32_t* slots, void* stream) {
+  if (!ctx || !cu_new || !slots || total_new < 0 || total_new > (1 << 30)) return FLUX_EINVAL;
+  const int rc = check_page_table(pt, true);
+  if (rc != FLUX_OK) return rc;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  if (total_new == 0) return FLUX_OK;
+  const hipError_t e = launch_page_plan(ctx->c, *pt, cu_new, total_new, slots, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+int flux_page_release(flux_ctx* ctx, const flux_page_table* pt, const int32_t* keep_len, void* stream) {
+  if (!ctx || !keep_len) return FLUX_EINVAL;
+  const int rc = check_page_table(pt, true);
+  if (rc != FLUX_OK) return rc;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  const hipError_t e = launch_page_release(ctx->c, *pt, keep_len, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+int flux_kv_append_paged(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int head_dim, const void* k_new,
+                         const void* v_new, const int32_t* slots, int total_new, void* stream) {
+  if (!ctx || !k_new || !v_new || !slots) return FLUX_EINVAL;
+  if (head_dim != 64 && head_dim != 128) return FLUX_EINVAL;
+  if (n_kv_heads <= 0 || total_new < 0 || total_new > (1 << 30)) return FLUX_EINVAL;
+  const int rc = check_paged_kv(kv, head_dim);
+  if (rc != FLUX_OK) return rc;
+  if (!aligned16(k_new) || !aligned16(v_new)) return FLUX_EINVAL;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  if (total_new == 0) return FLUX_OK;
+  const hipError_t e = launch_kv_append_paged(ctx->c, *kv, n_kv_heads, head_dim, k_new, v_new, slots, total_new, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, int max_kv_len, const flux_paged_kv* kv,
+                           const flux_page_table* pt, const uint8_t* mode, void* out, void* stream) {
+  if (!ctx || !q || !mode || !out) return FLUX_EINVAL;
+  const int rc = check_paged_attention(cfg, q, max_kv_len, kv, pt, out);
+  if (rc != FLUX_OK) return rc;
+  const DecodePlan p = plan_decode_paged(*cfg, pt->batch, max_kv_len);
+  if ((long long)pt->batch * p.pps > 0x7FFFFFFFll / (pages_of(max_kv_len) + 16)) return FLUX_EINVAL;   // pages are counted in 32 bits
+  if (ctx->c.device >= 0 && decode_partials_bytes(*cfg, p) > ctx->c.partials_bytes) return FLUX_EWORKSPACE;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  const hipError_t e = launch_decode_paged(ctx->c, *cfg, q, max_kv_len, *kv, *pt, mode, out, (hipStream_t)stream);
   return e == hipSuccess ? FLUX_OK : hip_fail(e);
 }
 

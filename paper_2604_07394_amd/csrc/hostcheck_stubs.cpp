@@ -2,7 +2,7 @@
 // reports that there is no device.  (The real ones live next to their kernels.)  The two calls of the runtime with which the
 // static scratch is looked up are answered here, so that flux_attn_decode_static gets as far as its launcher, which notes
 // what it was given.
-#include "flux_internal.h"
+#include "paged.h"
 
 extern "C" {
 hipError_t hipGetDevice(int* device) { *device = 0; return hipSuccess; }
@@ -55,5 +55,12 @@ hipError_t launch_router(const Ctx&, const void*, const int32_t*, int, int, int,
                          const void*, int, uint8_t*, float*, hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_xa_select(const Ctx&, const flux_attn_cfg&, const void*, const int32_t*, int, const flux_kv_cache&, float,
                             uint8_t*, int, int, hipStream_t) { return hipErrorNoDevice; }
+
+hipError_t launch_page_plan(const Ctx&, const flux_page_table&, const int32_t*, int, int32_t*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_page_release(const Ctx&, const flux_page_table&, const int32_t*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_kv_append_paged(const Ctx&, const flux_paged_kv&, int, int, const void*, const void*, const int32_t*, int,
+                                  hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_decode_paged(const Ctx&, const flux_attn_cfg&, const void*, int, const flux_paged_kv&, const flux_page_table&,
+                               const uint8_t*, void*, hipStream_t) { return hipErrorNoDevice; }
 
 }  // namespace flux

@@ -1,0 +1,186 @@
+// flux_kv_append_paged: new K/V rows are quantised into the pages that their slots name.
+//
+// The new rows of one page and KV head are a BLOCK.  Its scale is 2^e, e the smallest exponent >= kMinScaleExp with
+// amax <= 448 * 2^e (448 = 1.75 * 2^8 is the largest e4m3 value), which is read off the bits of amax; a code is x * 2^-e rounded to
+// nearest even, and as the product is exact there is one rounding.  A page that holds rows already keeps its scale or takes
+// the larger one of the new rows, and then its old codes are rounded once more.
+//
+// One wave per block, K or V: up to 64 rows stay in its registers between the maximum and the rounding, so every row is read once,
+// with up to 16 KB on their way per wave, and nothing passes between waves.
+// What bounds it: the memory for long prompts, latencies (slots, scale, row) for a decode step.
+#include "paged.h"
+
+namespace flux {
+
+struct PagedAppendArgs {
+  const char *k_new, *v_new;      // bf16 [total, hkv, D]
+  char *k, *v;
+  float *k_scale, *v_scale;
+  int64_t stride_p, stride_h, stride_t;
+  const int32_t* slots;
+  int hkv, total, n_pages;
+  long long units;                // (tile of ROWS token rows, head, K or V)
+  uint32_t* status;
+};
+
+typedef __attribute__((__vector_size__(2 * sizeof(uint16_t)))) uint16_t u16x2;
+
+// largest of the values' magnitudes, as bits
+__device__ __forceinline__ uint32_t pk_max(uint32_t a, uint32_t b) {
+  const u16x2 x = __builtin_bit_cast(u16x2, a), y = __builtin_bit_cast(u16x2, b);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
+}
+__device__ __forceinline__ uint32_t finite_bits(uint32_t pair) {   // magnitudes, those that are not finite as 0
+  const uint32_t lo = pair & 0x7FFFu, hi = (pair >> 16) & 0x7FFFu;
+  return (lo < 0x7F80u ? lo : 0u) | (hi < 0x7F80u ? hi << 16 : 0u);
+}
+
+// Four values times `inv` as codes, to nearest even.  (The conversion would make a large number of an infinite value: it is NaN
+// by then.)
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, r, true);
+}
+__device__ __forceinline__ float finite_or_nan(float x) { return x - x == 0.f ? x : __builtin_nanf(""); }
+
+// ROWS: token rows that a wave looks after: it does every block that begins in them.  1 where there are few rows, so that the
+// blocks of a decode step are worked on side by side; 64 for long prompts, where a page's rows begin in every tile.
+template <int D, int ROWS>
+__global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a) {
+  constexpr int LPR = D / 8;                                 // lanes per row, 16 bytes each
+  constexpr int RPS = 64 / LPR;                              // rows per step
+  constexpr int STEPS = 64 / RPS;
+  const int l = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int per_tile = 2 * a.hkv;
+  for (long long u = (long long)blockIdx.x * 4 + w; u < a.units; u += (long long)gridDim.x * 4) {
+    const int tile = (int)(u / per_tile), rest = (int)(u - (long long)tile * per_tile);
+    const int h = rest >> 1;
+    const bool is_v = rest & 1;
+    const int t0 = tile * ROWS;
+    // where blocks begin: a row whose slot does not follow that of the row before in the same page
+    uint64_t begins = 1;
+    if (ROWS > 1) {
+      const int t = t0 + l;
+      const int s = t < a.total ? a.slots[t] : -1, p = t > 0 && t < a.total ? a.slots[t - 1] : -1;
+      begins = __builtin_amdgcn_ballot_w64(s >= 0 && !(p == s - 1 && (s & 63) != 0));
+    }
+    while (begins != 0) {
+      const int t = t0 + __builtin_ctzll(begins);
+      begins &= begins - 1;
+      const int mine = t + l < a.total ? a.slots[t + l] : -1;
+      const int slot = __builtin_amdgcn_readfirstlane(mine);
+      if (slot < 0) break;                                   // (ROWS = 1: the row has no place)
+      if (ROWS == 1 && (slot & 63) != 0 && t > 0 && a.slots[t - 1] == slot - 1) break;   // belongs to the block of the row before
+      const int page = slot >> 6, first = slot & 63;
+      if (page >= a.n_pages) {
+        if (l == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
+        continue;
+      }
+      const uint64_t others = ~__builtin_amdgcn_ballot_w64(first + l < 64 && mine == slot + l);
+      const int rows = others == 0 ? 64 : __builtin_ctzll(others);
+      const char* src = (is_v ? a.v_new : a.k_new) + (((int64_t)t * a.hkv + h) * D + (l % LPR) * 8) * 2;
+      const int64_t src_step = (int64_t)a.hkv * D * 2;
+      float* const scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.hkv + h;
+      char* const dst = (is_v ? a.v : a.k) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h + (l % LPR) * 8;
+      u32x4 x[STEPS];
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        x[i] = u32x4{0, 0, 0, 0};
+        if (i * RPS < rows) {                                // (uniform)
+          const int r = i * RPS + l / LPR;
+          if (r < rows) x[i] = *(const u32x4*)(src + r * src_step);
+        }
+      }
+      const float old = first != 0 ? *scale_at : 0.f;
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = pk_max(top, x[i][j] & 0x7FFF7FFFu);
+      bool odd = (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u;
+      odd = __builtin_amdgcn_ballot_w64(odd) != 0;           // some value is not finite
+      if (odd) {
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) top = pk_max(top, finite_bits(x[i][j]));
+      }
+      int amax = max((int)(top & 0xFFFFu), (int)(top >> 16));
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) amax = max(amax, __shfl_xor(amax, off));
+      amax = __builtin_amdgcn_readfirstlane(amax);
+      // amax = (1 + f / 128) 2^(E - 127): it fits under 1.75 * 2^(8 + e) from e = E - 135 on, or one more where f > 96
+      const int e = max((amax >> 7) - 135 + ((amax & 127) > 96 ? 1 : 0), kMinScaleExp);
+      float scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
+      scale = old > scale ? old : scale;
+      const float inv = 1.0f / scale;                        // exact: a power of two
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        if (i * RPS >= rows) continue;
+        const int r = i * RPS + l / LPR;
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f[2 * j] = bf16_lo(x[i][j]);
+          f[2 * j + 1] = bf16_hi(x[i][j]);
+        }
+        if (odd) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = finite_or_nan(f[j]);
+        }
+        if (r < rows) *(u32x2*)(dst + (first + r) * a.stride_t) = u32x2{codes4(f[0], f[1], f[2], f[3], inv), codes4(f[4], f[5], f[6], f[7], inv)};
+      }
+      if (first != 0 && scale > old) {                       // the rows that the page holds take the new scale too
+        const float down = old * inv;
+        for (int r0 = 0; r0 < first; r0 += RPS) {
+          const int r = r0 + l / LPR;
+          if (r >= first) continue;
+          u32x2* const at = (u32x2*)(dst + r * a.stride_t);
+          u32x2 c = *at;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[j], true);
+            c[j] = codes4(lo[0], lo[1], hi[0], hi[1], down);
+          }
+          *at = c;
+        }
+      }
+      if (l == 0 && (first == 0 || scale > old)) *scale_at = scale;
+    }
+  }
+}
+
+hipError_t launch_kv_append_paged(const Ctx& c, const flux_paged_kv& kv, int hkv, int d, const void* k_new, const void* v_new,
+                                  const int32_t* slots, int total_new, hipStream_t s) {
+  PagedAppendArgs a;
+  a.k_new = (const char*)k_new;
+  a.v_new = (const char*)v_new;
+  a.k = (char*)kv.k;
+  a.v = (char*)kv.v;
+  a.k_scale = kv.k_scale;
+  a.v_scale = kv.v_scale;
+  a.stride_p = kv.stride_p;
+  a.stride_h = kv.stride_h;
+  a.stride_t = kv.stride_t;
+  a.slots = slots;
+  a.hkv = hkv;
+  a.total = total_new;
+  a.n_pages = kv.n_pages;
+  a.status = c.status;
+  const bool few = (long long)total_new * hkv <= kAppendPagedFew;
+  a.units = ((long long)total_new + (few ? 0 : 63)) / (few ? 1 : 64) * 2 * hkv;
+  const long long wgs = (a.units + 3) / 4;
+  const dim3 grid((unsigned)(wgs < kAppendMost ? wgs : kAppendMost)), block(256);
+  if (d == 128) {
+    if (few) hipLaunchKernelGGL((kv_append_paged_kernel<128, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((kv_append_paged_kernel<128, 64>), grid, block, 0, s, a);
+  } else {
+    if (few) hipLaunchKernelGGL((kv_append_paged_kernel<64, 1>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((kv_append_paged_kernel<64, 64>), grid, block, 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace flux
