@@ -351,6 +351,20 @@ int flux_kv_append_paged(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads,
 int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, int max_kv_len, const flux_paged_kv* kv,
                            const flux_page_table* pt, const uint8_t* mode, void* out, void* stream);
 
+/* flux_attn_prefill over a paged 8-bit cache: q, cu_q, max_q_len, max_kv_len, mode, out as there (the queries of sequence b are the
+ * last n_q(b) positions of its pages: flux_page_plan and flux_kv_append_paged first); keys and values are code * scale (any
+ * finite scale >= 0; a scale of V that is not a power of two rounds its values to bf16).  A tile of query rows holds all heads
+ * of a group, token by token, and walks only pages of which a row sees something; pages of a tile may be shared out over several
+ * workgroups where max_kv_len >= 1024, as far as the workspace has room for their results (any context will do), in a way that
+ * depends on the bounds, lengths and modes of the whole batch.  max_q_len * group <= 2^30, and
+ * batch * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^22 is always enough (FLUX_EINVAL).
+ * What lies behind kv_len[b] in a page is never used; the codes of a page of which a row of a tile sees something must not be NaN
+ * below that, or rows of the tile that do not see them may become NaN as well.  A table entry outside the pool counts as a page that is
+ * not there, and raises FLUX_DEV_BAD_PAGE; rows without any key are zero. */
+int flux_attn_prefill_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q, int max_q_len,
+                            int max_kv_len, const flux_paged_kv* kv, const flux_page_table* pt, const uint8_t* mode,
+                            void* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,8 @@ EXPORTS = ["flux_create", "flux_destroy", "flux_strerror", "flux_workspace_neede
            "flux_router", "flux_kv_append", "flux_attn_prefill", "flux_attn_decode",
            "flux_kv_append_ring", "flux_kv_compact_ring", "flux_attn_decode_ring", "flux_attn_decode_static",
            "flux_attn_prefill_blocksparse", "flux_xa_select", "flux_attn_decode_append",
-           "flux_page_plan", "flux_page_release", "flux_kv_append_paged", "flux_attn_decode_paged"]
+           "flux_page_plan", "flux_page_release", "flux_kv_append_paged", "flux_attn_decode_paged",
+           "flux_attn_prefill_paged"]
 PAGE_TOKENS, MAX_PAGED_BATCH = 64, 4096
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024 + 256
 
@@ -116,6 +117,9 @@ _lib.flux_kv_append_paged.restype = C.c_int
 _lib.flux_attn_decode_paged.argtypes = [C.c_void_p, C.POINTER(FluxAttnCfg), C.c_void_p, C.c_int, C.c_void_p, C.c_void_p,
                                         C.c_void_p, C.c_void_p, C.c_void_p]
 _lib.flux_attn_decode_paged.restype = C.c_int
+_lib.flux_attn_prefill_paged.argtypes = [C.c_void_p, C.POINTER(FluxAttnCfg), C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
+                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.flux_attn_prefill_paged.restype = C.c_int
 
 
 class FluxError(RuntimeError):
@@ -339,3 +343,8 @@ def flux_kv_append_paged(ctx, kv, n_kv_heads, head_dim, k_new, v_new, slots, tot
 def flux_attn_decode_paged(ctx, cfg, q, max_kv_len, kv, pt, mode, out, stream=None) -> None:
     _check(_lib.flux_attn_decode_paged(ctx, C.byref(cfg), _ptr(q), max_kv_len, _paged_kv_arg(kv), _pages_arg(pt), _ptr(mode), _ptr(out),
                                        _stream(stream)))
+
+
+def flux_attn_prefill_paged(ctx, cfg, q, cu_q, max_q_len, max_kv_len, kv, pt, mode, out, stream=None) -> None:
+    _check(_lib.flux_attn_prefill_paged(ctx, C.byref(cfg), _ptr(q), _ptr(cu_q), max_q_len, max_kv_len, _paged_kv_arg(kv), _pages_arg(pt),
+                                        _ptr(mode), _ptr(out), _stream(stream)))

@@ -474,4 +474,19 @@ int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* 
   return e == hipSuccess ? FLUX_OK : hip_fail(e);
 }
 
+int flux_attn_prefill_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
+                            const flux_paged_kv* kv, const flux_page_table* pt, const uint8_t* mode, void* out, void* stream) {
+  if (!ctx || !q || !cu_q || !mode || !out) return FLUX_EINVAL;
+  const int rc = check_paged_attention(cfg, q, max_kv_len, kv, pt, out);
+  if (rc != FLUX_OK) return rc;
+  if (max_q_len < 0 || max_q_len > max_kv_len) return FLUX_EINVAL;
+  // rows of a group and workgroups are counted in 32 bits
+  if ((long long)max_q_len * (cfg->n_q_heads / cfg->n_kv_heads) > (1 << 30)) return FLUX_EINVAL;
+  const PagedPrefillPlan p = plan_prefill_paged(*cfg, pt->batch, max_q_len, max_kv_len, ctx->c.partials_bytes);
+  if (p.wgs > kAppendMost) return FLUX_EINVAL;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  const hipError_t e = launch_prefill_paged(ctx->c, *cfg, q, cu_q, max_q_len, max_kv_len, *kv, *pt, mode, out, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
 }  // extern "C"

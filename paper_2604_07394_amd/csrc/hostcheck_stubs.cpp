@@ -62,5 +62,7 @@ hipError_t launch_kv_append_paged(const Ctx&, const flux_paged_kv&, int, int, co
                                   hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_decode_paged(const Ctx&, const flux_attn_cfg&, const void*, int, const flux_paged_kv&, const flux_page_table&,
                                const uint8_t*, void*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_prefill_paged(const Ctx&, const flux_attn_cfg&, const void*, const int32_t*, int, int, const flux_paged_kv&,
+                                const flux_page_table&, const uint8_t*, void*, hipStream_t) { return hipErrorNoDevice; }
 
 }  // namespace flux

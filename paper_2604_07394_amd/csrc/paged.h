@@ -23,4 +23,40 @@ inline DecodePlan plan_decode_paged(const flux_attn_cfg& cfg, int batch, int max
 hipError_t launch_decode_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, int max_kv_len, const flux_paged_kv& kv,
                                const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s);
 
+// ---- prefill over pages: what its launch is bounded by (the plan itself is taken on the device, see paged_plan)
+constexpr int kPagedResident = 512;           // workgroups that the chip holds at once, two per CU
+constexpr int kPagedMinPages = 8;             // a unit that shares a tile with others has at least so many pages
+// Units of one (KV head, part) have ids of one residue mod 8, or of 8 / groups residues: units that `groups` of them take, some of
+// them padding.
+constexpr int share_shift(int groups) { return groups == 1 ? 3 : (groups == 2 ? 2 : (groups == 4 ? 1 : 0)); }
+constexpr int unit_count(int groups, int tiles) {
+  return share_shift(groups) > 0 ? ((tiles + (1 << share_shift(groups)) - 1) >> share_shift(groups)) * 8 : groups * tiles;
+}
+struct PagedPrefillPlan {
+  int bm;               // rows of a tile
+  int tiles;            // of a sequence and KV head, at most
+  long long wgs;        // workgroups launched
+  int part_units;       // units whose rows the workspace has room for; 0: tiles are not shared out
+  size_t info_bytes;    // of the table in front of these rows
+};
+inline PagedPrefillPlan plan_prefill_paged(const flux_attn_cfg& cfg, int batch, int max_q_len, int max_kv_len, size_t partials_bytes) {
+  PagedPrefillPlan p;
+  const long long rows = (long long)max_q_len * (cfg.n_q_heads / cfg.n_kv_heads);
+  p.bm = rows <= 64 ? 64 : 128;
+  p.tiles = (int)((rows + p.bm - 1) / p.bm);
+  p.wgs = (long long)batch * unit_count(cfg.n_kv_heads, p.tiles);
+  p.part_units = 0;
+  p.info_bytes = ((size_t)batch * cfg.n_kv_heads * p.tiles * 16 + 255) / 256 * 256;
+  // worth a second launch where lists may be long and tiles few (in a batch, only the device knows how few)
+  if (pages_of(max_kv_len) >= 2 * kPagedMinPages && (batch > 1 || 3 * p.wgs <= 2 * kPagedResident) && p.info_bytes <= partials_bytes / 4) {
+    const size_t fit = (partials_bytes - p.info_bytes) / ((size_t)p.bm * (cfg.head_dim + 2) * sizeof(float));
+    const size_t want = 2 * kPagedResident + (size_t)8 * batch;
+    p.part_units = (int)(fit < want ? fit : want);
+    if (p.wgs < p.part_units) p.wgs = p.part_units;
+  }
+  return p;
+}
+hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
+                                const flux_paged_kv& kv, const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s);
+
 }  // namespace flux

@@ -1,0 +1,609 @@
+// flux_attn_prefill_paged: attention of the newest tokens of every sequence over a cache of 8-bit pages (Eq. 1 / Eq. 2, chosen per
+// sequence by the mode byte).  The mathematics is that of decode_paged.hip, the shape that of prefill.hip: a workgroup of four
+// waves owns a tile of query rows and walks the pages that a row of it sees, 64 keys at a time,
+//   S^T[key][q]  = ck[key][:] . Q[q][:]            MFMA 16x16x32 bf16, A = keys from LDS, B = Q in registers
+//   weights against a reference that moves only when a weight leaves the guarded range, rounded to bf16 (2^-9 of a weight; the
+//   denominator sums the rounded ones)
+//   O^T[d][q]   += (sv cv)^T[d][key] . p^T[key][q] V from LDS through the transposing read
+//
+// A tile is BM = 64 QB rows: the query rows of all heads of the group, token by token (row R is head R % group of token R /
+// group), so that short runs of queries fill their tiles and K and V are read once per group.
+//
+// Codes become bf16 on their way into LDS: once per workgroup and page.  (In the waves' registers, behind the LDS reads, each of
+// the four waves would convert every code.)  A page's codes are asked for an iteration ahead of that, two ahead of their use.  The
+// scale of K goes into the exponent's factor, that of V into the conversion: exact for powers of two, which the append
+// writes; any other scale rounds V * scale to bf16, 2^-9 of it at most.
+//
+// Where the tiles do not fill the chip their pages are shared out over several workgroups, whose unnormalised rows a second
+// launch merges (see paged_plan).
+#include <type_traits>
+
+#include "paged.h"
+
+namespace flux {
+
+typedef __attribute__((__vector_size__(4 * sizeof(int32_t)))) int32_t i32x4;
+
+struct PagedPrefillArgs {
+  const __bf16* q;        // [T, Hq, D]
+  const int32_t* cu_q;
+  const char *k, *v;
+  const float *k_scale, *v_scale;
+  int64_t stride_p, stride_h, stride_t;
+  const int32_t* table;
+  int table_pages, n_pages;
+  const int32_t* kv_len;
+  const uint8_t* mode;
+  int hq, hkv, group, batch;
+  int sink_lim, win_blocks, blk_shift;   // SA geometry (see sa_geom)
+  int n_qtiles;           // tiles that a sequence has at most, by the host's bound
+  int n_wg;
+  float scale_log2;
+  int out_fp32;
+  void* out;
+  uint32_t* status;
+  int part_units;         // units whose rows the workspace holds; 0: tiles are never shared out
+  float* part_o;          // unnormalised rows of a unit [unit][BM][D]
+  float* part_ml;         // their reference (log2 units) and weight sum [unit][BM][2]
+  i32x4* tile_info;       // [batch][hkv][n_qtiles]: first unit, unit stride, units of the tile
+};
+
+constexpr float kPagedGuard = 1073741824.0f;  // 2^30: a page whose weights sum past this moves the reference
+constexpr int kPagedNoSplit = 0x3FFFFFFF;
+
+struct PagedSeq {
+  int q_begin, n_q, len, tiles, pages;   // pages: of its longest tile (an upper bound for SA)
+  bool sa, bad;
+};
+__device__ __forceinline__ PagedSeq paged_seq(const PagedPrefillArgs& a, int b, int bm) {
+  PagedSeq s = {0, 0, 0, 0, 0, false, false};
+  if (b >= a.batch) return s;
+  s.q_begin = a.cu_q[b];
+  s.n_q = a.cu_q[b + 1] - s.q_begin;
+  s.len = a.kv_len[b];
+  s.sa = a.mode[b] == 0;
+  const int cap = a.table_pages * kPageTokens;
+  s.bad = s.n_q < 0 || s.len < 0 || s.len > cap || s.n_q > s.len || s.q_begin < 0;
+  s.len = s.len < 0 ? 0 : min(s.len, cap);
+  s.n_q = s.n_q < 0 || s.q_begin < 0 ? 0 : min(s.n_q, s.len);
+  s.tiles = (int)min(((int64_t)s.n_q * a.group + bm - 1) / bm, (int64_t)a.n_qtiles);
+  s.pages = (s.len + 63) >> 6;
+  if (s.sa) {
+    const int64_t win = min((int64_t)a.win_blocks << a.blk_shift, (int64_t)s.len);
+    s.pages = min(s.pages, ((min(a.sink_lim, s.len) + 63) >> 6) + (int)((win + bm) >> 6) + 2);
+  }
+  return s;
+}
+
+// ---- the plan of a launch, taken on the device by every wave: which unit of work a workgroup is.  A unit is (sequence, KV head,
+// part, tile): part i of a tile has its pages [i * chunk, (i + 1) * chunk).  Where the tiles by themselves fill two thirds of
+// the chip or more, there is one part; otherwise chunk is the share that one of the resident workgroups has of all pages.
+// Units of one (KV head, part) walk the same pages; workgroups go to the 8 XCDs by id mod 8, each with an L2 of its own, so these
+// units get ids of one residue (or of 8 / groups residues).
+struct PagedUnit {
+  PagedSeq s;
+  int b, kvh, tile, part, chunk, unit, stride;   // b < 0: past the last unit; the tile's units are unit - part * stride + i * stride
+};
+__device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, int bm, const PagedSeq& first) {
+  if (a.part_units == 0) return kPagedNoSplit;
+  float tiles = 0.f, pages = 0.f;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const PagedSeq s = b0 == 0 ? first : paged_seq(a, b0 + l, bm);
+    tiles += (float)s.tiles;
+    pages += (float)s.tiles * (float)s.pages;
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    tiles += __shfl_xor(tiles, off);
+    pages += __shfl_xor(pages, off);
+  }
+  tiles *= (float)a.hkv;
+  pages *= (float)a.hkv;
+  if (3.f * tiles > 2.f * kPagedResident) return kPagedNoSplit;
+  int chunk = max(kPagedMinPages, (int)(pages * (1.0f / kPagedResident)) + 1);
+  // the units must fit the launch and the workspace (they do where both have their usual size)
+  for (;;) {
+    int units = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+      const PagedSeq s = b0 == 0 ? first : paged_seq(a, b0 + l, bm);
+      int n = s.tiles > 0 ? unit_count(a.hkv * ((s.pages + chunk - 1) / chunk), s.tiles) : 0;
+      n = wave_inclusive_sum(n);
+      units += __builtin_amdgcn_readlane(n, 63);
+    }
+    if (units <= min(a.n_wg, a.part_units)) return chunk;
+    if (chunk >= (1 << 25)) return kPagedNoSplit;
+    chunk *= 2;
+  }
+}
+__device__ __forceinline__ PagedSeq seq_from_lane(const PagedSeq& s, int i) {
+  PagedSeq r;
+  r.q_begin = __builtin_amdgcn_readlane(s.q_begin, i);
+  r.n_q = __builtin_amdgcn_readlane(s.n_q, i);
+  r.len = __builtin_amdgcn_readlane(s.len, i);
+  r.tiles = __builtin_amdgcn_readlane(s.tiles, i);
+  r.pages = __builtin_amdgcn_readlane(s.pages, i);
+  r.sa = __builtin_amdgcn_readlane((int)s.sa, i) != 0;
+  r.bad = false;
+  return r;
+}
+__device__ __forceinline__ PagedUnit paged_plan(const PagedPrefillArgs& a, int wg, int l, int bm) {
+  const PagedSeq first = paged_seq(a, l, bm);
+  PagedUnit u;
+  u.b = -1;
+  u.chunk = paged_chunk(a, l, bm, first);
+  int base = 0;
+  bool bad = false;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    const PagedSeq s = b0 == 0 ? first : paged_seq(a, b0 + l, bm);
+    bad |= s.bad;
+    const int parts = (s.pages + u.chunk - 1) / u.chunk;
+    const int incl = base + wave_inclusive_sum(s.tiles > 0 ? unit_count(a.hkv * parts, s.tiles) : 0);
+    const int end = __builtin_amdgcn_readlane(incl, 63);
+    if (u.b < 0 && wg < end) {                               // (uniform)
+      const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= wg));
+      u.s = seq_from_lane(s, at);
+      u.b = b0 + at;
+      const int n_parts = __builtin_amdgcn_readlane(parts, at), groups = a.hkv * n_parts, n_t = u.s.tiles;
+      const int before = __builtin_amdgcn_readlane(incl, at) - unit_count(groups, n_t), local = wg - before;
+      const int sh = share_shift(groups);
+      int grp, t;
+      if (sh > 0) {
+        grp = (local & 7) & (groups - 1);
+        t = ((local >> 3) << sh) + ((local & 7) >> (3 - sh));
+      } else if ((groups & 7) == 0) {
+        grp = ((local >> 3) / n_t) * 8 + (local & 7);
+        t = (local >> 3) % n_t;
+      } else {
+        grp = local / n_t;
+        t = local % n_t;
+      }
+      grp = __builtin_amdgcn_readfirstlane(grp);
+      t = __builtin_amdgcn_readfirstlane(t);
+      if (t >= n_t) {                                        // padding of the last round
+        u.b = -1;
+        return u;
+      }
+      u.part = grp / a.hkv;
+      u.kvh = grp - u.part * a.hkv;
+      u.tile = n_t - 1 - t;                                  // heaviest first
+      // rows of unit (kvh, part, tile) in the workspace: any numbering without gaps or clashes
+      u.unit = before + (u.part * a.hkv + u.kvh) * n_t + u.tile;
+      u.stride = a.hkv * n_t;
+    }
+    base = end;
+    if (u.b >= 0 && wg != 0) break;
+  }
+  if (wg == 0 && threadIdx.x < 64 && bad) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_LENGTH);
+  return u;
+}
+
+__device__ __forceinline__ u32x4 unpack8_scaled(uint32_t lo, uint32_t hi, float scale /*power of two*/) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
+}
+__device__ __forceinline__ u32x4 unpack8_rounded(uint32_t lo, uint32_t hi, float scale) {
+  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(lo, true);
+  const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+  return u32x4{pack_bf16(a[0] * scale, a[1] * scale), pack_bf16(b[0] * scale, b[1] * scale), pack_bf16(c[0] * scale, c[1] * scale),
+               pack_bf16(d[0] * scale, d[1] * scale)};
+}
+
+template <int D, int QB>
+__global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a) {
+  constexpr int WR = 16 * QB;             // query rows per wave
+  constexpr int BM = 4 * WR;              // query rows per workgroup
+  constexpr int KC = D / 32;              // MFMA k-steps over the head dimension (QK^T)
+  constexpr int DB = D / 16;              // 16-wide output blocks over the head dimension (PV)
+  constexpr int KB = 4;                   // 16-key blocks of S^T per page
+  constexpr int KS = 2;                   // 32-key steps of the PV product per page
+  constexpr int CPR = D / 16;             // 16-code chunks per row
+  constexpr int NS = 64 * CPR / 256;      // chunks of K, and of V, that a thread stages
+  constexpr int RPS = 256 / CPR;          // rows from one of them to the next
+  constexpr int ROWB = 2 * D;             // bytes per row in LDS
+  constexpr int TILE = 64 * ROWB;
+  constexpr int STAGE = 2 * TILE;         // K, V
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+
+  const int tid = threadIdx.x;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l = tid & 63;
+  const int g = l >> 4, n = l & 15;
+  const PagedUnit u = paged_plan(a, blockIdx.x, l, BM);
+  if (u.b < 0) return;                                       // uniform for the workgroup
+
+  // ---- rows and pages of the tile
+  const int rows = (int)min((int64_t)u.s.n_q * a.group - (int64_t)u.tile * BM, (int64_t)BM);
+  const int r0 = u.tile * BM;                                // (n_q * group may pass 2^31 only with tiles that the bound cuts)
+  const int pos0 = u.s.len - u.s.n_q;                        // position of the sequence's first query
+  const int i_min = pos0 + r0 / a.group, i_max = pos0 + (r0 + rows - 1) / a.group;
+  const int last = i_max >> 6;                               // the page of the last query
+  int seam = 0x7FFFFFFF, skip = 0;                           // list index x >= seam is page x + skip
+  if (u.s.sa) {
+    seam = min((int)(((int64_t)a.sink_lim + 63) >> 6), last + 1);
+    skip = max((window_start(i_min, a.blk_shift, a.win_blocks) >> 6) - seam, 0);
+  }
+  const int list = last + 1 - skip;
+  const int x0 = u.part * u.chunk;                           // (chunk < 2^30 / parts)
+  const int parts = (list + u.chunk - 1) / u.chunk;
+  const bool split = parts > 1;
+  if (a.part_units > 0 && u.part == 0 && tid == 0)
+    a.tile_info[((int64_t)u.b * a.hkv + u.kvh) * a.n_qtiles + u.tile] = i32x4{u.unit, u.stride, parts, 0};
+  if (u.part >= parts) return;                               // (the bound on the pages was above this tile's)
+  const int n_x = min(u.chunk, list - x0);                   // pages of this unit
+  const int32_t* const pages = a.table + (int64_t)u.b * a.table_pages;
+  auto page_at = [&](int x) __attribute__((always_inline)) { return x + (x >= seam ? skip : 0); };   // list index -> page of the sequence
+
+  // ---- what a lane knows of its rows: position and start of the window; rows past the last one repeat it
+  const int r_w0 = w * WR;
+  int i_mine[QB], w_lo_mine[QB];
+  bf16x8 qf[QB][KC];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int r = r0 + min(r_w0 + 16 * qb + n, rows - 1), tok = r / a.group, head = r - tok * a.group;
+    i_mine[qb] = pos0 + tok;
+    w_lo_mine[qb] = u.s.sa ? window_start(i_mine[qb], a.blk_shift, a.win_blocks) : 0;
+    const __bf16* qrow = a.q + ((int64_t)(u.s.q_begin + tok) * a.hq + (int64_t)u.kvh * a.group + head) * D;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) qf[qb][kc] = *(const bf16x8*)(qrow + 32 * kc + 8 * g);
+  }
+  const bool wave_active = r_w0 < rows;
+  const int i_w_min = pos0 + (r0 + min(r_w0, rows - 1)) / a.group, i_w_max = pos0 + (r0 + min(r_w0 + WR, rows) - 1) / a.group;
+  const int w_lo_first = u.s.sa ? window_start(i_w_min, a.blk_shift, a.win_blocks) : 0;
+  const int w_lo_last = u.s.sa ? window_start(i_w_max, a.blk_shift, a.win_blocks) : 0;
+
+  // ---- pages: lane i holds number and scales of the i-th page of 64
+  int ids, ids_next;
+  float ks, vs;
+  auto load_ids = [&](int x) __attribute__((always_inline)) { return pages[page_at(x0 + min(x + l, n_x - 1))]; };
+  auto load_scales = [&]() __attribute__((always_inline)) {
+    const int64_t page = (uint32_t)ids < (uint32_t)a.n_pages ? ids : 0;
+    ks = a.k_scale[page * a.hkv + u.kvh];
+    vs = a.v_scale[page * a.hkv + u.kvh];
+  };
+  const char* const kbase = a.k + (int64_t)u.kvh * a.stride_h;
+  const char* const vbase = a.v + (int64_t)u.kvh * a.stride_h;
+  u32x4 kcode[NS], vcode[NS];
+  bool there_loaded, there = false;                          // whether the page in registers / in LDS is in the pool
+  auto load_page = [&](int x) __attribute__((always_inline)) {   // x: page of this unit
+    if ((x & 63) == 0 && x > 0) {
+      ids = ids_next;
+      load_scales();
+      ids_next = load_ids(x + 64);
+    }
+    const int id = __builtin_amdgcn_readlane(ids, x & 63);
+    there_loaded = (uint32_t)id < (uint32_t)a.n_pages;
+    const int64_t off = (int64_t)(there_loaded ? id : 0) * a.stride_p;
+    // rows behind the length are not read: the last one stands in for them, with weight zero
+    const int row_max = u.s.len - 1 - (page_at(x0 + x) << 6);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const int at = min(i * RPS + tid / CPR, row_max) * (int)a.stride_t + 16 * (tid % CPR);
+      kcode[i] = *(const u32x4*)(kbase + off + at);
+      vcode[i] = *(const u32x4*)(vbase + off + at);
+    }
+  };
+  // K tile: 16-byte chunks XOR-swizzled by the row, V tile: 32-byte units likewise, as in prefill.hip
+  auto k_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 15 : (row >> 1) & 7; };
+  auto v_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 7 : (row >> 1) & 3; };
+  float k_staged = 0.f;                                      // scale of K of the page staged last
+  auto stage = [&](int x, FLUX_LDS char* st) __attribute__((always_inline)) {
+    k_staged = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), x & 63));
+    const uint32_t vbits = (uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), x & 63);
+    const float vsc = __builtin_bit_cast(float, vbits);
+    const bool exact = (vbits & 0x7FFFFF) == 0 && vbits != 0;
+    const int c = tid % CPR;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      const int row = i * RPS + tid / CPR;
+      FLUX_LDS char* const kr = st + row * ROWB;
+      *(FLUX_LDS u32x4*)(kr + ((2 * c) ^ k_swz(row)) * 16) = unpack8_scaled(kcode[i][0], kcode[i][1], 1.0f);
+      *(FLUX_LDS u32x4*)(kr + ((2 * c + 1) ^ k_swz(row)) * 16) = unpack8_scaled(kcode[i][2], kcode[i][3], 1.0f);
+      FLUX_LDS u32x4* const vr = (FLUX_LDS u32x4*)(st + TILE + row * ROWB + (c ^ v_swz(row)) * 32);
+      if (exact) {                                           // (uniform)
+        vr[0] = unpack8_scaled(vcode[i][0], vcode[i][1], vsc);
+        vr[1] = unpack8_scaled(vcode[i][2], vcode[i][3], vsc);
+      } else {
+        vr[0] = unpack8_rounded(vcode[i][0], vcode[i][1], vsc);
+        vr[1] = unpack8_rounded(vcode[i][2], vcode[i][3], vsc);
+      }
+    }
+    if (!there_loaded && tid == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
+  };
+
+  int k_rd[KC], v_rd[DB];
+#pragma unroll
+  for (int kc = 0; kc < KC; ++kc) k_rd[kc] = n * ROWB + ((4 * kc + g) ^ k_swz(n)) * 16;
+  const int v_row = 4 * g + (n >> 2);
+#pragma unroll
+  for (int db = 0; db < DB; ++db) v_rd[db] = TILE + v_row * ROWB + (db ^ v_swz(v_row)) * 32 + 8 * (n & 3);
+
+  // ---- accumulators.  A row's reference is -1e30 until it sees a key.
+  float m_ref[QB], l_run[QB];
+  f32x4 o[DB][QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    m_ref[qb] = -1e30f;
+    l_run[qb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  ids = load_ids(0);
+  ids_next = load_ids(64);
+  load_page(0);
+  load_scales();
+  stage(0, (FLUX_LDS char*)smem);
+  float k_now = k_staged;
+  there = there_loaded;
+  if (n_x > 1) load_page(1);
+  __syncthreads();
+
+  auto iteration = [&](int x, auto stg_c) __attribute__((always_inline)) {
+    constexpr int STG = decltype(stg_c)::value;
+    FLUX_LDS char* const st = (FLUX_LDS char*)smem + STG * STAGE;
+    const float c = fmaxf(a.scale_log2 * k_now, 0x1p-126f);  // (not 0: a masked score is -inf times this)
+    const bool here = there;
+    if (x + 1 < n_x) {                                       // the next page into the other stage, the one behind it from memory
+      stage(x + 1, (FLUX_LDS char*)smem + (STG ^ 1) * STAGE);
+      k_now = k_staged;
+      there = there_loaded;
+      if (x + 2 < n_x) load_page(x + 2);
+    }
+    const int j0 = page_at(x0 + x) << 6;
+    bool hidden = !here || !wave_active || j0 > i_w_max;
+    const bool all_sink = j0 + 64 <= a.sink_lim;
+    hidden |= u.s.sa && j0 >= a.sink_lim && j0 + 63 < w_lo_first;
+    if (!hidden) {
+      const bool causal = j0 + 63 > i_w_min, edge = u.s.sa && !all_sink && j0 < w_lo_last;
+      f32x4 s[KB][QB];
+      bf16x8 pf[QB][KS];
+      if (causal || edge) {
+        // element masks are put into the accumulators that the scores start from: key j0 + 4 g + c, c a constant
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          const int hi = i_mine[qb] - j0 - 4 * g, lo = w_lo_mine[qb] - j0 - 4 * g, sl = a.sink_lim - j0 - 4 * g;
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int k = 16 * kb + i;
+              s[kb][qb][i] = (k <= hi) & ((k < sl) | (k >= lo)) ? 0.f : -INFINITY;
+            }
+        }
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) s[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) {
+          const bf16x8 kf = *(FLUX_LDS bf16x8*)(st + k_rd[kc] + 16 * kb * ROWB);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qb][kc], s[kb][qb], 0, 0, 0);
+        }
+      float l_page[QB];
+      auto weights = [&]() __attribute__((always_inline)) {
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          l_page[qb] = 0.f;
+#pragma unroll
+          for (int h = 0; h < KS; ++h) {
+            uint32_t pk[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const f32x4& sv = s[2 * h + (t >> 1)][qb];
+              pk[t] = pack_bf16(fast_exp2(__builtin_fmaf(sv[2 * (t & 1)], c, -m_ref[qb])), fast_exp2(__builtin_fmaf(sv[2 * (t & 1) + 1], c, -m_ref[qb])));
+              l_page[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[t]), ones, l_page[qb], false);
+            }
+            pf[qb][h] = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
+          }
+        }
+      };
+      weights();
+      if (__builtin_amdgcn_ballot_w64(!(l_page[0] < kPagedGuard) | !(l_page[QB - 1] < kPagedGuard)) != 0) {
+        // a row without a reference, or a weight that has left the guarded range: the rows that have one of 2^31 and more (which
+        // trips the guard by itself, so that a row does not depend on those that share its wave) move the reference there
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+          float m = s[0][qb][0];
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = fmaxf(m, s[kb][qb][i]);
+          m = fmaxf(m, __shfl_xor(m, 16));
+          m = fmaxf(m, __shfl_xor(m, 32)) * c;
+          const bool moves = m - m_ref[qb] >= 31.f;
+          const float m_new = moves ? m : m_ref[qb];
+          const float al = fast_exp2(m_ref[qb] - m_new);
+          m_ref[qb] = m_new;
+          l_run[qb] *= al;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) o[db][qb] *= al;
+        }
+        weights();
+      }
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) l_run[qb] += l_page[qb];
+#pragma unroll
+      for (int h = 0; h < KS; ++h)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          FLUX_LDS char* const vp = st + v_rd[db] + 32 * h * ROWB;
+          const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)vp);
+          const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)(vp + 16 * ROWB));
+          const bf16x8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qb][h], o[db][qb], 0, 0, 0);
+        }
+    }
+    __syncthreads();                                         // this stage is free, and the other one written
+  };
+  for (int x = 0; x < n_x; x += 2) {
+    iteration(x, std::integral_constant<int, 0>());
+    if (x + 1 < n_x) iteration(x + 1, std::integral_constant<int, 1>());
+  }
+
+  // ---- lane (n, g) holds d = 16 * db + 4 * g .. +3 of its rows
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    float l_tot = l_run[qb];
+    l_tot += __shfl_xor(l_tot, 16);
+    l_tot += __shfl_xor(l_tot, 32);
+    const int x = r_w0 + 16 * qb + n;
+    if (x >= rows) continue;
+    if (split) {
+      const int64_t row = (int64_t)u.unit * BM + x;
+      if (g == 0) *(f32x2*)(a.part_ml + 2 * row) = f32x2{m_ref[qb], l_tot};
+#pragma unroll
+      for (int db = 0; db < DB; ++db) *(f32x4*)(a.part_o + row * D + 16 * db + 4 * g) = o[db][qb];
+      continue;
+    }
+    const float inv = l_tot > 0.f || l_tot != l_tot ? 1.0f / l_tot : 0.f;   // (no key there: a row of zeros)
+    const int r = r0 + x, tok = r / a.group, head = r - tok * a.group;
+    const int64_t off = ((int64_t)(u.s.q_begin + tok) * a.hq + (int64_t)u.kvh * a.group + head) * D + 4 * g;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const f32x4 y = o[db][qb] * inv;
+      if (a.out_fp32) *(f32x4*)((float*)a.out + off + 16 * db) = y;
+      else *(u32x2*)((__bf16*)a.out + off + 16 * db) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    }
+  }
+}
+
+// The merge of the units of a tile: out = sum_i w_i O_i / sum_i w_i l_i, w_i = 2^(m_i - max m).  D / 4 lanes per row, four columns
+// each; a workgroup takes rows of one tile, and as many tiles as there are for it.
+struct PagedMergeArgs {
+  const int32_t *cu_q, *kv_len;
+  const float *part_o, *part_ml;
+  const i32x4* tile_info;
+  int batch, hq, hkv, group, n_qtiles, bm, capacity, out_fp32;
+  void* out;
+};
+template <int D>
+__global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
+  constexpr int TPR = D / 4, RPW = 256 / TPR;                // rows that a workgroup has in work
+  const int groups = a.bm / RPW;
+  const long long items = (long long)a.batch * a.hkv * a.n_qtiles * groups;
+  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+    const int rg = (int)(it % groups);
+    const int64_t t = it / groups;
+    const int tile = (int)(t % a.n_qtiles), kvh = (int)(t / a.n_qtiles % a.hkv), b = (int)(t / a.n_qtiles / a.hkv);
+    const int q_begin = a.cu_q[b];
+    int n_q = a.cu_q[b + 1] - q_begin, len = a.kv_len[b];
+    len = len < 0 ? 0 : min(len, a.capacity);
+    n_q = n_q < 0 || q_begin < 0 ? 0 : min(n_q, len);
+    const int64_t rows = min((int64_t)n_q * a.group - (int64_t)tile * a.bm, (int64_t)a.bm);
+    const int x = rg * RPW + threadIdx.x / TPR, d = 4 * (threadIdx.x % TPR);
+    if (rg * RPW >= rows) continue;                          // (no such tile: what its entry holds is not read)
+    const i32x4 info = a.tile_info[t];
+    if (info[2] < 2 || x >= rows) continue;
+    float m = -INFINITY, den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < info[2]; i0 += 8) {
+      f32x2 ml[8];
+      f32x4 o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t row = (int64_t)(info[0] + min(i0 + i, info[2] - 1) * info[1]) * a.bm + x;
+        ml[i] = *(const f32x2*)(a.part_ml + 2 * row);
+        o[i] = *(const f32x4*)(a.part_o + row * D + d);
+      }
+      float m_new = m;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m_new = fmaxf(m_new, ml[i][0]);
+      const float al = fast_exp2(m - m_new);                 // 0 for the first ones (every reference is -1e30 at least)
+      num *= al;
+      den *= al;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float wgt = i0 + i < info[2] ? fast_exp2(ml[i][0] - m_new) : 0.f;
+        num += wgt * o[i];
+        den += wgt * ml[i][1];
+      }
+      m = m_new;
+    }
+    const float inv = den > 0.f || den != den ? 1.0f / den : 0.f;
+    const int r = tile * a.bm + x, tok = r / a.group, head = r - tok * a.group;
+    const int64_t off = ((int64_t)(q_begin + tok) * a.hq + (int64_t)kvh * a.group + head) * D + d;
+    const f32x4 y = num * inv;
+    if (a.out_fp32) *(f32x4*)((float*)a.out + off) = y;
+    else *(u32x2*)((__bf16*)a.out + off) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+  }
+}
+
+hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
+                                const flux_paged_kv& kv, const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s) {
+  const PagedPrefillPlan plan = plan_prefill_paged(cfg, pt.batch, max_q_len, max_kv_len, c.partials_bytes);
+  if (plan.tiles == 0) return hipSuccess;
+  PagedPrefillArgs a;
+  a.q = (const __bf16*)q;
+  a.cu_q = cu_q;
+  a.k = (const char*)kv.k;
+  a.v = (const char*)kv.v;
+  a.k_scale = kv.k_scale;
+  a.v_scale = kv.v_scale;
+  a.stride_p = kv.stride_p;
+  a.stride_h = kv.stride_h;
+  a.stride_t = kv.stride_t;
+  a.table = pt.table;
+  a.table_pages = pt.table_pages;
+  a.n_pages = kv.n_pages;
+  a.kv_len = pt.kv_len;
+  a.mode = mode;
+  a.hq = cfg.n_q_heads;
+  a.hkv = cfg.n_kv_heads;
+  a.group = cfg.n_q_heads / cfg.n_kv_heads;
+  a.batch = pt.batch;
+  const SaGeom geom = sa_geom(cfg);
+  a.sink_lim = geom.sink_lim;
+  a.win_blocks = geom.win_blocks;
+  a.blk_shift = geom.shift;
+  a.n_qtiles = plan.tiles;
+  a.n_wg = (int)plan.wgs;
+  a.scale_log2 = (cfg.softmax_scale != 0.f ? cfg.softmax_scale : 1.0f / sqrtf((float)cfg.head_dim)) * kLog2e;
+  a.out_fp32 = cfg.out_dtype;
+  a.out = out;
+  a.status = c.status;
+  a.part_units = plan.part_units;
+  a.tile_info = (i32x4*)c.partials;
+  a.part_o = (float*)((char*)c.partials + plan.info_bytes);
+  a.part_ml = a.part_o + (size_t)plan.part_units * plan.bm * cfg.head_dim;
+  const dim3 grid((unsigned)plan.wgs), block(256);
+  if (cfg.head_dim == 128) {
+    if (plan.bm == 128) hipLaunchKernelGGL((paged_prompt_kernel<128, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_prompt_kernel<128, 1>), grid, block, 0, s, a);
+  } else {
+    if (plan.bm == 128) hipLaunchKernelGGL((paged_prompt_kernel<64, 2>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_prompt_kernel<64, 1>), grid, block, 0, s, a);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.part_units == 0) return e;
+  PagedMergeArgs m;
+  m.cu_q = cu_q;
+  m.kv_len = pt.kv_len;
+  m.part_o = a.part_o;
+  m.part_ml = a.part_ml;
+  m.tile_info = a.tile_info;
+  m.batch = pt.batch;
+  m.hq = a.hq;
+  m.hkv = a.hkv;
+  m.group = a.group;
+  m.n_qtiles = plan.tiles;
+  m.bm = plan.bm;
+  m.capacity = pt.table_pages * kPageTokens;
+  m.out_fp32 = a.out_fp32;
+  m.out = out;
+  const long long items = (long long)pt.batch * a.hkv * plan.tiles * (plan.bm / (1024 / cfg.head_dim));
+  const dim3 mgrid((unsigned)(items < 2048 ? items : 2048));
+  if (cfg.head_dim == 128) hipLaunchKernelGGL(paged_prompt_merge<128>, mgrid, block, 0, s, m);
+  else hipLaunchKernelGGL(paged_prompt_merge<64>, mgrid, block, 0, s, m);
+  return hipGetLastError();
+}
+
+}  // namespace flux
