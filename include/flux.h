@@ -353,7 +353,7 @@ int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* 
 
 /* flux_attn_prefill over a paged 8-bit cache: q, cu_q, max_q_len, max_kv_len, mode, out as there (the queries of sequence b are the
  * last n_q(b) positions of its pages: flux_page_plan and flux_kv_append_paged first); keys and values are code * scale (any
- * finite scale >= 0; a scale of V that is not a power of two rounds its values to bf16).  A tile of query rows holds all heads
+ * finite scale >= 0; one of V below 2^-126 counts as that).  A tile of query rows holds all heads
  * of a group, token by token, and walks only pages of which a row sees something; pages of a tile may be shared out over several
  * workgroups where max_kv_len >= 1024, as far as the workspace has room for their results (any context will do), in a way that
  * depends on the bounds, lengths and modes of the whole batch.  max_q_len * group <= 2^30, and

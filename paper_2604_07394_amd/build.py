@@ -19,7 +19,7 @@ FLUX_SOURCES = ["flux_api.hip", "kv_append.hip", "decode.hip", "prefill.hip", "r
                 "decode_paged.hip", "prefill_paged.hip"]
 # Regions whose branches are the same for all lanes are left as they are written: the compiler structurises them by default, and
 # the loops of the prefill kernels then take up to seven branches per block and hold 20 registers more.
-SOURCE_FLAGS = {"prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"]}
+SOURCE_FLAGS = {"prefill_paged.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"], "prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"]}
 
 
 def _run(cmd):

@@ -11,8 +11,8 @@
 //
 // Codes become bf16 on their way into LDS: once per workgroup and page.  (In the waves' registers, behind the LDS reads, each of
 // the four waves would convert every code.)  A page's codes are asked for an iteration ahead of that, two ahead of their use.  The
-// scale of K goes into the exponent's factor, that of V into the conversion: exact for powers of two, which the append
-// writes; any other scale rounds V * scale to bf16, 2^-9 of it at most.
+// scale of K goes into the exponent's factor, the power of two of V's into the conversion and what is left of it into the weights:
+// nothing of K and V is rounded.
 //
 // Where the tiles do not fill the chip their pages are shared out over several workgroups, whose unnormalised rows a second
 // launch merges (see paged_plan).
@@ -84,6 +84,8 @@ struct PagedUnit {
   PagedSeq s;
   int b, kvh, tile, part, chunk, unit, stride;   // b < 0: past the last unit; the tile's units are unit - part * stride + i * stride
 };
+// (values that are the same in all lanes, where the compiler cannot know it)
+__device__ __forceinline__ float first_lane(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, int bm, const PagedSeq& first) {
   if (a.part_units == 0) return kPagedNoSplit;
   float tiles = 0.f, pages = 0.f;
@@ -97,10 +99,10 @@ __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, int
     tiles += __shfl_xor(tiles, off);
     pages += __shfl_xor(pages, off);
   }
-  tiles *= (float)a.hkv;
-  pages *= (float)a.hkv;
+  tiles = first_lane(tiles) * (float)a.hkv;
+  pages = first_lane(pages) * (float)a.hkv;
   if (3.f * tiles > 2.f * kPagedResident) return kPagedNoSplit;
-  int chunk = max(kPagedMinPages, (int)(pages * (1.0f / kPagedResident)) + 1);
+  int chunk = __builtin_amdgcn_readfirstlane(max(kPagedMinPages, (int)(pages * (1.0f / kPagedResident)) + 1));
   // the units must fit the launch and the workspace (they do where both have their usual size)
   for (;;) {
     int units = 0;
@@ -163,7 +165,7 @@ __device__ __forceinline__ PagedUnit paged_plan(const PagedPrefillArgs& a, int w
         u.b = -1;
         return u;
       }
-      u.part = grp / a.hkv;
+      u.part = __builtin_amdgcn_readfirstlane(grp / a.hkv);
       u.kvh = grp - u.part * a.hkv;
       u.tile = n_t - 1 - t;                                  // heaviest first
       // rows of unit (kvh, part, tile) in the workspace: any numbering without gaps or clashes
@@ -183,13 +185,6 @@ __device__ __forceinline__ u32x4 unpack8_scaled(uint32_t lo, uint32_t hi, float 
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
 }
-__device__ __forceinline__ u32x4 unpack8_rounded(uint32_t lo, uint32_t hi, float scale) {
-  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(lo, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(lo, true);
-  const f32x2 c = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), d = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-  return u32x4{pack_bf16(a[0] * scale, a[1] * scale), pack_bf16(b[0] * scale, b[1] * scale), pack_bf16(c[0] * scale, c[1] * scale),
-               pack_bf16(d[0] * scale, d[1] * scale)};
-}
-
 template <int D, int QB>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a) {
   constexpr int WR = 16 * QB;             // query rows per wave
@@ -217,7 +212,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int rows = (int)min((int64_t)u.s.n_q * a.group - (int64_t)u.tile * BM, (int64_t)BM);
   const int r0 = u.tile * BM;                                // (n_q * group may pass 2^31 only with tiles that the bound cuts)
   const int pos0 = u.s.len - u.s.n_q;                        // position of the sequence's first query
-  const int i_min = pos0 + r0 / a.group, i_max = pos0 + (r0 + rows - 1) / a.group;
+  auto token_of = [&](int r) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(r / a.group); };   // (r: uniform)
+  const int i_min = pos0 + token_of(r0), i_max = pos0 + token_of(r0 + rows - 1);
   const int last = i_max >> 6;                               // the page of the last query
   int seam = 0x7FFFFFFF, skip = 0;                           // list index x >= seam is page x + skip
   if (u.s.sa) {
@@ -226,7 +222,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   }
   const int list = last + 1 - skip;
   const int x0 = u.part * u.chunk;                           // (chunk < 2^30 / parts)
-  const int parts = (list + u.chunk - 1) / u.chunk;
+  const int parts = __builtin_amdgcn_readfirstlane((list + u.chunk - 1) / u.chunk);
   const bool split = parts > 1;
   if (a.part_units > 0 && u.part == 0 && tid == 0)
     a.tile_info[((int64_t)u.b * a.hkv + u.kvh) * a.n_qtiles + u.tile] = i32x4{u.unit, u.stride, parts, 0};
@@ -249,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
     for (int kc = 0; kc < KC; ++kc) qf[qb][kc] = *(const bf16x8*)(qrow + 32 * kc + 8 * g);
   }
   const bool wave_active = r_w0 < rows;
-  const int i_w_min = pos0 + (r0 + min(r_w0, rows - 1)) / a.group, i_w_max = pos0 + (r0 + min(r_w0 + WR, rows) - 1) / a.group;
+  const int i_w_min = pos0 + token_of(r0 + min(r_w0, rows - 1)), i_w_max = pos0 + token_of(r0 + min(r_w0 + WR, rows) - 1);
   const int w_lo_first = u.s.sa ? window_start(i_w_min, a.blk_shift, a.win_blocks) : 0;
   const int w_lo_last = u.s.sa ? window_start(i_w_max, a.blk_shift, a.win_blocks) : 0;
 
@@ -265,6 +261,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const char* const kbase = a.k + (int64_t)u.kvh * a.stride_h;
   const char* const vbase = a.v + (int64_t)u.kvh * a.stride_h;
   u32x4 kcode[NS], vcode[NS];
+  const int st_at = (tid / CPR) * (int)a.stride_t + 16 * (tid % CPR);
   bool there_loaded, there = false;                          // whether the page in registers / in LDS is in the pool
   auto load_page = [&](int x) __attribute__((always_inline)) {   // x: page of this unit
     if ((x & 63) == 0 && x > 0) {
@@ -277,47 +274,52 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
     const int64_t off = (int64_t)(there_loaded ? id : 0) * a.stride_p;
     // rows behind the length are not read: the last one stands in for them, with weight zero
     const int row_max = u.s.len - 1 - (page_at(x0 + x) << 6);
+    const char *const kp = kbase + off, *const vp = vbase + off;
+    if (row_max >= 63) {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const int at = min(i * RPS + tid / CPR, row_max) * (int)a.stride_t + 16 * (tid % CPR);
-      kcode[i] = *(const u32x4*)(kbase + off + at);
-      vcode[i] = *(const u32x4*)(vbase + off + at);
-    }
-  };
-  // K tile: 16-byte chunks XOR-swizzled by the row, V tile: 32-byte units likewise, as in prefill.hip
-  auto k_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 15 : (row >> 1) & 7; };
-  auto v_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 7 : (row >> 1) & 3; };
-  float k_staged = 0.f;                                      // scale of K of the page staged last
-  auto stage = [&](int x, FLUX_LDS char* st) __attribute__((always_inline)) {
-    k_staged = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), x & 63));
-    const uint32_t vbits = (uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), x & 63);
-    const float vsc = __builtin_bit_cast(float, vbits);
-    const bool exact = (vbits & 0x7FFFFF) == 0 && vbits != 0;
-    const int c = tid % CPR;
+      for (int i = 0; i < NS; ++i) {
+        kcode[i] = *(const u32x4*)(kp + i * RPS * a.stride_t + st_at);
+        vcode[i] = *(const u32x4*)(vp + i * RPS * a.stride_t + st_at);
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const int row = i * RPS + tid / CPR;
-      FLUX_LDS char* const kr = st + row * ROWB;
-      *(FLUX_LDS u32x4*)(kr + ((2 * c) ^ k_swz(row)) * 16) = unpack8_scaled(kcode[i][0], kcode[i][1], 1.0f);
-      *(FLUX_LDS u32x4*)(kr + ((2 * c + 1) ^ k_swz(row)) * 16) = unpack8_scaled(kcode[i][2], kcode[i][3], 1.0f);
-      FLUX_LDS u32x4* const vr = (FLUX_LDS u32x4*)(st + TILE + row * ROWB + (c ^ v_swz(row)) * 32);
-      if (exact) {                                           // (uniform)
-        vr[0] = unpack8_scaled(vcode[i][0], vcode[i][1], vsc);
-        vr[1] = unpack8_scaled(vcode[i][2], vcode[i][3], vsc);
-      } else {
-        vr[0] = unpack8_rounded(vcode[i][0], vcode[i][1], vsc);
-        vr[1] = unpack8_rounded(vcode[i][2], vcode[i][3], vsc);
+      for (int i = 0; i < NS; ++i) {
+        const int at = min(i * RPS + tid / CPR, row_max) * (int)a.stride_t + 16 * (tid % CPR);
+        kcode[i] = *(const u32x4*)(kp + at);
+        vcode[i] = *(const u32x4*)(vp + at);
       }
     }
+  };
+  // K tile: 16-byte chunks XOR-swizzled by the row.  V tile: 32-byte units likewise (both as in prefill.hip), and of a unit the
+  // two halves change places in every other row of a bank's, so that a wave's stores of first halves meet all banks.
+  auto k_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 15 : (row >> 1) & 7; };
+  auto v_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 7 : (row >> 1) & 3; };
+  auto v_half = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 1 : (row >> 1) & 1; };
+  const int st_row = tid / CPR, st_c = tid % CPR;            // (the rows that a thread stages are 32 or 64 apart: the same swizzle)
+  const int k_wr = st_row * ROWB + ((2 * st_c) ^ k_swz(st_row)) * 16, v_wr = TILE + st_row * ROWB + (st_c ^ v_swz(st_row)) * 32 + 16 * v_half(st_row);
+  // The page in registers becomes bf16 in LDS, in 4 NS steps of 8 codes.  The scale of V: its power of two goes into
+  // the conversion, which is exact; the rest, 1 <= r < 2, into the weights.
+  float k_staged = 0.f, v_rest_staged = 1.f, v_power;        // of the page staged last
+  auto begin_stage = [&](int x) __attribute__((always_inline)) {
+    k_staged = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), x & 63));
+    const uint32_t bits = max((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), x & 63), 0x00800000u);
+    v_power = __builtin_bit_cast(float, bits & 0x7F800000u);
+    v_rest_staged = __builtin_bit_cast(float, (bits & 0x007FFFFFu) | 0x3F800000u);
     if (!there_loaded && tid == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
   };
+  auto stage_step = [&](int j, FLUX_LDS char* st) __attribute__((always_inline)) {
+    const int i = (j >> 1) % NS, h = j & 1;                  // chunk of the thread, half of the chunk
+    if (j < 2 * NS) *(FLUX_LDS u32x4*)(st + (k_wr ^ (16 * h)) + i * RPS * ROWB) = unpack8_scaled(kcode[i][2 * h], kcode[i][2 * h + 1], 1.0f);
+    else *(FLUX_LDS u32x4*)(st + (v_wr ^ (16 * h)) + i * RPS * ROWB) = unpack8_scaled(vcode[i][2 * h], vcode[i][2 * h + 1], v_power);
+  };
+  static_assert(4 * NS == DB, "a step of the staging for every output block");
 
   int k_rd[KC], v_rd[DB];
 #pragma unroll
   for (int kc = 0; kc < KC; ++kc) k_rd[kc] = n * ROWB + ((4 * kc + g) ^ k_swz(n)) * 16;
   const int v_row = 4 * g + (n >> 2);
 #pragma unroll
-  for (int db = 0; db < DB; ++db) v_rd[db] = TILE + v_row * ROWB + (db ^ v_swz(v_row)) * 32 + 8 * (n & 3);
+  for (int db = 0; db < DB; ++db) v_rd[db] = TILE + v_row * ROWB + (db ^ v_swz(v_row)) * 32 + ((8 * (n & 3)) ^ (16 * v_half(v_row)));
 
   // ---- accumulators.  A row's reference is -1e30 until it sees a key.
   float m_ref[QB], l_run[QB];
@@ -334,8 +336,10 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   ids_next = load_ids(64);
   load_page(0);
   load_scales();
-  stage(0, (FLUX_LDS char*)smem);
-  float k_now = k_staged;
+  begin_stage(0);
+#pragma unroll
+  for (int j = 0; j < DB; ++j) stage_step(j, (FLUX_LDS char*)smem);
+  float k_now = k_staged, v_rest = v_rest_staged;
   there = there_loaded;
   if (n_x > 1) load_page(1);
   __syncthreads();
@@ -345,20 +349,32 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
     FLUX_LDS char* const st = (FLUX_LDS char*)smem + STG * STAGE;
     const float c = fmaxf(a.scale_log2 * k_now, 0x1p-126f);  // (not 0: a masked score is -inf times this)
     const bool here = there;
-    if (x + 1 < n_x) {                                       // the next page into the other stage, the one behind it from memory
-      stage(x + 1, (FLUX_LDS char*)smem + (STG ^ 1) * STAGE);
-      k_now = k_staged;
-      there = there_loaded;
-      if (x + 2 < n_x) load_page(x + 2);
-    }
+    const bool more = x + 1 < n_x;                           // the next page goes into the other stage, the one behind it is asked for
+    FLUX_LDS char* const st_next = (FLUX_LDS char*)smem + (STG ^ 1) * STAGE;
+    const float log_rest = v_rest == 1.f ? 0.f : __builtin_amdgcn_logf(v_rest), inv_rest = 1.0f / v_rest;
     const int j0 = page_at(x0 + x) << 6;
     bool hidden = !here || !wave_active || j0 > i_w_max;
     const bool all_sink = j0 + 64 <= a.sink_lim;
     hidden |= u.s.sa && j0 >= a.sink_lim && j0 + 63 < w_lo_first;
+    if (more) begin_stage(x + 1);
     if (!hidden) {
       const bool causal = j0 + 63 > i_w_min, edge = u.s.sa && !all_sink && j0 < w_lo_last;
       f32x4 s[KB][QB];
-      bf16x8 pf[QB][KS];
+      bf16x8 pf[QB][KS], kf[KB][KC], vf[KS][DB];
+      auto read_k = [&](int kb, int kc) __attribute__((always_inline)) { kf[kb][kc] = *(FLUX_LDS bf16x8*)(st + k_rd[kc] + 16 * kb * ROWB); };
+      auto read_v = [&](int h, int db) __attribute__((always_inline)) {
+        FLUX_LDS char* const vp = st + v_rd[db] + 32 * h * ROWB;
+        const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)vp);
+        const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)(vp + 16 * ROWB));
+        vf[h][db] = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      // wave priorities as in prefill.hip: the second product above the scores, those above the softmax and the staging
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) read_k(kb, kc);
+      __builtin_amdgcn_sched_barrier(0);
       if (causal || edge) {
         // element masks are put into the accumulators that the scores start from: key j0 + 4 g + c, c a constant
 #pragma unroll
@@ -378,27 +394,41 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) s[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
+      // S^T of keys 0..31 with the K fragments of keys 32..63 read between the MFMAs, then S^T of keys 32..63 with the V
+      // fragments of keys 0..31 read between them
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+      for (int t = 0; t < 2 * KC; ++t) {
+        const int kc = t >> 1, kb = t & 1;
 #pragma unroll
-        for (int kc = 0; kc < KC; ++kc) {
-          const bf16x8 kf = *(FLUX_LDS bf16x8*)(st + k_rd[kc] + 16 * kb * ROWB);
+        for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][kc], qf[qb][kc], s[kb][qb], 0, 0, 0);
+        read_k(2 + kb, kc);
+        __builtin_amdgcn_sched_barrier(0);
+      }
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qb][kc], s[kb][qb], 0, 0, 0);
-        }
+      for (int t = 0; t < 2 * KC; ++t) {
+        const int kc = t >> 1, kb = 2 + (t & 1);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][kc], qf[qb][kc], s[kb][qb], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) read_v(0, db);
+      __builtin_amdgcn_sched_barrier(0);
       float l_page[QB];
       auto weights = [&]() __attribute__((always_inline)) {
         const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
           l_page[qb] = 0.f;
+          const float shift = log_rest - m_ref[qb];
 #pragma unroll
           for (int h = 0; h < KS; ++h) {
             uint32_t pk[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
               const f32x4& sv = s[2 * h + (t >> 1)][qb];
-              pk[t] = pack_bf16(fast_exp2(__builtin_fmaf(sv[2 * (t & 1)], c, -m_ref[qb])), fast_exp2(__builtin_fmaf(sv[2 * (t & 1) + 1], c, -m_ref[qb])));
+              pk[t] = pack_bf16(fast_exp2(__builtin_fmaf(sv[2 * (t & 1)], c, shift)), fast_exp2(__builtin_fmaf(sv[2 * (t & 1) + 1], c, shift)));
               l_page[qb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[t]), ones, l_page[qb], false);
             }
             pf[qb][h] = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
@@ -429,18 +459,41 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
         weights();
       }
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) l_run[qb] += l_page[qb];
+      for (int qb = 0; qb < QB; ++qb) l_run[qb] = __builtin_fmaf(l_page[qb], inv_rest, l_run[qb]);
+      __builtin_amdgcn_s_setprio(2);
+      __builtin_amdgcn_sched_barrier(0);
+      // O^T += keys 0..31 with the V fragments of keys 32..63 read between the MFMAs
 #pragma unroll
-      for (int h = 0; h < KS; ++h)
+      for (int db = 0; db < DB; ++db) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[0][db], pf[qb][0], o[db][qb], 0, 0, 0);
+        read_v(1, db);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // and those of keys 32..63 with the staging of the next page between them
+      auto second = [&](auto stages) __attribute__((always_inline)) {
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          FLUX_LDS char* const vp = st + v_rd[db] + 32 * h * ROWB;
-          const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)vp);
-          const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)(vp + 16 * ROWB));
-          const bf16x8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qb][h], o[db][qb], 0, 0, 0);
+          for (int qb = 0; qb < QB; ++qb) o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[1][db], pf[qb][1], o[db][qb], 0, 0, 0);
+          if constexpr (decltype(stages)::value) {
+            stage_step(db, st_next);
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
+      };
+      if (more) second(std::true_type());
+      else second(std::false_type());
+      __builtin_amdgcn_s_setprio(0);
+    } else if (more) {
+#pragma unroll
+      for (int j = 0; j < DB; ++j) stage_step(j, st_next);
+    }
+    if (more) {
+      k_now = k_staged;
+      v_rest = v_rest_staged;
+      there = there_loaded;
+      if (x + 2 < n_x) load_page(x + 2);
     }
     __syncthreads();                                         // this stage is free, and the other one written
   };
