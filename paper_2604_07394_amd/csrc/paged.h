@@ -46,9 +46,10 @@ inline PagedPrefillPlan plan_prefill_paged(const flux_attn_cfg& cfg, int batch, 
   p.tiles = (int)((rows + p.bm - 1) / p.bm);
   p.wgs = (long long)batch * unit_count(cfg.n_kv_heads, p.tiles);
   p.part_units = 0;
-  p.info_bytes = ((size_t)batch * cfg.n_kv_heads * p.tiles * 16 + 255) / 256 * 256;
-  // worth a second launch where lists may be long and tiles few (in a batch, only the device knows how few)
-  if (pages_of(max_kv_len) >= 2 * kPagedMinPages && (batch > 1 || 3 * p.wgs <= 2 * kPagedResident) && p.info_bytes <= partials_bytes / 4) {
+  p.info_bytes = (((size_t)batch * cfg.n_kv_heads * p.tiles + 1) * 16 + 255) / 256 * 256;
+  // worth a second launch where lists may be long and tiles few (the tiles of the longest run of queries are, and the device knows
+  // the others)
+  if (batch <= 64 && pages_of(max_kv_len) >= 2 * kPagedMinPages && 3ll * cfg.n_kv_heads * p.tiles <= 2 * kPagedResident && p.info_bytes <= partials_bytes / 4) {
     const size_t fit = (partials_bytes - p.info_bytes) / ((size_t)p.bm * (cfg.head_dim + 2) * sizeof(float));
     const size_t want = 2 * kPagedResident + (size_t)8 * batch;
     p.part_units = (int)(fit < want ? fit : want);

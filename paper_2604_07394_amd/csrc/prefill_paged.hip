@@ -10,7 +10,7 @@
 // group), so that short runs of queries fill their tiles and K and V are read once per group.
 //
 // Codes become bf16 on their way into LDS: once per workgroup and page.  (In the waves' registers, behind the LDS reads, each of
-// the four waves would convert every code.)  A page's codes are asked for an iteration ahead of that, two ahead of their use.  The
+// the four waves would convert every code.)  A page's codes are asked for one or two iterations ahead of that.  The
 // scale of K goes into the exponent's factor, the power of two of V's into the conversion and what is left of it into the weights:
 // nothing of K and V is rounded.
 //
@@ -45,7 +45,7 @@ struct PagedPrefillArgs {
   int part_units;         // units whose rows the workspace holds; 0: tiles are never shared out
   float* part_o;          // unnormalised rows of a unit [unit][BM][D]
   float* part_ml;         // their reference (log2 units) and weight sum [unit][BM][2]
-  i32x4* tile_info;       // [batch][hkv][n_qtiles]: first unit, unit stride, units of the tile
+  i32x4* tile_info;       // whether tiles are shared out; behind it, [batch][hkv][n_qtiles]: first unit, unit stride, units of the tile
 };
 
 constexpr float kPagedGuard = 1073741824.0f;  // 2^30: a page whose weights sum past this moves the reference
@@ -77,23 +77,24 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedPrefillArgs& a, int b, 
 
 // ---- the plan of a launch, taken on the device by every wave: which unit of work a workgroup is.  A unit is (sequence, KV head,
 // part, tile): part i of a tile has its pages [i * chunk, (i + 1) * chunk).  Where the tiles by themselves fill two thirds of
-// the chip or more, there is one part; otherwise chunk is the share that one of the resident workgroups has of all pages.
+// the chip or more, there is one part; otherwise see paged_chunk.
 // Units of one (KV head, part) walk the same pages; workgroups go to the 8 XCDs by id mod 8, each with an L2 of its own, so these
 // units get ids of one residue (or of 8 / groups residues).
 struct PagedUnit {
   PagedSeq s;
-  int b, kvh, tile, part, chunk, unit, stride;   // b < 0: past the last unit; the tile's units are unit - part * stride + i * stride
+  int b, kvh, tile, part, chunk, unit, stride;
+  bool shared;            // some tile of the launch is shared out
+  // b < 0: past the last unit; the tile's units are unit - part * stride + i * stride
 };
 // (values that are the same in all lanes, where the compiler cannot know it)
 __device__ __forceinline__ float first_lane(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
-__device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, int bm, const PagedSeq& first) {
-  if (a.part_units == 0) return kPagedNoSplit;
-  float tiles = 0.f, pages = 0.f;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const PagedSeq s = b0 == 0 ? first : paged_seq(a, b0 + l, bm);
-    tiles += (float)s.tiles;
-    pages += (float)s.tiles * (float)s.pages;
-  }
+// Pages that a part has at most: every lane works out one candidate, from the share that one of the resident workgroups has of
+// all pages upwards, by a model in units of one page: the longest part, or, where the units take more than one round, that
+// share and half a part of unevenness; and 0.02 for writing and merging the rows of a part.  (With the share alone a call of 16 x 8
+// lists took 576 units, the last 64 of them by themselves: 16 x 5 queries 62 us, now 36.)
+__device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, const PagedSeq& mine) {
+  if (a.part_units == 0) return kPagedNoSplit;               // (the batch has at most 64 sequences otherwise)
+  float tiles = (float)mine.tiles, pages = (float)mine.tiles * (float)mine.pages;
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
     tiles += __shfl_xor(tiles, off);
@@ -102,20 +103,28 @@ __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, int
   tiles = first_lane(tiles) * (float)a.hkv;
   pages = first_lane(pages) * (float)a.hkv;
   if (3.f * tiles > 2.f * kPagedResident) return kPagedNoSplit;
-  int chunk = __builtin_amdgcn_readfirstlane(max(kPagedMinPages, (int)(pages * (1.0f / kPagedResident)) + 1));
-  // the units must fit the launch and the workspace (they do where both have their usual size)
-  for (;;) {
-    int units = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 64) {
-      const PagedSeq s = b0 == 0 ? first : paged_seq(a, b0 + l, bm);
-      int n = s.tiles > 0 ? unit_count(a.hkv * ((s.pages + chunk - 1) / chunk), s.tiles) : 0;
-      n = wave_inclusive_sum(n);
-      units += __builtin_amdgcn_readlane(n, 63);
-    }
-    if (units <= min(a.n_wg, a.part_units)) return chunk;
-    if (chunk >= (1 << 25)) return kPagedNoSplit;
-    chunk *= 2;
+  const float share = pages * (1.0f / kPagedResident);
+  const int cand = l == 63 ? kPagedNoSplit : max(kPagedMinPages, (int)(share * (float)(l + 32) * (1.0f / 32.0f)) + 1);
+  const float inv = 1.0f / (float)cand;
+  int units = 0, rows = 0;
+  float longest = 0.f;
+  for (int j = 0; j < a.batch; ++j) {
+    const int t = __builtin_amdgcn_readlane(mine.tiles, j), p = __builtin_amdgcn_readlane(mine.pages, j);
+    if (t == 0) continue;
+    int n = (int)((float)(p - 1) * inv);                     // parts: (p - 1) / cand, put right by one, and one
+    n += (n + 1) * cand <= p - 1 ? 1 : (n * cand > p - 1 ? -1 : 0);
+    ++n;
+    units += unit_count(a.hkv * n, t);
+    rows += n > 1 ? a.hkv * n * t : 0;
+    longest = fmaxf(longest, (float)p / (float)n);
   }
+  float cost = (units <= kPagedResident ? longest : fmaxf(longest, share + 0.5f * longest)) + 0.02f * (float)rows;
+  if (units > a.n_wg || units > a.part_units) cost = 1e30f;
+  if (l == 63) cost = fminf(cost, 1e29f);                    // (splits nothing, and always fits)
+  int best = (__builtin_bit_cast(int, cost) & ~63) | l;      // (positive floats order like their bits)
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) best = min(best, __shfl_xor(best, off));
+  return __builtin_amdgcn_readlane(cand, __builtin_amdgcn_readfirstlane(best) & 63);
 }
 __device__ __forceinline__ PagedSeq seq_from_lane(const PagedSeq& s, int i) {
   PagedSeq r;
@@ -132,21 +141,34 @@ __device__ __forceinline__ PagedUnit paged_plan(const PagedPrefillArgs& a, int w
   const PagedSeq first = paged_seq(a, l, bm);
   PagedUnit u;
   u.b = -1;
-  u.chunk = paged_chunk(a, l, bm, first);
+  u.chunk = kPagedNoSplit;
+  const int chunk = paged_chunk(a, l, first);
+  u.shared = chunk < kPagedNoSplit;
   int base = 0;
   bool bad = false;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
     const PagedSeq s = b0 == 0 ? first : paged_seq(a, b0 + l, bm);
     bad |= s.bad;
-    const int parts = (s.pages + u.chunk - 1) / u.chunk;
-    const int incl = base + wave_inclusive_sum(s.tiles > 0 ? unit_count(a.hkv * parts, s.tiles) : 0);
+    const int parts = (s.pages + chunk - 1) / chunk, units = s.tiles > 0 ? unit_count(a.hkv * parts, s.tiles) : 0;
+    // longest first, 64 sequences at a time
+    int rank = l, units_s = units;
+    if (a.batch > 1) {
+      const int key = (s.pages << 6) | (63 - l);             // no two alike (pages <= 2^24)
+      const int count = min(64, a.batch - b0);
+      rank = 0;
+      for (int j = 0; j < count; ++j) rank += __builtin_amdgcn_readlane(key, j) > key ? 1 : 0;
+      rank = l < count ? rank : l;
+      units_s = __builtin_amdgcn_ds_permute(4 * rank, units);
+    }
+    const int incl = base + wave_inclusive_sum(units_s);
     const int end = __builtin_amdgcn_readlane(incl, 63);
     if (u.b < 0 && wg < end) {                               // (uniform)
-      const int at = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= wg));
+      const int place = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= wg));
+      const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == place));
       u.s = seq_from_lane(s, at);
       u.b = b0 + at;
       const int n_parts = __builtin_amdgcn_readlane(parts, at), groups = a.hkv * n_parts, n_t = u.s.tiles;
-      const int before = __builtin_amdgcn_readlane(incl, at) - unit_count(groups, n_t), local = wg - before;
+      const int before = __builtin_amdgcn_readlane(incl, place) - unit_count(groups, n_t), local = wg - before;
       const int sh = share_shift(groups);
       int grp, t;
       if (sh > 0) {
@@ -166,6 +188,7 @@ __device__ __forceinline__ PagedUnit paged_plan(const PagedPrefillArgs& a, int w
         return u;
       }
       u.part = __builtin_amdgcn_readfirstlane(grp / a.hkv);
+      u.chunk = n_parts > 1 ? __builtin_amdgcn_readfirstlane((u.s.pages + n_parts - 1) / n_parts) : kPagedNoSplit;   // even parts
       u.kvh = grp - u.part * a.hkv;
       u.tile = n_t - 1 - t;                                  // heaviest first
       // rows of unit (kvh, part, tile) in the workspace: any numbering without gaps or clashes
@@ -193,6 +216,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   constexpr int DB = D / 16;              // 16-wide output blocks over the head dimension (PV)
   constexpr int KB = 4;                   // 16-key blocks of S^T per page
   constexpr int KS = 2;                   // 32-key steps of the PV product per page
+  constexpr int AHEAD = QB == 1 ? 2 : 1;  // pages on their way, in registers: calls of few rows are bound by the memory
   constexpr int CPR = D / 16;             // 16-code chunks per row
   constexpr int NS = 64 * CPR / 256;      // chunks of K, and of V, that a thread stages
   constexpr int RPS = 256 / CPR;          // rows from one of them to the next
@@ -206,6 +230,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int l = tid & 63;
   const int g = l >> 4, n = l & 15;
   const PagedUnit u = paged_plan(a, blockIdx.x, l, BM);
+  if (a.part_units > 0 && blockIdx.x == 0 && tid == 0) a.tile_info[0] = i32x4{u.shared, 0, 0, 0};
   if (u.b < 0) return;                                       // uniform for the workgroup
 
   // ---- rows and pages of the tile
@@ -224,8 +249,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int x0 = u.part * u.chunk;                           // (chunk < 2^30 / parts)
   const int parts = __builtin_amdgcn_readfirstlane((list + u.chunk - 1) / u.chunk);
   const bool split = parts > 1;
-  if (a.part_units > 0 && u.part == 0 && tid == 0)
-    a.tile_info[((int64_t)u.b * a.hkv + u.kvh) * a.n_qtiles + u.tile] = i32x4{u.unit, u.stride, parts, 0};
+  if (u.shared && u.part == 0 && tid == 0)
+    a.tile_info[1 + ((int64_t)u.b * a.hkv + u.kvh) * a.n_qtiles + u.tile] = i32x4{u.unit, u.stride, parts, 0};
   if (u.part >= parts) return;                               // (the bound on the pages was above this tile's)
   const int n_x = min(u.chunk, list - x0);                   // pages of this unit
   const int32_t* const pages = a.table + (int64_t)u.b * a.table_pages;
@@ -249,68 +274,79 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int w_lo_first = u.s.sa ? window_start(i_w_min, a.blk_shift, a.win_blocks) : 0;
   const int w_lo_last = u.s.sa ? window_start(i_w_max, a.blk_shift, a.win_blocks) : 0;
 
-  // ---- pages: lane i holds number and scales of the i-th page of 64
+  // ---- pages: lane i holds number and scales of the i-th page of 64: ids of the 64 that are being asked for, ids_next of the ones
+  // behind them, ks and vs of the ones that are being staged, ks_next and vs_next of those in ids
   int ids, ids_next;
-  float ks, vs;
+  float ks, vs, ks_next, vs_next;
   auto load_ids = [&](int x) __attribute__((always_inline)) { return pages[page_at(x0 + min(x + l, n_x - 1))]; };
   auto load_scales = [&]() __attribute__((always_inline)) {
     const int64_t page = (uint32_t)ids < (uint32_t)a.n_pages ? ids : 0;
-    ks = a.k_scale[page * a.hkv + u.kvh];
-    vs = a.v_scale[page * a.hkv + u.kvh];
+    ks_next = a.k_scale[page * a.hkv + u.kvh];
+    vs_next = a.v_scale[page * a.hkv + u.kvh];
   };
   const char* const kbase = a.k + (int64_t)u.kvh * a.stride_h;
   const char* const vbase = a.v + (int64_t)u.kvh * a.stride_h;
-  u32x4 kcode[NS], vcode[NS];
-  const int st_at = (tid / CPR) * (int)a.stride_t + 16 * (tid % CPR);
-  bool there_loaded, there = false;                          // whether the page in registers / in LDS is in the pool
-  auto load_page = [&](int x) __attribute__((always_inline)) {   // x: page of this unit
+  u32x4 kcode[AHEAD][NS], vcode[AHEAD][NS];
+  // The chunk that a thread stages: of 8 neighbouring lanes, which store at a time, half have a row whose swizzle takes their
+  // chunks to the banks that the others leave out.
+  const int st_c = D == 128 ? (tid & 3) | ((tid & 8) >> 1) : tid & 3;
+  const int st_row = D == 128 ? ((tid >> 4) << 1) | ((tid >> 2) & 1) : ((tid >> 4) << 2) | ((tid >> 1) & 2) | ((tid >> 3) & 1);
+  const int st_at = st_row * (int)a.stride_t + 16 * st_c;
+  bool there_loaded[AHEAD], there = false;                   // whether a page in registers / the one in LDS is in the pool
+  auto load_page = [&](int x, auto set_c) __attribute__((always_inline)) {   // x: page of this unit
+    constexpr int SET = decltype(set_c)::value % AHEAD;
     if ((x & 63) == 0 && x > 0) {
       ids = ids_next;
       load_scales();
       ids_next = load_ids(x + 64);
     }
     const int id = __builtin_amdgcn_readlane(ids, x & 63);
-    there_loaded = (uint32_t)id < (uint32_t)a.n_pages;
-    const int64_t off = (int64_t)(there_loaded ? id : 0) * a.stride_p;
+    there_loaded[SET] = (uint32_t)id < (uint32_t)a.n_pages;
+    const int64_t off = (int64_t)(there_loaded[SET] ? id : 0) * a.stride_p;
     // rows behind the length are not read: the last one stands in for them, with weight zero
     const int row_max = u.s.len - 1 - (page_at(x0 + x) << 6);
     const char *const kp = kbase + off, *const vp = vbase + off;
     if (row_max >= 63) {
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        kcode[i] = *(const u32x4*)(kp + i * RPS * a.stride_t + st_at);
-        vcode[i] = *(const u32x4*)(vp + i * RPS * a.stride_t + st_at);
+        kcode[SET][i] = *(const u32x4*)(kp + i * RPS * a.stride_t + st_at);
+        vcode[SET][i] = *(const u32x4*)(vp + i * RPS * a.stride_t + st_at);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        const int at = min(i * RPS + tid / CPR, row_max) * (int)a.stride_t + 16 * (tid % CPR);
-        kcode[i] = *(const u32x4*)(kp + at);
-        vcode[i] = *(const u32x4*)(vp + at);
+        const int at = min(i * RPS + st_row, row_max) * (int)a.stride_t + 16 * st_c;
+        kcode[SET][i] = *(const u32x4*)(kp + at);
+        vcode[SET][i] = *(const u32x4*)(vp + at);
       }
     }
   };
   // K tile: 16-byte chunks XOR-swizzled by the row.  V tile: 32-byte units likewise (both as in prefill.hip), and of a unit the
-  // two halves change places in every other row of a bank's, so that a wave's stores of first halves meet all banks.
+  // two halves change places in every other row of a bank's.
   auto k_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 15 : (row >> 1) & 7; };
   auto v_swz = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 7 : (row >> 1) & 3; };
   auto v_half = [](int row) __attribute__((always_inline)) { return D == 128 ? row & 1 : (row >> 1) & 1; };
-  const int st_row = tid / CPR, st_c = tid % CPR;            // (the rows that a thread stages are 32 or 64 apart: the same swizzle)
+  // (the rows that a thread stages are 32 or 64 apart: the same swizzle)
   const int k_wr = st_row * ROWB + ((2 * st_c) ^ k_swz(st_row)) * 16, v_wr = TILE + st_row * ROWB + (st_c ^ v_swz(st_row)) * 32 + 16 * v_half(st_row);
   // The page in registers becomes bf16 in LDS, in 4 NS steps of 8 codes.  The scale of V: its power of two goes into
   // the conversion, which is exact; the rest, 1 <= r < 2, into the weights.
   float k_staged = 0.f, v_rest_staged = 1.f, v_power;        // of the page staged last
-  auto begin_stage = [&](int x) __attribute__((always_inline)) {
+  auto begin_stage = [&](int x, bool is_there) __attribute__((always_inline)) {
+    if ((x & 63) == 0) {
+      ks = ks_next;
+      vs = vs_next;
+    }
     k_staged = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), x & 63));
     const uint32_t bits = max((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), x & 63), 0x00800000u);
     v_power = __builtin_bit_cast(float, bits & 0x7F800000u);
     v_rest_staged = __builtin_bit_cast(float, (bits & 0x007FFFFFu) | 0x3F800000u);
-    if (!there_loaded && tid == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
+    if (!is_there && tid == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
   };
-  auto stage_step = [&](int j, FLUX_LDS char* st) __attribute__((always_inline)) {
+  auto stage_step = [&](int j, auto set_c, FLUX_LDS char* st) __attribute__((always_inline)) {
+    constexpr int SET = decltype(set_c)::value % AHEAD;
     const int i = (j >> 1) % NS, h = j & 1;                  // chunk of the thread, half of the chunk
-    if (j < 2 * NS) *(FLUX_LDS u32x4*)(st + (k_wr ^ (16 * h)) + i * RPS * ROWB) = unpack8_scaled(kcode[i][2 * h], kcode[i][2 * h + 1], 1.0f);
-    else *(FLUX_LDS u32x4*)(st + (v_wr ^ (16 * h)) + i * RPS * ROWB) = unpack8_scaled(vcode[i][2 * h], vcode[i][2 * h + 1], v_power);
+    if (j < 2 * NS) *(FLUX_LDS u32x4*)(st + (k_wr ^ (16 * h)) + i * RPS * ROWB) = unpack8_scaled(kcode[SET][i][2 * h], kcode[SET][i][2 * h + 1], 1.0f);
+    else *(FLUX_LDS u32x4*)(st + (v_wr ^ (16 * h)) + i * RPS * ROWB) = unpack8_scaled(vcode[SET][i][2 * h], vcode[SET][i][2 * h + 1], v_power);
   };
   static_assert(4 * NS == DB, "a step of the staging for every output block");
 
@@ -334,18 +370,26 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
 
   ids = load_ids(0);
   ids_next = load_ids(64);
-  load_page(0);
+  typedef std::integral_constant<int, 0> Even;
+  typedef std::integral_constant<int, 1> Odd;
+  load_page(0, Even());
   load_scales();
-  begin_stage(0);
+  if (AHEAD == 2 && n_x > 1) load_page(1, Odd());
+  begin_stage(0, there_loaded[0]);
 #pragma unroll
-  for (int j = 0; j < DB; ++j) stage_step(j, (FLUX_LDS char*)smem);
+  for (int j = 0; j < DB; ++j) stage_step(j, Even(), (FLUX_LDS char*)smem);
   float k_now = k_staged, v_rest = v_rest_staged;
-  there = there_loaded;
-  if (n_x > 1) load_page(1);
+  there = there_loaded[0];
+  if (AHEAD == 2) {
+    if (n_x > 2) load_page(2, Even());
+  } else if (n_x > 1) {
+    load_page(1, Odd());
+  }
   __syncthreads();
 
   auto iteration = [&](int x, auto stg_c) __attribute__((always_inline)) {
     constexpr int STG = decltype(stg_c)::value;
+    typedef std::integral_constant<int, STG ^ 1> Other;      // registers of the next page, and its stage
     FLUX_LDS char* const st = (FLUX_LDS char*)smem + STG * STAGE;
     const float c = fmaxf(a.scale_log2 * k_now, 0x1p-126f);  // (not 0: a masked score is -inf times this)
     const bool here = there;
@@ -356,7 +400,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
     bool hidden = !here || !wave_active || j0 > i_w_max;
     const bool all_sink = j0 + 64 <= a.sink_lim;
     hidden |= u.s.sa && j0 >= a.sink_lim && j0 + 63 < w_lo_first;
-    if (more) begin_stage(x + 1);
+    if (more) begin_stage(x + 1, there_loaded[Other::value % AHEAD]);
     if (!hidden) {
       const bool causal = j0 + 63 > i_w_min, edge = u.s.sa && !all_sink && j0 < w_lo_last;
       f32x4 s[KB][QB];
@@ -409,12 +453,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
         const int kc = t >> 1, kb = 2 + (t & 1);
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][kc], qf[qb][kc], s[kb][qb], 0, 0, 0);
+#pragma unroll
+        for (int db = t * DB / (2 * KC); db < (t + 1) * DB / (2 * KC); ++db) read_v(0, db);
         __builtin_amdgcn_sched_barrier(0);
       }
       __builtin_amdgcn_s_setprio(0);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) read_v(0, db);
-      __builtin_amdgcn_sched_barrier(0);
       float l_page[QB];
       auto weights = [&]() __attribute__((always_inline)) {
         const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
@@ -477,7 +520,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[1][db], pf[qb][1], o[db][qb], 0, 0, 0);
           if constexpr (decltype(stages)::value) {
-            stage_step(db, st_next);
+            stage_step(db, Other(), st_next);
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -487,19 +530,19 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
       __builtin_amdgcn_s_setprio(0);
     } else if (more) {
 #pragma unroll
-      for (int j = 0; j < DB; ++j) stage_step(j, st_next);
+      for (int j = 0; j < DB; ++j) stage_step(j, Other(), st_next);
     }
     if (more) {
       k_now = k_staged;
       v_rest = v_rest_staged;
-      there = there_loaded;
-      if (x + 2 < n_x) load_page(x + 2);
+      there = there_loaded[Other::value % AHEAD];
+      if (x + 1 + AHEAD < n_x) load_page(x + 1 + AHEAD, Other());
     }
     __syncthreads();                                         // this stage is free, and the other one written
   };
   for (int x = 0; x < n_x; x += 2) {
-    iteration(x, std::integral_constant<int, 0>());
-    if (x + 1 < n_x) iteration(x + 1, std::integral_constant<int, 1>());
+    iteration(x, Even());
+    if (x + 1 < n_x) iteration(x + 1, Odd());
   }
 
   // ---- lane (n, g) holds d = 16 * db + 4 * g .. +3 of its rows
@@ -541,6 +584,7 @@ struct PagedMergeArgs {
 template <int D>
 __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
   constexpr int TPR = D / 4, RPW = 256 / TPR;                // rows that a workgroup has in work
+  if (a.tile_info[0][0] == 0) return;
   const int groups = a.bm / RPW;
   const long long items = (long long)a.batch * a.hkv * a.n_qtiles * groups;
   for (long long it = blockIdx.x; it < items; it += gridDim.x) {
@@ -554,7 +598,7 @@ __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
     const int64_t rows = min((int64_t)n_q * a.group - (int64_t)tile * a.bm, (int64_t)a.bm);
     const int x = rg * RPW + threadIdx.x / TPR, d = 4 * (threadIdx.x % TPR);
     if (rg * RPW >= rows) continue;                          // (no such tile: what its entry holds is not read)
-    const i32x4 info = a.tile_info[t];
+    const i32x4 info = a.tile_info[1 + t];
     if (info[2] < 2 || x >= rows) continue;
     float m = -INFINITY, den = 0.f;
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
