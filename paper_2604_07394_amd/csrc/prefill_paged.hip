@@ -395,7 +395,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
     const bool here = there;
     const bool more = x + 1 < n_x;                           // the next page goes into the other stage, the one behind it is asked for
     FLUX_LDS char* const st_next = (FLUX_LDS char*)smem + (STG ^ 1) * STAGE;
-    const float log_rest = v_rest == 1.f ? 0.f : __builtin_amdgcn_logf(v_rest), inv_rest = 1.0f / v_rest;
+    float log_rest = 0.f, inv_rest = 1.f;
+    if (__builtin_expect(v_rest != 1.f, 0)) {                // (uniform; the scales that the append writes are powers of two)
+      log_rest = __builtin_amdgcn_logf(v_rest);
+      inv_rest = 1.0f / v_rest;
+    }
     const int j0 = page_at(x0 + x) << 6;
     bool hidden = !here || !wave_active || j0 > i_w_max;
     const bool all_sink = j0 + 64 <= a.sink_lim;
@@ -419,6 +423,27 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
 #pragma unroll
         for (int kc = 0; kc < KC; ++kc) read_k(kb, kc);
       __builtin_amdgcn_sched_barrier(0);
+      auto scores = [&]() __attribute__((always_inline)) {
+        // S^T of keys 0..31 with the K fragments of keys 32..63 read between the MFMAs, then S^T of keys 32..63 with the V
+        // fragments of keys 0..31 read between them
+#pragma unroll
+        for (int t = 0; t < 2 * KC; ++t) {
+          const int kc = t >> 1, kb = t & 1;
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][kc], qf[qb][kc], s[kb][qb], 0, 0, 0);
+          read_k(2 + kb, kc);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int t = 0; t < 2 * KC; ++t) {
+          const int kc = t >> 1, kb = 2 + (t & 1);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][kc], qf[qb][kc], s[kb][qb], 0, 0, 0);
+#pragma unroll
+          for (int db = t * DB / (2 * KC); db < (t + 1) * DB / (2 * KC); ++db) read_v(0, db);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
       if (causal || edge) {
         // element masks are put into the accumulators that the scores start from: key j0 + 4 g + c, c a constant
 #pragma unroll
@@ -432,30 +457,13 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
               s[kb][qb][i] = (k <= hi) & ((k < sl) | (k >= lo)) ? 0.f : -INFINITY;
             }
         }
-      } else {
+        scores();
+      } else {                                               // (a path of its own: merged with the other one, the zeros would be moved into 32 registers)
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int qb = 0; qb < QB; ++qb) s[kb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-      // S^T of keys 0..31 with the K fragments of keys 32..63 read between the MFMAs, then S^T of keys 32..63 with the V
-      // fragments of keys 0..31 read between them
-#pragma unroll
-      for (int t = 0; t < 2 * KC; ++t) {
-        const int kc = t >> 1, kb = t & 1;
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][kc], qf[qb][kc], s[kb][qb], 0, 0, 0);
-        read_k(2 + kb, kc);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int t = 0; t < 2 * KC; ++t) {
-        const int kc = t >> 1, kb = 2 + (t & 1);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[kb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kb][kc], qf[qb][kc], s[kb][qb], 0, 0, 0);
-#pragma unroll
-        for (int db = t * DB / (2 * KC); db < (t + 1) * DB / (2 * KC); ++db) read_v(0, db);
-        __builtin_amdgcn_sched_barrier(0);
+        scores();
       }
       __builtin_amdgcn_s_setprio(0);
       float l_page[QB];
