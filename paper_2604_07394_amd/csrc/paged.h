@@ -32,6 +32,16 @@ constexpr int share_shift(int groups) { return groups == 1 ? 3 : (groups == 2 ? 
 constexpr int unit_count(int groups, int tiles) {
   return share_shift(groups) > 0 ? ((tiles + (1 << share_shift(groups)) - 1) >> share_shift(groups)) * 8 : groups * tiles;
 }
+// n / d = (mulhi(n, mul) + n) >> shift for n < 2^31: the round-up method of Granlund and Montgomery (Division by invariant integers
+// using multiplication, 1994), mul = floor(2^32 (2^shift - d) / d) + 1 with 2^shift >= d.
+struct Reciprocal {
+  uint32_t mul, shift;
+};
+inline Reciprocal reciprocal(uint32_t d) {
+  uint32_t shift = 0;
+  while (shift < 31 && (1ull << shift) < d) ++shift;
+  return {(uint32_t)(((((uint64_t)1 << shift) - d) << 32) / d + 1), shift};
+}
 struct PagedPrefillPlan {
   int bm;               // rows of a tile
   int tiles;            // of a sequence and KV head, at most

@@ -35,6 +35,7 @@ struct PagedPrefillArgs {
   const int32_t* kv_len;
   const uint8_t* mode;
   int hq, hkv, group, batch;
+  Reciprocal by_group;
   int sink_lim, win_blocks, blk_shift;   // SA geometry (see sa_geom)
   int n_qtiles;           // tiles that a sequence has at most, by the host's bound
   int n_wg;
@@ -50,6 +51,8 @@ struct PagedPrefillArgs {
 
 constexpr float kPagedGuard = 1073741824.0f;  // 2^30: a page whose weights sum past this moves the reference
 constexpr int kPagedNoSplit = 0x3FFFFFFF;
+
+__device__ __forceinline__ int quotient(int n, Reciprocal d) { return (int)(((uint32_t)(((uint64_t)(uint32_t)n * d.mul) >> 32) + (uint32_t)n) >> d.shift); }
 
 struct PagedSeq {
   int q_begin, n_q, len, tiles, pages;   // pages: of its longest tile (an upper bound for SA)
@@ -86,8 +89,26 @@ struct PagedUnit {
   bool shared;            // some tile of the launch is shared out
   // b < 0: past the last unit; the tile's units are unit - part * stride + i * stride
 };
-// (values that are the same in all lanes, where the compiler cannot know it)
-__device__ __forceinline__ float first_lane(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
+// Over the 64 lanes, by moves between them as in wave_inclusive_sum; lane 63 has the result.  (Through LDS, a step takes a hundred
+// cycles.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int old, int x) { return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus_moved(float x) { return x + __builtin_bit_cast(float, moved<CTRL, ROWS>(0, __builtin_bit_cast(int, x))); }
+__device__ __forceinline__ float wave_sum(float x) {
+  x = plus_moved<0x118, 0xf>(plus_moved<0x114, 0xf>(plus_moved<0x112, 0xf>(plus_moved<0x111, 0xf>(x))));
+  x = plus_moved<0x143, 0xc>(plus_moved<0x142, 0xa>(x));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ __forceinline__ int wave_min(int x) {
+  x = min(x, moved<0x111, 0xf>(x, x));
+  x = min(x, moved<0x112, 0xf>(x, x));
+  x = min(x, moved<0x114, 0xf>(x, x));
+  x = min(x, moved<0x118, 0xf>(x, x));
+  x = min(x, moved<0x142, 0xa>(x, x));
+  x = min(x, moved<0x143, 0xc>(x, x));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 // Pages that a part has at most: every lane works out one candidate, from the share that one of the resident workgroups has of
 // all pages upwards, by a model in units of one page: the longest part, or, where the units take more than one round, that
 // share and half a part of unevenness; and 0.02 for writing and merging the rows of a part.  (With the share alone a call of 16 x 8
@@ -95,16 +116,11 @@ __device__ __forceinline__ float first_lane(float x) { return __builtin_bit_cast
 __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, const PagedSeq& mine) {
   if (a.part_units == 0) return kPagedNoSplit;               // (the batch has at most 64 sequences otherwise)
   float tiles = (float)mine.tiles, pages = (float)mine.tiles * (float)mine.pages;
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) {
-    tiles += __shfl_xor(tiles, off);
-    pages += __shfl_xor(pages, off);
-  }
-  tiles = first_lane(tiles) * (float)a.hkv;
-  pages = first_lane(pages) * (float)a.hkv;
+  tiles = wave_sum(tiles) * (float)a.hkv;
+  pages = wave_sum(pages) * (float)a.hkv;
   if (3.f * tiles > 2.f * kPagedResident) return kPagedNoSplit;
   const float share = pages * (1.0f / kPagedResident);
-  const int cand = l == 63 ? kPagedNoSplit : max(kPagedMinPages, (int)(share * (float)(l + 32) * (1.0f / 32.0f)) + 1);
+  const int cand = l == 63 ? kPagedNoSplit : max(kPagedMinPages, (int)(share * (float)(l + 32) * (1.0f / 32.0f)) + 1);   // (1 to 3 shares)
   const float inv = 1.0f / (float)cand;
   int units = 0, rows = 0;
   float longest = 0.f;
@@ -121,10 +137,7 @@ __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, con
   float cost = (units <= kPagedResident ? longest : fmaxf(longest, share + 0.5f * longest)) + 0.02f * (float)rows;
   if (units > a.n_wg || units > a.part_units) cost = 1e30f;
   if (l == 63) cost = fminf(cost, 1e29f);                    // (splits nothing, and always fits)
-  int best = (__builtin_bit_cast(int, cost) & ~63) | l;      // (positive floats order like their bits)
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) best = min(best, __shfl_xor(best, off));
-  return __builtin_amdgcn_readlane(cand, __builtin_amdgcn_readfirstlane(best) & 63);
+  return __builtin_amdgcn_readlane(cand, wave_min((__builtin_bit_cast(int, cost) & ~63) | l) & 63);   // (positive floats order like their bits)
 }
 __device__ __forceinline__ PagedSeq seq_from_lane(const PagedSeq& s, int i) {
   PagedSeq r;
@@ -237,7 +250,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int rows = (int)min((int64_t)u.s.n_q * a.group - (int64_t)u.tile * BM, (int64_t)BM);
   const int r0 = u.tile * BM;                                // (n_q * group may pass 2^31 only with tiles that the bound cuts)
   const int pos0 = u.s.len - u.s.n_q;                        // position of the sequence's first query
-  auto token_of = [&](int r) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(r / a.group); };   // (r: uniform)
+  auto token_of = [&](int r) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(quotient(r, a.by_group)); };   // (r: uniform)
   const int i_min = pos0 + token_of(r0), i_max = pos0 + token_of(r0 + rows - 1);
   const int last = i_max >> 6;                               // the page of the last query
   int seam = 0x7FFFFFFF, skip = 0;                           // list index x >= seam is page x + skip
@@ -256,13 +269,20 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int32_t* const pages = a.table + (int64_t)u.b * a.table_pages;
   auto page_at = [&](int x) __attribute__((always_inline)) { return x + (x >= seam ? skip : 0); };   // list index -> page of the sequence
 
+  // ---- pages: lane i holds number and scales of the i-th page of 64: ids of the 64 that are being asked for, ids_next of the ones
+  // behind them, ks and vs of the ones that are being staged, ks_next and vs_next of those in ids
+  float ks, vs, ks_next, vs_next;
+  auto load_ids = [&](int x) __attribute__((always_inline)) { return pages[page_at(x0 + min(x + l, n_x - 1))]; };
+  int ids = load_ids(0), ids_next = load_ids(64);
+  __builtin_amdgcn_sched_barrier(0);
+
   // ---- what a lane knows of its rows: position and start of the window; rows past the last one repeat it
   const int r_w0 = w * WR;
   int i_mine[QB], w_lo_mine[QB];
   bf16x8 qf[QB][KC];
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const int r = r0 + min(r_w0 + 16 * qb + n, rows - 1), tok = r / a.group, head = r - tok * a.group;
+    const int r = r0 + min(r_w0 + 16 * qb + n, rows - 1), tok = quotient(r, a.by_group), head = r - tok * a.group;
     i_mine[qb] = pos0 + tok;
     w_lo_mine[qb] = u.s.sa ? window_start(i_mine[qb], a.blk_shift, a.win_blocks) : 0;
     const __bf16* qrow = a.q + ((int64_t)(u.s.q_begin + tok) * a.hq + (int64_t)u.kvh * a.group + head) * D;
@@ -274,11 +294,6 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int w_lo_first = u.s.sa ? window_start(i_w_min, a.blk_shift, a.win_blocks) : 0;
   const int w_lo_last = u.s.sa ? window_start(i_w_max, a.blk_shift, a.win_blocks) : 0;
 
-  // ---- pages: lane i holds number and scales of the i-th page of 64: ids of the 64 that are being asked for, ids_next of the ones
-  // behind them, ks and vs of the ones that are being staged, ks_next and vs_next of those in ids
-  int ids, ids_next;
-  float ks, vs, ks_next, vs_next;
-  auto load_ids = [&](int x) __attribute__((always_inline)) { return pages[page_at(x0 + min(x + l, n_x - 1))]; };
   auto load_scales = [&]() __attribute__((always_inline)) {
     const int64_t page = (uint32_t)ids < (uint32_t)a.n_pages ? ids : 0;
     ks_next = a.k_scale[page * a.hkv + u.kvh];
@@ -559,6 +574,17 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
     float l_tot = l_run[qb];
     l_tot += __shfl_xor(l_tot, 16);
     l_tot += __shfl_xor(l_tot, 32);
+    const float inv = l_tot > 0.f || l_tot != l_tot ? 1.0f / l_tot : 0.f;   // (no key there: a row of zeros)
+    // bf16 rows: of two output blocks side by side, the lanes of odd g hand their part of the first to the lane of g - 1 and
+    // get its part of the second, so that a lane stores eight columns in a row (all lanes take part, whatever they store)
+    u32x4 pk[DB / 2];
+#pragma unroll
+    for (int db = 0; db < DB; db += 2) {
+      const f32x4 lo = o[db][qb] * inv, hi = o[db + 1][qb] * inv;
+      const auto y0 = __builtin_amdgcn_permlane16_swap(pack_bf16(lo[0], lo[1]), pack_bf16(hi[0], hi[1]), false, false);
+      const auto y1 = __builtin_amdgcn_permlane16_swap(pack_bf16(lo[2], lo[3]), pack_bf16(hi[2], hi[3]), false, false);
+      pk[db / 2] = u32x4{y0[0], y1[0], y0[1], y1[1]};
+    }
     const int x = r_w0 + 16 * qb + n;
     if (x >= rows) continue;
     if (split) {
@@ -568,14 +594,15 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
       for (int db = 0; db < DB; ++db) *(f32x4*)(a.part_o + row * D + 16 * db + 4 * g) = o[db][qb];
       continue;
     }
-    const float inv = l_tot > 0.f || l_tot != l_tot ? 1.0f / l_tot : 0.f;   // (no key there: a row of zeros)
-    const int r = r0 + x, tok = r / a.group, head = r - tok * a.group;
-    const int64_t off = ((int64_t)(u.s.q_begin + tok) * a.hq + (int64_t)u.kvh * a.group + head) * D + 4 * g;
+    const int r = r0 + x, tok = quotient(r, a.by_group), head = r - tok * a.group;
+    const int64_t off = ((int64_t)(u.s.q_begin + tok) * a.hq + (int64_t)u.kvh * a.group + head) * D;
+    if (a.out_fp32) {
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      const f32x4 y = o[db][qb] * inv;
-      if (a.out_fp32) *(f32x4*)((float*)a.out + off + 16 * db) = y;
-      else *(u32x2*)((__bf16*)a.out + off + 16 * db) = u32x2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+      for (int db = 0; db < DB; ++db) *(f32x4*)((float*)a.out + off + 16 * db + 4 * g) = o[db][qb] * inv;
+    } else {
+      __bf16* const dst = (__bf16*)a.out + off + 16 * (g & 1) + 8 * (g >> 1);
+#pragma unroll
+      for (int db = 0; db < DB; db += 2) *(u32x4*)(dst + 16 * db) = pk[db / 2];
     }
   }
 }
@@ -587,6 +614,7 @@ struct PagedMergeArgs {
   const float *part_o, *part_ml;
   const i32x4* tile_info;
   int batch, hq, hkv, group, n_qtiles, bm, capacity, out_fp32;
+  Reciprocal by_group;
   void* out;
 };
 template <int D>
@@ -594,11 +622,10 @@ __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
   constexpr int TPR = D / 4, RPW = 256 / TPR;                // rows that a workgroup has in work
   if (a.tile_info[0][0] == 0) return;
   const int groups = a.bm / RPW;
-  const long long items = (long long)a.batch * a.hkv * a.n_qtiles * groups;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int rg = (int)(it % groups);
-    const int64_t t = it / groups;
-    const int tile = (int)(t % a.n_qtiles), kvh = (int)(t / a.n_qtiles % a.hkv), b = (int)(t / a.n_qtiles / a.hkv);
+  const int items = a.batch * a.hkv * a.n_qtiles * groups;   // (64 sequences and two thirds of kPagedResident tiles of one at most)
+  for (int it = blockIdx.x; it < items; it += gridDim.x) {
+    const int t = it / groups, rg = it - t * groups;
+    const int pair = t / a.n_qtiles, tile = t - pair * a.n_qtiles, b = pair / a.hkv, kvh = pair - b * a.hkv;
     const int q_begin = a.cu_q[b];
     int n_q = a.cu_q[b + 1] - q_begin, len = a.kv_len[b];
     len = len < 0 ? 0 : min(len, a.capacity);
@@ -634,7 +661,7 @@ __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
       m = m_new;
     }
     const float inv = den > 0.f || den != den ? 1.0f / den : 0.f;
-    const int r = tile * a.bm + x, tok = r / a.group, head = r - tok * a.group;
+    const int r = tile * a.bm + x, tok = quotient(r, a.by_group), head = r - tok * a.group;
     const int64_t off = ((int64_t)(q_begin + tok) * a.hq + (int64_t)kvh * a.group + head) * D + d;
     const f32x4 y = num * inv;
     if (a.out_fp32) *(f32x4*)((float*)a.out + off) = y;
@@ -664,6 +691,7 @@ hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const vo
   a.hq = cfg.n_q_heads;
   a.hkv = cfg.n_kv_heads;
   a.group = cfg.n_q_heads / cfg.n_kv_heads;
+  a.by_group = reciprocal((uint32_t)a.group);
   a.batch = pt.batch;
   const SaGeom geom = sa_geom(cfg);
   a.sink_lim = geom.sink_lim;
@@ -699,6 +727,7 @@ hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const vo
   m.hq = a.hq;
   m.hkv = a.hkv;
   m.group = a.group;
+  m.by_group = a.by_group;
   m.n_qtiles = plan.tiles;
   m.bm = plan.bm;
   m.capacity = pt.table_pages * kPageTokens;
