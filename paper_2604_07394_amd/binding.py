@@ -215,14 +215,24 @@ def _cache_arg(cache):
     return _pack_cache(k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], cache.kv_len.data_ptr(), b, cap)
 
 
-@dataclass
+@dataclass(frozen=True)
 class PageTable:
     """Which pages the sequences of a batch have, for all layers: table int32 [B, table_pages], kv_len int32 [B], and the free
-    pages, free_pages int32 [n_pages] (entries 0 .. n_free - 1) and n_free int32 [1]."""
+    pages, free_pages int32 [n_pages] (entries 0 .. n_free - 1) and n_free int32 [1].  A handle: its tensors are checked and their
+    addresses taken when it is made (which costs as much as the launch of a small call)."""
     table: torch.Tensor
     kv_len: torch.Tensor
     free_pages: torch.Tensor
     n_free: torch.Tensor
+
+    def __post_init__(self):
+        t = self.table
+        b, wide = t.shape
+        assert t.is_contiguous() and self.kv_len.shape == (b,) and self.kv_len.is_contiguous()
+        assert self.free_pages.is_contiguous() and self.free_pages.dim() == 1 and self.n_free.numel() == 1
+        assert all(x.dtype == torch.int32 for x in (t, self.kv_len, self.free_pages, self.n_free))
+        object.__setattr__(self, "packed", _pack_pages(t.data_ptr(), self.kv_len.data_ptr(), self.free_pages.data_ptr(), self.n_free.data_ptr(),
+                                                       b, wide, self.free_pages.shape[0]))
 
     @classmethod
     def empty(cls, batch, n_pages, table_pages, device="cuda"):
@@ -233,14 +243,24 @@ class PageTable:
                    torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device), i32([n_pages]))
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedKV:
     """One layer's pool of pages: k, v [n_pages, Hkv, 64, D] e4m3 codes (torch.float8_e4m3fn or uint8; any strides of multiples of
-    16 with D contiguous), k_scale, v_scale fp32 [n_pages, Hkv].  Plain device memory; all reads and writes happen in the library."""
+    16 with D contiguous), k_scale, v_scale fp32 [n_pages, Hkv].  Plain device memory; all reads and writes happen in the library.
+    A handle, as PageTable."""
     k: torch.Tensor
     v: torch.Tensor
     k_scale: torch.Tensor
     v_scale: torch.Tensor
+
+    def __post_init__(self):
+        k, v = self.k, self.v
+        strides, (n, h, tokens, _) = k.stride(), k.shape
+        assert tokens == PAGE_TOKENS and strides == v.stride() and strides[3] == 1 and k.element_size() == v.element_size() == 1 and v.shape == k.shape
+        for s in (self.k_scale, self.v_scale):
+            assert s.shape == (n, h) and s.is_contiguous() and s.dtype == torch.float32
+        object.__setattr__(self, "packed", _pack_paged_kv(k.data_ptr(), v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                                                          strides[0], strides[1], strides[2], n))
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, head_dim, device="cuda"):
@@ -249,23 +269,8 @@ class PagedKV:
         return cls(k, torch.empty_like(k), s, torch.empty_like(s))
 
 
-def _pages_arg(pt):
-    if type(pt) is not PageTable:
-        return C.byref(pt)
-    t = pt.table
-    b, wide = t.shape
-    assert t.is_contiguous() and pt.kv_len.shape[0] == b
-    return _pack_pages(t.data_ptr(), pt.kv_len.data_ptr(), pt.free_pages.data_ptr(), pt.n_free.data_ptr(), b, wide, pt.free_pages.shape[0])
-
-
-def _paged_kv_arg(kv):
-    if type(kv) is not PagedKV:
-        return C.byref(kv)
-    k, v = kv.k, kv.v
-    strides, (n, h, tokens, _) = k.stride(), k.shape
-    assert tokens == PAGE_TOKENS and strides == v.stride() and strides[3] == 1 and k.element_size() == 1 and v.shape == k.shape
-    assert kv.k_scale.shape == (n, h) == kv.v_scale.shape and kv.k_scale.is_contiguous() and kv.v_scale.is_contiguous()
-    return _pack_paged_kv(k.data_ptr(), v.data_ptr(), kv.k_scale.data_ptr(), kv.v_scale.data_ptr(), strides[0], strides[1], strides[2], n)
+def _handle_arg(h):
+    return h.packed if type(h) in (PageTable, PagedKV) else C.byref(h)
 
 
 def flux_router(ctx, x, cu_seqlens, batch, hidden, pool, w1, b1, w2, b2, inner, mode_out, logits_out=None,
@@ -328,23 +333,23 @@ def flux_attn_decode_ring(ctx, cfg, q, ring, out, stream=None) -> None:
 
 
 def flux_page_plan(ctx, pt, cu_new, total_new, slots, stream=None) -> None:
-    _check(_lib.flux_page_plan(ctx, _pages_arg(pt), _ptr(cu_new), total_new, _ptr(slots), _stream(stream)))
+    _check(_lib.flux_page_plan(ctx, _handle_arg(pt), _ptr(cu_new), total_new, _ptr(slots), _stream(stream)))
 
 
 def flux_page_release(ctx, pt, keep_len, stream=None) -> None:
-    _check(_lib.flux_page_release(ctx, _pages_arg(pt), _ptr(keep_len), _stream(stream)))
+    _check(_lib.flux_page_release(ctx, _handle_arg(pt), _ptr(keep_len), _stream(stream)))
 
 
 def flux_kv_append_paged(ctx, kv, n_kv_heads, head_dim, k_new, v_new, slots, total_new, stream=None) -> None:
-    _check(_lib.flux_kv_append_paged(ctx, _paged_kv_arg(kv), n_kv_heads, head_dim, _ptr(k_new), _ptr(v_new), _ptr(slots), total_new,
+    _check(_lib.flux_kv_append_paged(ctx, _handle_arg(kv), n_kv_heads, head_dim, _ptr(k_new), _ptr(v_new), _ptr(slots), total_new,
                                      _stream(stream)))
 
 
 def flux_attn_decode_paged(ctx, cfg, q, max_kv_len, kv, pt, mode, out, stream=None) -> None:
-    _check(_lib.flux_attn_decode_paged(ctx, C.byref(cfg), _ptr(q), max_kv_len, _paged_kv_arg(kv), _pages_arg(pt), _ptr(mode), _ptr(out),
+    _check(_lib.flux_attn_decode_paged(ctx, C.byref(cfg), _ptr(q), max_kv_len, _handle_arg(kv), _handle_arg(pt), _ptr(mode), _ptr(out),
                                        _stream(stream)))
 
 
 def flux_attn_prefill_paged(ctx, cfg, q, cu_q, max_q_len, max_kv_len, kv, pt, mode, out, stream=None) -> None:
-    _check(_lib.flux_attn_prefill_paged(ctx, C.byref(cfg), _ptr(q), _ptr(cu_q), max_q_len, max_kv_len, _paged_kv_arg(kv), _pages_arg(pt),
+    _check(_lib.flux_attn_prefill_paged(ctx, C.byref(cfg), _ptr(q), _ptr(cu_q), max_q_len, max_kv_len, _handle_arg(kv), _handle_arg(pt),
                                         _ptr(mode), _ptr(out), _stream(stream)))

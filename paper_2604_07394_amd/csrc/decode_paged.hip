@@ -14,7 +14,7 @@
 //   online softmax in the accumulator layout (one query per lane column, 16 keys per lane), in units of log2
 //   O^T[d][q]   += cv^T[d][key] . (p sv)^T[key][q]   the codes of V go through wave-private LDS and come back with the
 //                                            transposing 8-bit LDS read, 8 keys of one d per lane, in the order in which the
-//                                            accumulators hold them; the weights as two bf16 terms, as in decode.hip
+//                                            accumulators hold them; the weights as two bf16 terms (three for fp32 outputs)
 #include <type_traits>
 
 #include "decode_cut.h"
@@ -74,28 +74,30 @@ struct PagedDecodeArgs {
   uint32_t* status;
   uint32_t* arrived;
   void* out;
-  int out_fp32;
 };
 
 typedef __attribute__((__vector_size__(2 * sizeof(int)))) int i32x2;
 
-// 8 codes as bf16 values
-__device__ __forceinline__ bf16x8 unpack8(uint32_t lo, uint32_t hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// 8 codes times a power of two as bf16 values
+__device__ __forceinline__ bf16x8 unpack8(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)});
 }
 
-template <int D, bool NT, int W>
+// FP32: the outputs are fp32, and a weight takes three bf16 terms (bf16 outputs: two)
+template <int D, bool NT, int W, bool FP32>
 __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs a) {
   constexpr int KK = D / 64;          // 16-byte K loads per lane and 16 keys
   constexpr int DB = D / 16;          // 16-wide output blocks over the head dimension
   constexpr int CPR = D / 16;         // 16-byte chunks per row
   constexpr int RPL = 64 / CPR;       // V rows per wave-wide load
   constexpr int VL = 64 / RPL;        // V loads per lane and page
-  constexpr int VROW = D + 16;        // LDS row of V (bytes): the 16 rows that a pass of the transposing read takes lie in different banks
+  // LDS row of V and block of 16 of them (bytes): the 8 rows of each of two blocks that a pass of the transposing read takes lie in
+  // different banks
+  constexpr int VROW = D + 16, VBLOCK = 16 * VROW + 128;
   constexpr int RED = D + 4;          // floats from one row of the merge buffer to the next
-  constexpr int STAGING = W * 64 * VROW, RED_BYTES = W * 16 * (RED + 2) * 4;
+  constexpr int VWAVE = 4 * VBLOCK - 128, STAGING = W * VWAVE, RED_BYTES = W * 16 * (RED + 2) * 4;
   __shared__ __attribute__((aligned(16))) char smem[STAGING > RED_BYTES ? STAGING : RED_BYTES];
   __shared__ int last_of_pair;
 
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
       const int64_t off = (int64_t)b * a.hq * D;
       for (int x = 8 * tid; x < a.hq * D; x += 8 * 64 * W) {
         const u32x4 zero = {0, 0, 0, 0};
-        if (a.out_fp32) {
+        if constexpr (FP32) {
           *(u32x4*)((float*)a.out + off + x) = zero;
           *(u32x4*)((float*)a.out + off + x + 4) = zero;
         } else {
@@ -177,8 +179,8 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
 
   auto ld = [](const u32x4* x) -> u32x4 { return NT ? __builtin_nontemporal_load(x) : *x; };
   u32x4 kreg[4][KK], vreg[VL];
-  const int k_lane = n * (int)a.stride_t + 16 * g;
-  const int v_lane = (l / CPR) * (int)a.stride_t + 16 * (l % CPR);
+  const uint32_t k_lane = n * (uint32_t)a.stride_t + 16 * g;
+  const uint32_t v_lane = (l / CPR) * (uint32_t)a.stride_t + 16 * (l % CPR);
   // the page's first position, and whether all of its positions are visible
   auto first_of = [&](int x) __attribute__((always_inline)) { return (x + (x >= list.seam ? list.skip : 0)) << 6; };
   auto is_full = [&](int pos) __attribute__((always_inline)) {
@@ -203,11 +205,11 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
         const int key = pos + r;
         return key < place.len && (list.tail_start == list.s_end || key < list.s_end || key >= list.tail_start) ? r : stand_in;
       };
-      int krow[4], vrow[VL];
+      uint32_t krow[4], vrow[VL];
 #pragma unroll
-      for (int sb = 0; sb < 4; ++sb) krow[sb] = row_of(16 * sb + n) * (int)a.stride_t + 16 * g;
+      for (int sb = 0; sb < 4; ++sb) krow[sb] = row_of(16 * sb + n) * (uint32_t)a.stride_t + 16 * g;
 #pragma unroll
-      for (int i = 0; i < VL; ++i) vrow[i] = row_of(i * RPL + l / CPR) * (int)a.stride_t + 16 * (l % CPR);
+      for (int i = 0; i < VL; ++i) vrow[i] = row_of(i * RPL + l / CPR) * (uint32_t)a.stride_t + 16 * (l % CPR);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int sb = 0; sb < 4; ++sb)
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
     }
   };
 
-  FLUX_LDS char* const vs_lds = (FLUX_LDS char*)smem + w * 64 * VROW;
+  FLUX_LDS char* const vs_lds = (FLUX_LDS char*)smem + w * VWAVE;
   bf16x8 qf[2 * KK];
   int id_now;                                                // number of the page in flight
   auto begin_part = [&]() __attribute__((always_inline)) {
@@ -253,21 +255,27 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
 
     for (int i = 0; p < x1; ++i) {
       const int pos = first_of(p), id = id_now;
-      const float c = a.scale_log2 * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), i));
-      const float vsc = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), i));
+      const float c = fmaxf(a.scale_log2 * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), i)), 0x1p-126f);   // (not 0: a masked score is -inf times this)
+      // the scale of V: its power of two goes into the conversion, the rest, 1 <= r < 2, into the weights
+      const uint32_t v_bits = max((uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), i), 0x00800000u);
+      const float v_power = __builtin_bit_cast(float, v_bits & 0x7F800000u);
+      float log_rest = 0.f, inv_rest = 1.f;
+      if (__builtin_expect((v_bits & 0x007FFFFFu) != 0, 0)) {   // (uniform; the scales that the append writes are powers of two)
+        const float rest = __builtin_bit_cast(float, (v_bits & 0x007FFFFFu) | 0x3F800000u);
+        log_rest = __builtin_amdgcn_logf(rest);
+        inv_rest = 1.0f / rest;
+      }
 #pragma unroll
-      for (int j = 0; j < VL; ++j) *(FLUX_LDS u32x4*)(vs_lds + (j * RPL + l / CPR) * VROW + 16 * (l % CPR)) = vreg[j];
+      for (int j = 0; j < VL; ++j) *(FLUX_LDS u32x4*)(vs_lds + (j * RPL / 16) * VBLOCK + (j * RPL % 16 + l / CPR) * VROW + 16 * (l % CPR)) = vreg[j];
       // ---- scores: s[sb][i] is key 16 * sb + 4 * g + i of the page against query n
       f32x4 s[4];
 #pragma unroll
-      for (int sb = 0; sb < 4; ++sb) {
-        s[sb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int sb = 0; sb < 4; ++sb) s[sb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          s[sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack8(kreg[sb][kk][0], kreg[sb][kk][1]), qf[2 * kk], s[sb], 0, 0, 0);
-          s[sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack8(kreg[sb][kk][2], kreg[sb][kk][3]), qf[2 * kk + 1], s[sb], 0, 0, 0);
-        }
-      }
+      for (int kk = 0; kk < 2 * KK; ++kk)
+#pragma unroll
+        for (int sb = 0; sb < 4; ++sb)
+          s[sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack8(kreg[sb][kk >> 1][2 * (kk & 1)], kreg[sb][kk >> 1][2 * (kk & 1) + 1], 1.0f), qf[kk], s[sb], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
       const int next = x1 - p > W ? p + W : x1;
       if (next < x1) {
@@ -286,8 +294,6 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
         if (l == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
         continue;
       }
-#pragma unroll
-      for (int sb = 0; sb < 4; ++sb) s[sb] *= c;
       if (!is_full(pos)) {
 #pragma unroll
         for (int sb = 0; sb < 4; ++sb)
@@ -297,43 +303,61 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
             if (key >= place.len || (list.tail_start != list.s_end && key >= list.s_end && key < list.tail_start)) s[sb][j] = -INFINITY;
           }
       }
-      // ---- online softmax (row maximum over the 4 lane groups of this query)
-      float mloc = m_run;
+      // ---- weights against the reference that the accumulators refer to, without looking for the page's maximum first: any
+      // reference gives the same quotient.  Only where a weight leaves the guarded range, or a query has no reference yet, the
+      // maximum is taken (over the 4 lane groups of a query), the references move there and the weights are taken again.
+      float e[16], psum;
+      auto weights = [&]() __attribute__((always_inline)) {
+        const float shift = log_rest - m_run;
+        psum = 0.f;
 #pragma unroll
-      for (int sb = 0; sb < 4; ++sb) mloc = fmaxf(mloc, fmaxf(fmaxf(s[sb][0], s[sb][1]), fmaxf(s[sb][2], s[sb][3])));
-      mloc = fmaxf(mloc, __shfl_xor(mloc, 16));
-      mloc = fmaxf(mloc, __shfl_xor(mloc, 32));
-      const float alpha = fast_exp2(m_run - mloc);
-      m_run = mloc;
-      float psum = 0.f;
-      uint32_t pk[8], rest[8];
-#pragma unroll
-      for (int sb = 0; sb < 4; ++sb)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float ea = fast_exp2(s[sb][2 * j] - mloc), eb = fast_exp2(s[sb][2 * j + 1] - mloc);
-          psum += ea + eb;
-          const float pa = ea * vsc, pb = eb * vsc;
-          const uint32_t hi = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, pb), __builtin_bit_cast(uint32_t, pa), 0x07060302u);
-          pk[2 * sb + j] = hi;
-          rest[2 * sb + j] = pack_bf16(pa - bf16_lo(hi), pb - bf16_hi(hi));
+        for (int j = 0; j < 16; ++j) {
+          e[j] = fast_exp2(__builtin_fmaf(s[j >> 2][j & 3], c, shift));
+          psum += e[j];
         }
-      l_run = l_run * alpha + psum;
-      // ---- O^T += V^T P^T, 32 keys at a time: lane (n, g) has the keys 32 kh + 4 g + (0..3) and 16 more of P, and takes the same of V
+      };
+      weights();
+      if (__builtin_amdgcn_ballot_w64(!(psum < kPagedGuard)) != 0) {
+        float m = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
-      for (int db = 0; db < DB; ++db) o[db] *= alpha;
+        for (int sb = 1; sb < 4; ++sb) m = fmaxf(m, fmaxf(fmaxf(s[sb][0], s[sb][1]), fmaxf(s[sb][2], s[sb][3])));
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m_run, fmaxf(m, __shfl_xor(m, 32)) * c);
+        const float alpha = fast_exp2(m_run - m);
+        m_run = m;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] *= alpha;
+        weights();
+      }
+      l_run = __builtin_fmaf(psum, inv_rest, l_run);
+      // O^T += V^T P^T, 32 keys at a time: lane (n, g) has the keys 32 kh + 4 g + (0..3) and 16 more of P, and takes the same of V.
+      // TERMS bf16 values make a weight: two leave 2^-16 of it (see decode.hip), three 2^-24, which is what an fp32 output holds
+      // (8/2 heads of 64, 2001 keys: 2-norm of the error 3.7e-6 of the result's with two).
+      constexpr int TERMS = FP32 ? 3 : 2;
+      uint32_t pk[TERMS][8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float x = e[2 * j], y = e[2 * j + 1];
+#pragma unroll
+        for (int t = 0; t < TERMS - 1; ++t) {              // the upper bits of what is left
+          pk[t][j] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
+          x -= bf16_lo(pk[t][j]);
+          y -= bf16_hi(pk[t][j]);
+        }
+        pk[TERMS - 1][j] = pack_bf16(x, y);
+      }
 #pragma unroll
       for (int kh = 0; kh < 2; ++kh) {
-        const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pk[4 * kh], pk[4 * kh + 1], pk[4 * kh + 2], pk[4 * kh + 3]});
-        const bf16x8 pr = __builtin_bit_cast(bf16x8, u32x4{rest[4 * kh], rest[4 * kh + 1], rest[4 * kh + 2], rest[4 * kh + 3]});
         const int j = n >> 1;
-        FLUX_LDS char* const src = vs_lds + (32 * kh + 4 * g + (j & 3) + 16 * (j >> 2)) * VROW + 8 * (n & 1);
+        FLUX_LDS char* const src = vs_lds + (2 * kh + (j >> 2)) * VBLOCK + (4 * g + (j & 3)) * VROW + 8 * (n & 1);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           const i32x2 t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((FLUX_LDS i32x2*)(src + 16 * db));
-          const bf16x8 vf = unpack8((uint32_t)t[0], (uint32_t)t[1]);
-          o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[db], 0, 0, 0);
-          o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pr, o[db], 0, 0, 0);
+          const bf16x8 vf = unpack8((uint32_t)t[0], (uint32_t)t[1], v_power);
+#pragma unroll
+          for (int i = 0; i < TERMS; ++i)
+            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, u32x4{pk[i][4 * kh], pk[i][4 * kh + 1], pk[i][4 * kh + 2], pk[i][4 * kh + 3]}), o[db], 0, 0, 0);
         }
       }
     }
@@ -373,7 +397,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
     __syncthreads();
     auto store_out = [&](int qi, int d, f32x4 r) __attribute__((always_inline)) {
       const int64_t off = out0 + qi * D + d;
-      if (a.out_fp32) *(f32x4*)((float*)a.out + off) = r;
+      if constexpr (FP32) *(f32x4*)((float*)a.out + off) = r;
       else *(u32x2*)((__bf16*)a.out + off) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
     };
     const int row0 = part_place(first, wg - first) * a.rpu;
@@ -458,18 +482,22 @@ hipError_t launch_decode_paged(const Ctx& c, const flux_attn_cfg& cfg, const voi
   a.status = c.status;
   a.arrived = c.decode_counters;
   a.out = out;
-  a.out_fp32 = cfg.out_dtype;
   const dim3 grid(plan.wgs);
   // rows that are evicted before the next step are fetched with nontemporal loads (see launch_decode)
   const bool nt = 2.0 * pt.batch * cfg.n_kv_heads * cfg.head_dim * (double)max_kv_len > 64.0 * 1024 * 1024;
-  auto launch = [&](auto d) {
+  auto launch = [&](auto d, auto fp32) {
     constexpr int D = decltype(d)::value;
-    if (plan.waves == 8) hipLaunchKernelGGL((paged_decode_kernel<D, false, 8>), grid, dim3(512), 0, s, a);
-    else if (nt) hipLaunchKernelGGL((paged_decode_kernel<D, true, 4>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_decode_kernel<D, false, 4>), grid, dim3(256), 0, s, a);
+    constexpr bool FP32 = decltype(fp32)::value;
+    if (plan.waves == 8) hipLaunchKernelGGL((paged_decode_kernel<D, false, 8, FP32>), grid, dim3(512), 0, s, a);
+    else if (nt) hipLaunchKernelGGL((paged_decode_kernel<D, true, 4, FP32>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_decode_kernel<D, false, 4, FP32>), grid, dim3(256), 0, s, a);
   };
-  if (cfg.head_dim == 128) launch(std::integral_constant<int, 128>());
-  else launch(std::integral_constant<int, 64>());
+  auto launch_d = [&](auto d) {
+    if (cfg.out_dtype != 0) launch(d, std::true_type());
+    else launch(d, std::false_type());
+  };
+  if (cfg.head_dim == 128) launch_d(std::integral_constant<int, 128>());
+  else launch_d(std::integral_constant<int, 64>());
   return hipGetLastError();
 }
 

@@ -49,7 +49,6 @@ struct PagedPrefillArgs {
   i32x4* tile_info;       // whether tiles are shared out; behind it, [batch][hkv][n_qtiles]: first unit, unit stride, units of the tile
 };
 
-constexpr float kPagedGuard = 1073741824.0f;  // 2^30: a page whose weights sum past this moves the reference
 constexpr int kPagedNoSplit = 0x3FFFFFFF;
 
 __device__ __forceinline__ int quotient(int n, Reciprocal d) { return (int)(((uint32_t)(((uint64_t)(uint32_t)n * d.mul) >> 32) + (uint32_t)n) >> d.shift); }

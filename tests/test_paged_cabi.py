@@ -91,13 +91,17 @@ def test_attention(F, nodev, prefill):
 def test_the_binding_checks_shapes_and_layouts(F):
     import torch
     kv = F.PagedKV.empty(3, 2, 64, device="cpu")
-    assert kv.k.shape == (3, 2, 64, 64) and kv.k.dtype == torch.float8_e4m3fn and C.sizeof(F.FluxPagedKV) == len(F._paged_kv_arg(kv))
+    assert kv.k.shape == (3, 2, 64, 64) and kv.k.dtype == torch.float8_e4m3fn and C.sizeof(F.FluxPagedKV) == len(kv.packed)
     pt = F.PageTable.empty(2, 3, 5, device="cpu")
-    assert len(F._pages_arg(pt)) == C.sizeof(F.FluxPageTable) and pt.n_free.tolist() == [3] and pt.free_pages.tolist() == [2, 1, 0]
-    for bad in (F.PagedKV(kv.k[:, :, :32], kv.v[:, :, :32], kv.k_scale, kv.v_scale), F.PagedKV(kv.k, kv.v.transpose(0, 1).contiguous().transpose(0, 1), kv.k_scale, kv.v_scale),
-                F.PagedKV(kv.k.float(), kv.v.float(), kv.k_scale, kv.v_scale), F.PagedKV(kv.k, kv.v, kv.k_scale[:, :1], kv.v_scale),
-                F.PagedKV(kv.k, kv.v, kv.k_scale, kv.v_scale.t().contiguous().t())):
+    assert len(pt.packed) == C.sizeof(F.FluxPageTable) and pt.n_free.tolist() == [3] and pt.free_pages.tolist() == [2, 1, 0]
+    k, v, ks, vs = kv.k, kv.v, kv.k_scale, kv.v_scale
+    for bad in ((k[:, :, :32], v[:, :, :32], ks, vs), (k, v.view(torch.uint8).transpose(0, 1).contiguous().transpose(0, 1), ks, vs),
+                (k.float(), v.float(), ks, vs), (k, v, ks[:, :1], vs), (k, v, ks, vs.t().contiguous().t()), (k, v, ks.double(), vs)):
         with pytest.raises(AssertionError):
-            F._paged_kv_arg(bad)
-    with pytest.raises(AssertionError):
-        F._pages_arg(F.PageTable(pt.table.t(), pt.kv_len, pt.free_pages, pt.n_free))
+            F.PagedKV(*bad)
+    t = (pt.table, pt.kv_len, pt.free_pages, pt.n_free)
+    for i, bad in ((0, pt.table.t()), (0, pt.table.long()), (1, pt.kv_len[:1]), (2, pt.free_pages[::2]), (3, pt.free_pages)):
+        with pytest.raises(AssertionError):
+            F.PageTable(*t[:i], bad, *t[i + 1:])
+    with pytest.raises(AttributeError):                      # a handle's tensors stay its own
+        pt.table = pt.table.clone()
