@@ -6,7 +6,7 @@
 namespace flux {
 
 constexpr int kPageTokens = FLUX_PAGE_TOKENS;
-constexpr int kPlanRows = 2048;               // slots that a workgroup of flux_page_plan writes
+constexpr int kPlanRows = 1024;               // slots that a workgroup of flux_page_plan writes
 constexpr float kPagedGuard = 1073741824.0f;  // 2^30: a page whose weights sum past this moves the softmax reference
 constexpr long long kAppendPagedFew = 16384;  // (rows, heads) of an append up to which a wave looks after one row
 constexpr int kMinScaleExp = -100;            // of the scale of a block; its codes reach down to 2^-109

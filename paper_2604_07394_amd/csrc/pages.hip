@@ -48,14 +48,18 @@ __device__ __forceinline__ int exclusive_sum(int x, int* sums, int& total) {
 
 __device__ __forceinline__ int clamped(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
+// A workgroup of 256 threads writes kPlanRows slots, a few per thread that are looked up side by side, and its share of the table
+// entries.  What a step of some hundred sequences takes is memory latencies one behind the other: the lengths; the page that a
+// sequence goes on in; the free pages, asked for together.  A launch of one workgroup has nobody to wait for.
 __global__ __launch_bounds__(256) void page_plan_kernel(PageArgs a) {
-  __shared__ int s_begin[kMaxBatch + 1], s_len[kMaxBatch], s_start[kMaxBatch], s_limit[kMaxBatch], s_sums[4], s_last;
+  __shared__ int s_begin[kMaxBatch + 1], s_len[kMaxBatch], s_start[kMaxBatch], s_limit[kMaxBatch], s_page[kMaxBatch], s_free[256], s_sums[4], s_last;
   const int tid = threadIdx.x;
   const int cap = a.table_pages << 6;                        // (table_pages <= 2^24)
   const int n_free = *a.n_free, avail = clamped(n_free, 0, a.n_pages);
+  const int next_free = tid < avail ? a.free_pages[avail - 1 - tid] : -1;   // the pages given out first: asked for along with the lengths
   uint32_t bad = n_free != avail ? FLUX_DEV_BAD_LENGTH : 0;
   const int run = (a.batch + 255) >> 8, b0 = tid * run, b1 = min(b0 + run, a.batch);
-  // lengths and rows of this thread's sequences, and the pages that they lack
+  // lengths and rows of this thread's sequences, the page that they go on in, and the pages that they lack
   int needed = 0;
   for (int b = b0; b < b1; ++b) {
     const int got = a.kv_len[b], from = a.cu[b], to = a.cu[b + 1];
@@ -63,18 +67,24 @@ __global__ __launch_bounds__(256) void page_plan_kernel(PageArgs a) {
     if (got != len || begin != from || end != to || end < begin) bad |= FLUX_DEV_BAD_LENGTH;
     const int n = end > begin ? end - begin : 0;
     int limit = (int)min((int64_t)len + n, (int64_t)cap);    // the length with all rows that the table has room for
-    if (n > 0 && (len & 63) != 0 && (uint32_t)a.table[(int64_t)b * a.table_pages + (len >> 6)] >= (uint32_t)a.n_pages) {
-      bad |= FLUX_DEV_BAD_PAGE;
-      limit = len;
+    int page = 0;
+    if (n > 0 && (len & 63) != 0) {
+      page = a.table[(int64_t)b * a.table_pages + (len >> 6)];
+      if ((uint32_t)page >= (uint32_t)a.n_pages) {
+        bad |= FLUX_DEV_BAD_PAGE;
+        limit = len;
+      }
     }
     if (limit - len < n) bad |= FLUX_DEV_KV_OVERFLOW;
     s_begin[b] = begin;
     if (b == a.batch - 1) s_begin[a.batch] = end;
     s_len[b] = len;
+    s_page[b] = page;
     s_limit[b] = limit;
     s_start[b] = needed;
     needed += ((limit + 63) >> 6) - ((len + 63) >> 6);
   }
+  s_free[tid] = next_free;
   int total;
   const int before = exclusive_sum<4>(needed, s_sums, total);
   for (int b = b0; b < b1; ++b) {
@@ -89,45 +99,66 @@ __global__ __launch_bounds__(256) void page_plan_kernel(PageArgs a) {
   if (blockIdx.x != 0) bad = 0;                              // (once per launch)
   __syncthreads();
 
-  const int taken = min(total, avail);
-  for (int i = blockIdx.x * 256 + tid; i < taken; i += gridDim.x * 256) {
-    const int b = last_not_above(s_start, a.batch, i);
-    int page = a.free_pages[avail - 1 - i];
+  auto free_page = [&](int i) { return i < 256 ? s_free[i] : a.free_pages[avail - 1 - i]; };
+  // the sequences of this thread's rows and of its first new page, looked up side by side
+  constexpr int U = kPlanRows / 256;
+  const int taken = min(total, avail), stride = gridDim.x * 256;
+  const int64_t t0 = (int64_t)blockIdx.x * kPlanRows + tid;
+  int i = blockIdx.x * 256 + tid;
+  int seq[U + 1];
+#pragma unroll
+  for (int j = 0; j <= U; ++j) seq[j] = 0;
+  for (int step = a.batch > 1 ? 1 << (31 - __builtin_clz(a.batch - 1)) : 0; step > 0; step >>= 1) {
+#pragma unroll
+    for (int j = 0; j <= U; ++j) {
+      const int mid = seq[j] + step;
+      const int first = mid < a.batch ? (j < U ? s_begin[mid] : s_start[mid]) : 0x7FFFFFFF;
+      if (first <= (j < U ? (int)(t0 + 256 * j) : i)) seq[j] = mid;
+    }
+  }
+  int slot[U], row[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t t = t0 + 256 * j;
+    const int b = seq[j], len = s_len[b];
+    const int64_t at = (int64_t)len + ((int)t - s_begin[b]);
+    slot[j] = -1;
+    row[j] = 0;
+    if (t < a.total && t >= s_begin[b] && t < s_begin[b + 1] && at < s_limit[b]) {
+      const int pos = (int)at, used = (len + 63) >> 6, p = pos >> 6;
+      slot[j] = p >= used ? free_page(s_start[b] + p - used) : s_page[b];
+      row[j] = pos & 63;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int64_t t = t0 + 256 * j;
+    if (t < a.total) a.slots[t] = (uint32_t)slot[j] < (uint32_t)a.n_pages ? (slot[j] << 6) + row[j] : -1;
+  }
+  for (int b = seq[U]; i < taken;) {
+    int page = free_page(i);
     if ((uint32_t)page >= (uint32_t)a.n_pages) {
       bad |= FLUX_DEV_BAD_PAGE;
       page = -1;
     }
     a.table[(int64_t)b * a.table_pages + ((s_len[b] + 63) >> 6) + (i - s_start[b])] = page;
-  }
-  const int t0 = blockIdx.x * kPlanRows, t1 = (int)min((int64_t)t0 + kPlanRows, (int64_t)a.total);
-  for (int t = t0 + tid; t < t1; t += 256) {
-    int slot = -1;
-    if (t >= s_begin[0]) {
-      const int b = last_not_above(s_begin, a.batch, t);
-      const int len = s_len[b];
-      const int64_t at = (int64_t)len + (t - s_begin[b]);
-      if (t >= s_begin[b] && t < s_begin[b + 1] && at < s_limit[b]) {
-        const int pos = (int)at, used = (len + 63) >> 6, i = pos >> 6;
-        const int page = i < used ? a.table[(int64_t)b * a.table_pages + i] : a.free_pages[avail - 1 - (s_start[b] + i - used)];
-        if ((uint32_t)page < (uint32_t)a.n_pages) slot = (page << 6) + (pos & 63);
-      }
-    }
-    a.slots[t] = slot;
+    i += stride;
+    if (i < taken) b = last_not_above(s_start, a.batch, i);
   }
   if (bad) atomicOr(a.status, bad);
 
   // the last workgroup to arrive writes the lengths: the others only read them, and a thread's loads have returned before the
   // barrier lets thread 0 count the arrival
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  if (tid == 0) s_last = atomicAdd(a.counter, 1u) == gridDim.x - 1;
-  __syncthreads();
-  if (!s_last) return;
-  for (int b = tid; b < a.batch; b += 256) a.kv_len[b] = s_limit[b];
-  if (tid == 0) {
-    *a.n_free = avail - taken;
-    *a.counter = 0;                                          // ready for the next launch on this stream
+  if (gridDim.x > 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) s_last = atomicAdd(a.counter, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!s_last) return;
+    if (tid == 0) *a.counter = 0;                            // ready for the next launch on this stream
   }
+  for (int b = tid; b < a.batch; b += 256) a.kv_len[b] = s_limit[b];
+  if (tid == 0) *a.n_free = avail - taken;
 }
 
 // Release.  One workgroup: the pages that go back, counted by sequence and place, are listed last one first, so that a plan
