@@ -19,7 +19,8 @@ struct PagedAppendArgs {
   int64_t stride_p, stride_h, stride_t;
   const int32_t* slots;
   int hkv, total, n_pages;
-  long long units;                // (tile of ROWS token rows, head, K or V)
+  long long units;                // (tile of 64 token rows, head, K or V, 2^share)
+  int share;
   uint32_t* status;
 };
 
@@ -43,35 +44,36 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, f
 }
 __device__ __forceinline__ float finite_or_nan(float x) { return x - x == 0.f ? x : __builtin_nanf(""); }
 
-// ROWS: token rows that a wave looks after: it does every block that begins in them.  1 where there are few rows, so that the
-// blocks of a decode step are worked on side by side; 64 for long prompts, where a page's rows begin in every tile.
-template <int D, int ROWS>
+// A wave looks at 64 token rows, where blocks begin in them, and does one block in 2^share for one head, K or V: in a decode step
+// every row begins a block, in a long prompt one or two of 64 do, and only the slots tell which it is.  So short calls have as many
+// waves as there may be blocks, and long ones about kAppendPagedWaves at least, most of which leave at once: us with 1024 / 2048 / 4096
+// / 8192 of them, 8 heads of 128, one row of 256 sequences 9.4 / 6.8 / 7.1 / 7.0, five of each 16.4 / 11.3 / 8.2 / 8.3, 512 rows of one
+// 6.0 / 7.0 / 7.8 / 10.8, 2100 rows of three 6.4 / 7.0 / 8.1 / 12.0, 8000 of four 13.4 / 13.5 / 12.3 / 13.1.  (32768 rows 42.4: 4.75 TB/s
+// read and written; a plain copy of 1 GB reaches 5.2.)
+template <int D>
 __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a) {
   constexpr int LPR = D / 8;                                 // lanes per row, 16 bytes each
   constexpr int RPS = 64 / LPR;                              // rows per step
   constexpr int STEPS = 64 / RPS;
   const int l = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per_tile = 2 * a.hkv;
+  const int per_tile = (2 * a.hkv) << a.share;
   for (long long u = (long long)blockIdx.x * 4 + w; u < a.units; u += (long long)gridDim.x * 4) {
     const int tile = (int)(u / per_tile), rest = (int)(u - (long long)tile * per_tile);
-    const int h = rest >> 1;
-    const bool is_v = rest & 1;
-    const int t0 = tile * ROWS;
+    const int turn = rest & ((1 << a.share) - 1), h = rest >> (a.share + 1);
+    const bool is_v = (rest >> a.share) & 1;
+    const int t0 = tile * 64;
     // where blocks begin: a row whose slot does not follow that of the row before in the same page
-    uint64_t begins = 1;
-    if (ROWS > 1) {
-      const int t = t0 + l;
-      const int s = t < a.total ? a.slots[t] : -1, p = t > 0 && t < a.total ? a.slots[t - 1] : -1;
-      begins = __builtin_amdgcn_ballot_w64(s >= 0 && !(p == s - 1 && (s & 63) != 0));
-    }
+    const int t_mine = t0 + l;
+    const int s = t_mine < a.total ? a.slots[t_mine] : -1, p = t_mine > 0 && t_mine < a.total ? a.slots[t_mine - 1] : -1;
+    uint64_t begins = __builtin_amdgcn_ballot_w64(s >= 0 && !(p == s - 1 && (s & 63) != 0));
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(begins >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)begins, 0));
+    begins &= __builtin_amdgcn_ballot_w64((before & ((1 << a.share) - 1)) == turn);
     while (begins != 0) {
       const int t = t0 + __builtin_ctzll(begins);
       begins &= begins - 1;
       const int mine = t + l < a.total ? a.slots[t + l] : -1;
       const int slot = __builtin_amdgcn_readfirstlane(mine);
-      if (slot < 0) break;                                   // (ROWS = 1: the row has no place)
-      if (ROWS == 1 && (slot & 63) != 0 && t > 0 && a.slots[t - 1] == slot - 1) break;   // belongs to the block of the row before
       const int page = slot >> 6, first = slot & 63;
       if (page >= a.n_pages) {
         if (l == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
@@ -169,17 +171,14 @@ hipError_t launch_kv_append_paged(const Ctx& c, const flux_paged_kv& kv, int hkv
   a.total = total_new;
   a.n_pages = kv.n_pages;
   a.status = c.status;
-  const bool few = (long long)total_new * hkv <= kAppendPagedFew;
-  a.units = ((long long)total_new + (few ? 0 : 63)) / (few ? 1 : 64) * 2 * hkv;
+  const long long tiles = ((long long)total_new + 63) / 64 * 2 * hkv;
+  a.share = 6;
+  while (a.share > 0 && (tiles << a.share) > kAppendPagedWaves) --a.share;
+  a.units = tiles << a.share;
   const long long wgs = (a.units + 3) / 4;
   const dim3 grid((unsigned)(wgs < kAppendMost ? wgs : kAppendMost)), block(256);
-  if (d == 128) {
-    if (few) hipLaunchKernelGGL((kv_append_paged_kernel<128, 1>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((kv_append_paged_kernel<128, 64>), grid, block, 0, s, a);
-  } else {
-    if (few) hipLaunchKernelGGL((kv_append_paged_kernel<64, 1>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((kv_append_paged_kernel<64, 64>), grid, block, 0, s, a);
-  }
+  if (d == 128) hipLaunchKernelGGL((kv_append_paged_kernel<128>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((kv_append_paged_kernel<64>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

@@ -8,7 +8,7 @@ namespace flux {
 constexpr int kPageTokens = FLUX_PAGE_TOKENS;
 constexpr int kPlanRows = 1024;               // slots that a workgroup of flux_page_plan writes
 constexpr float kPagedGuard = 1073741824.0f;  // 2^30: a page whose weights sum past this moves the softmax reference
-constexpr long long kAppendPagedFew = 16384;  // (rows, heads) of an append up to which a wave looks after one row
+constexpr long long kAppendPagedWaves = 4096; // an append takes as many as that where blocks may be many (see kv_append_paged_kernel)
 constexpr int kMinScaleExp = -100;            // of the scale of a block; its codes reach down to 2^-109
 
 hipError_t launch_page_plan(const Ctx& c, const flux_page_table& pt, const int32_t* cu_new, int total_new, int32_t* slots, hipStream_t s);
