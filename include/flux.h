@@ -356,7 +356,9 @@ int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* 
  * finite scale >= 0; one of V below 2^-126 counts as that).  A tile of query rows holds all heads
  * of a group, token by token, and walks only pages of which a row sees something; pages of a tile may be shared out over several
  * workgroups where max_kv_len >= 1024, as far as the workspace has room for their results (any context will do), in a way that
- * depends on the bounds, lengths and modes of the whole batch.  max_q_len * group <= 2^30, and
+ * depends on the bounds, lengths and modes of the whole batch.  Where max_q_len * group <= 32 the rows of a sequence are worked on
+ * like a decode call's.  kv_len[b] above max_kv_len raises FLUX_DEV_BAD_LENGTH (the oldest pages may be all that such a sequence is
+ * computed from).  max_q_len * group <= 2^30, and
  * batch * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^22 is always enough (FLUX_EINVAL).
  * What lies behind kv_len[b] in a page is never used; the codes of a page of which a row of a tile sees something must not be NaN
  * below that, or rows of the tile that do not see them may become NaN as well.  A table entry outside the pool counts as a page that is

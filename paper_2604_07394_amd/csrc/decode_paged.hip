@@ -37,10 +37,10 @@ struct PagedSplit {
 struct PageList {
   int pages, seam, skip, s_end, tail_start;
 };
-__device__ __forceinline__ PageList page_list(const PagedSplit& s, int len, int md) {
+__device__ __forceinline__ PageList page_list(const PagedSplit& s, int len, int md, int first) {   // first: position of the first query
   PageList r;
   r.s_end = min(len, s.sink_lim);
-  const int lo = len > 0 ? window_start(len - 1, s.blk_shift, s.win_blocks) : 0;
+  const int lo = len > 0 ? window_start(first, s.blk_shift, s.win_blocks) : 0;
   r.tail_start = max(lo, r.s_end);
   if ((md & 1) != 0) r.tail_start = r.s_end;                 // FA: nothing is hidden
   r.seam = (r.s_end + 63) >> 6;
@@ -53,8 +53,24 @@ __device__ __forceinline__ Seq load_counted(const PagedSplit& s, int b, bool& ba
   Seq q;
   q.len = got < 0 ? 0 : min(got, s.capacity);
   q.md = s.mode[b] != 0 ? 1 : 0;
-  q.nb = page_list(s, q.len, q.md).pages;
+  q.nb = page_list(s, q.len, q.md, q.len - 1).pages;
   bad |= got != q.len || q.nb > s.max_pages;
+  q.nb = min(q.nb, s.max_pages);
+  return q;
+}
+
+// Runs of a few queries per sequence (batches of up to 64): every lane holds the number of its sequence's.
+struct RunSplit : PagedSplit {
+  int n_q;
+};
+__device__ __forceinline__ Seq load_counted(const RunSplit& s, int b, bool& bad) {
+  const int got = s.kv_len[b];
+  Seq q;
+  q.len = got < 0 ? 0 : min(got, s.capacity);
+  q.md = s.mode[b] != 0 ? 1 : 0;
+  const int n = s.n_q < 0 ? 0 : min(s.n_q, q.len);
+  q.nb = n > 0 ? page_list(s, q.len, q.md, q.len - n).pages : 0;
+  bad |= got != q.len || n != s.n_q || q.nb > s.max_pages;
   q.nb = min(q.nb, s.max_pages);
   return q;
 }
@@ -67,7 +83,10 @@ struct PagedDecodeArgs {
   const int32_t* table;
   int table_pages, n_pages;
   PagedSplit sp;
-  int hq, hkv, group, qblocks, rpu;      // see DecodeArgs in decode.hip
+  int hq, hkv, group, qblocks, rpu;      // see DecodeArgs in decode.hip; runs: one pair per KV head, rpu = max_q * group
+  const int32_t* cu_q;    // runs only
+  int max_q;              // queries of a run that are computed
+  Reciprocal by_group;
   float scale_log2;
   float* part_o;
   float* part_ml;         // reference (log2 units) and weight sum
@@ -85,9 +104,14 @@ __device__ __forceinline__ bf16x8 unpack8(uint32_t lo, uint32_t hi, float scale)
   return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)});
 }
 
-// FP32: the outputs are fp32, and a weight takes three bf16 terms (bf16 outputs: two)
-template <int D, bool NT, int W, bool FP32>
-__global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs a) {
+// FP32: the outputs are fp32, and a weight takes three bf16 terms (bf16 outputs: two).
+// QB: 0, one query per sequence.  Otherwise the last n_q(b) positions of every sequence are queries (a step of speculative decoding),
+// whose rows, token by token the heads of a group, take QB blocks of 16 columns: K and V are read once for all of them.
+// (Two blocks at head dimension 128 take more registers than two workgroups per CU leave.)
+template <int D, bool NT, int W, bool FP32, int QB>
+__global__ __launch_bounds__(64 * W, runs_per_cu(D, QB)) void paged_decode_kernel(PagedDecodeArgs a) {
+  constexpr bool RUN = QB > 0;
+  constexpr int NB = RUN ? QB : 1;    // blocks of 16 columns
   constexpr int KK = D / 64;          // 16-byte K loads per lane and 16 keys
   constexpr int DB = D / 16;          // 16-wide output blocks over the head dimension
   constexpr int CPR = D / 16;         // 16-byte chunks per row
@@ -110,15 +134,27 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
   __shared__ u32x2 s_seq[W == 8 ? kDecodeFewWgs : kDecodeTable];   // (a call of eight waves has no more sequences than workgroups)
   SeqTable* const seqs = (SeqTable*)s_seq;
   Lanes lanes;
-  const Cut cut = find_cut<D, W>(a.sp, l, w, seqs, lanes);
+  typedef typename std::conditional<RUN, RunSplit, PagedSplit>::type Split;
+  Split split;
+  static_cast<PagedSplit&>(split) = a.sp;
+  int q_begin_mine = 0;
+  if constexpr (RUN) {
+    split.n_q = 0;
+    if (l < a.sp.batch) {
+      q_begin_mine = a.cu_q[l];
+      split.n_q = q_begin_mine < 0 ? -1 : a.cu_q[l + 1] - q_begin_mine;
+    }
+  }
+  const Cut cut = find_cut<D, W>(split, l, w, seqs, lanes);
   if constexpr (W == 8) __builtin_assume(cut.align > 0);
   if (wg == 0 && lanes.bad) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_LENGTH);
   // rows of sequences without keys are zero: shared out over the workgroups
   auto zero_rows = [&]() __attribute__((always_inline)) {
+    if constexpr (RUN) return;                               // (a run is not longer than what is cached)
     if (__builtin_amdgcn_ballot_w64(lanes.run > 1 || (l < a.sp.batch && lanes.q.nb == 0)) == 0) return;
     for (int b = wg; b < a.sp.batch; b += (int)gridDim.x) {
       const int i = b / lanes.run, j = b - i * lanes.run;
-      if ((lanes.run == 1 ? __builtin_amdgcn_readlane(lanes.q.nb, i) : seq_at(a.sp, seqs, lanes.run, i, j).nb) != 0) continue;
+      if ((lanes.run == 1 ? __builtin_amdgcn_readlane(lanes.q.nb, i) : seq_at(split, seqs, lanes.run, i, j).nb) != 0) continue;
       const int64_t off = (int64_t)b * a.hq * D;
       for (int x = 8 * tid; x < a.hq * D; x += 8 * 64 * W) {
         const u32x4 zero = {0, 0, 0, 0};
@@ -137,7 +173,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
   }
   int at = range_begin(cut, wg);
   const int range_end = range_begin(cut, wg + 1);
-  Place place = find_place(a.sp, cut, lanes, l, seqs, at);
+  Place place = find_place(split, cut, lanes, l, seqs, at);
   const int rows_at = at - place.begin;
   int pair = __builtin_amdgcn_readfirstlane((int)((float)rows_at / (float)place.nb));   // (put right below: the quotient may be off by one)
   pair -= pair * place.nb > rows_at ? 1 : 0;
@@ -149,12 +185,19 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
   const char *kbase, *vbase;
   const float *kscale, *vscale;
   const int32_t* pages;
+  int first_pos, run_rows;                                   // position of the first query, rows of the run that are computed
   auto set_part = [&]() __attribute__((always_inline)) {
     const int kvh = a.qblocks == 1 ? pair : pair / a.qblocks;
     const int begin = place.begin + pair * place.nb;
     x0 = at - begin;
     x1 = min(place.real, range_end - begin);
-    list = page_list(a.sp, place.len, place.md);
+    first_pos = place.len - 1;
+    if constexpr (RUN) {
+      const int n_q = min(__builtin_amdgcn_readlane(split.n_q, place.b), place.len);
+      first_pos = place.len - n_q;
+      run_rows = min(n_q, a.max_q) * a.group;
+    }
+    list = page_list(a.sp, place.len, place.md, first_pos);
     kbase = a.k + (int64_t)kvh * a.stride_h;
     vbase = a.v + (int64_t)kvh * a.stride_h;
     kscale = a.k_scale + kvh;
@@ -183,7 +226,7 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
   const uint32_t v_lane = (l / CPR) * (uint32_t)a.stride_t + 16 * (l % CPR);
   // the page's first position, and whether all of its positions are visible
   auto first_of = [&](int x) __attribute__((always_inline)) { return (x + (x >= list.seam ? list.skip : 0)) << 6; };
-  auto is_full = [&](int pos) __attribute__((always_inline)) {
+  auto is_full = [&](int pos) __attribute__((always_inline)) {   // (for loads: rows that some query sees are all of them)
     return pos + 64 <= place.len && (list.tail_start == list.s_end || pos + 64 <= list.s_end || pos >= list.tail_start);
   };
   auto load_page = [&](int x, int id) __attribute__((always_inline)) {   // both wave-uniform
@@ -221,7 +264,8 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
   };
 
   FLUX_LDS char* const vs_lds = (FLUX_LDS char*)smem + w * VWAVE;
-  bf16x8 qf[2 * KK];
+  bf16x8 qf[NB][2 * KK];
+  int i_mine[NB], w_lo_mine[NB], w_lo_last = 0;              // runs: position of a column's query, start of its window, of the last one's
   int id_now;                                                // number of the page in flight
   auto begin_part = [&]() __attribute__((always_inline)) {
     p = x0 + w;
@@ -235,23 +279,40 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
       load_scales();
     }
     __builtin_amdgcn_sched_barrier(0);
-    // Q operand: lane (n, g) holds d = 64 kk + 16 g + 8 h .. +7 of query head kvh * group + 16 * qb + n in qf[2 kk + h]
-    // (columns past the group's last head repeat its first one; what they give is left out at the end)
+    // Q operand: lane (n, g) holds d = 64 kk + 16 g + 8 h .. +7 of its query row in qf[2 kk + h]: of query head kvh * group + 16 *
+    // qb + n, or of the run's row 16 * qb + n (columns past the last one repeat a row; what they give is left out at the end)
     const int kvh = a.qblocks == 1 ? pair : pair / a.qblocks, qb = a.qblocks == 1 ? 0 : pair % a.qblocks;
-    const int qh = 16 * qb + n;
-    const __bf16* qrow = a.q + ((int64_t)place.b * a.hq + (int64_t)kvh * a.group + (qh < a.group ? qh : 0)) * D;
 #pragma unroll
-    for (int i = 0; i < 2 * KK; ++i) qf[i] = *(const bf16x8*)(qrow + 64 * (i >> 1) + 16 * g + 8 * (i & 1));
+    for (int b = 0; b < NB; ++b) {
+      const __bf16* qrow;
+      if constexpr (RUN) {
+        const int r = min(16 * b + n, run_rows - 1), tok = quotient(r, a.by_group);
+        i_mine[b] = first_pos + tok;
+        w_lo_mine[b] = place.md & 1 ? 0 : window_start(i_mine[b], a.sp.blk_shift, a.sp.win_blocks);
+        qrow = a.q + ((int64_t)(__builtin_amdgcn_readlane(q_begin_mine, place.b) + tok) * a.hq + (int64_t)kvh * a.group + (r - tok * a.group)) * D;
+      } else {
+        const int qh = 16 * qb + n;
+        qrow = a.q + ((int64_t)place.b * a.hq + (int64_t)kvh * a.group + (qh < a.group ? qh : 0)) * D;
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * KK; ++i) qf[b][i] = *(const bf16x8*)(qrow + 64 * (i >> 1) + 16 * g + 8 * (i & 1));
+    }
+    if constexpr (RUN) w_lo_last = place.md & 1 ? 0 : window_start(first_pos + quotient(run_rows - 1, a.by_group), a.sp.blk_shift, a.sp.win_blocks);
     __builtin_amdgcn_sched_barrier(0);
   };
   begin_part();
 
   for (;;) {
     // (a part of pages that are not there leaves this reference and a weight sum of almost nothing: zero rows)
-    float m_run = -1e30f, l_run = 0.f;
-    f32x4 o[DB];
+    float m_run[NB], l_run[NB];
+    f32x4 o[DB][NB];
 #pragma unroll
-    for (int i = 0; i < DB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < NB; ++b) {
+      m_run[b] = -1e30f;
+      l_run[b] = 0.f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     for (int i = 0; p < x1; ++i) {
       const int pos = first_of(p), id = id_now;
@@ -267,15 +328,20 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
       }
 #pragma unroll
       for (int j = 0; j < VL; ++j) *(FLUX_LDS u32x4*)(vs_lds + (j * RPL / 16) * VBLOCK + (j * RPL % 16 + l / CPR) * VROW + 16 * (l % CPR)) = vreg[j];
-      // ---- scores: s[sb][i] is key 16 * sb + 4 * g + i of the page against query n
-      f32x4 s[4];
+      // ---- scores: s[sb][b][i] is key 16 * sb + 4 * g + i of the page against query column (b, n)
+      f32x4 s[4][NB];
 #pragma unroll
-      for (int sb = 0; sb < 4; ++sb) s[sb] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int sb = 0; sb < 4; ++sb)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[sb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < 2 * KK; ++kk)
 #pragma unroll
-        for (int sb = 0; sb < 4; ++sb)
-          s[sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(unpack8(kreg[sb][kk >> 1][2 * (kk & 1)], kreg[sb][kk >> 1][2 * (kk & 1) + 1], 1.0f), qf[kk], s[sb], 0, 0, 0);
+        for (int sb = 0; sb < 4; ++sb) {
+          const bf16x8 kf = unpack8(kreg[sb][kk >> 1][2 * (kk & 1)], kreg[sb][kk >> 1][2 * (kk & 1) + 1], 1.0f);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) s[sb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[b][kk], s[sb][b], 0, 0, 0);
+        }
       __builtin_amdgcn_sched_barrier(0);
       const int next = x1 - p > W ? p + W : x1;
       if (next < x1) {
@@ -294,59 +360,76 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
         if (l == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
         continue;
       }
-      if (!is_full(pos)) {
+      if constexpr (RUN) {
+        const bool all = pos + 63 <= first_pos && ((place.md & 1) != 0 || pos + 64 <= a.sp.sink_lim || pos >= w_lo_last);
+        if (!all) {                                          // some column does not see all of the page
 #pragma unroll
-        for (int sb = 0; sb < 4; ++sb)
+          for (int b = 0; b < NB; ++b) {
+            const int hi = i_mine[b] - pos - 4 * g, lo = w_lo_mine[b] - pos - 4 * g, sl = a.sp.sink_lim - pos - 4 * g;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int key = pos + 16 * sb + 4 * g + j;
-            if (key >= place.len || (list.tail_start != list.s_end && key >= list.s_end && key < list.tail_start)) s[sb][j] = -INFINITY;
+            for (int j = 0; j < 16; ++j) {
+              const int k = 16 * (j >> 2) + (j & 3);
+              if (!((k <= hi) & ((k < sl) | (k >= lo)))) s[j >> 2][b][j & 3] = -INFINITY;
+            }
           }
+        }
+      } else if (!is_full(pos)) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int key = pos + 16 * (j >> 2) + 4 * g + (j & 3);
+          if (key >= place.len || (list.tail_start != list.s_end && key >= list.s_end && key < list.tail_start)) s[j >> 2][0][j & 3] = -INFINITY;
+        }
       }
       // ---- weights against the reference that the accumulators refer to, without looking for the page's maximum first: any
       // reference gives the same quotient.  Only where a weight leaves the guarded range, or a query has no reference yet, the
       // maximum is taken (over the 4 lane groups of a query), the references move there and the weights are taken again.
-      float e[16], psum;
-      auto weights = [&]() __attribute__((always_inline)) {
-        const float shift = log_rest - m_run;
-        psum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          e[j] = fast_exp2(__builtin_fmaf(s[j >> 2][j & 3], c, shift));
-          psum += e[j];
-        }
-      };
-      weights();
-      if (__builtin_amdgcn_ballot_w64(!(psum < kPagedGuard)) != 0) {
-        float m = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
-#pragma unroll
-        for (int sb = 1; sb < 4; ++sb) m = fmaxf(m, fmaxf(fmaxf(s[sb][0], s[sb][1]), fmaxf(s[sb][2], s[sb][3])));
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m_run, fmaxf(m, __shfl_xor(m, 32)) * c);
-        const float alpha = fast_exp2(m_run - m);
-        m_run = m;
-        l_run *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] *= alpha;
-        weights();
-      }
-      l_run = __builtin_fmaf(psum, inv_rest, l_run);
-      // O^T += V^T P^T, 32 keys at a time: lane (n, g) has the keys 32 kh + 4 g + (0..3) and 16 more of P, and takes the same of V.
       // TERMS bf16 values make a weight: two leave 2^-16 of it (see decode.hip), three 2^-24, which is what an fp32 output holds
       // (8/2 heads of 64, 2001 keys: 2-norm of the error 3.7e-6 of the result's with two).
-      constexpr int TERMS = FP32 ? 3 : 2;
-      uint32_t pk[TERMS][8];
+      // Runs take a term less: a weight of one is rounded to bf16, and the denominator sums the rounded ones.
+      constexpr int TERMS = (FP32 ? 3 : 2) - (RUN ? 1 : 0);
+      uint32_t pk[NB][TERMS][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float x = e[2 * j], y = e[2 * j + 1];
+      for (int b = 0; b < NB; ++b) {
+        float e[16], psum;
+        auto weights = [&]() __attribute__((always_inline)) {
+          const float shift = log_rest - m_run[b];
+          psum = 0.f;
 #pragma unroll
-        for (int t = 0; t < TERMS - 1; ++t) {              // the upper bits of what is left
-          pk[t][j] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
-          x -= bf16_lo(pk[t][j]);
-          y -= bf16_hi(pk[t][j]);
+          for (int j = 0; j < 16; ++j) {
+            e[j] = fast_exp2(__builtin_fmaf(s[j >> 2][b][j & 3], c, shift));
+            psum += e[j];
+          }
+        };
+        weights();
+        if (__builtin_amdgcn_ballot_w64(!(psum < kPagedGuard)) != 0) {
+          float m = s[0][b][0];
+#pragma unroll
+          for (int j = 1; j < 16; ++j) m = fmaxf(m, s[j >> 2][b][j & 3]);
+          m = fmaxf(m, __shfl_xor(m, 16));
+          m = fmaxf(m_run[b], fmaxf(m, __shfl_xor(m, 32)) * c);
+          const float alpha = fast_exp2(m_run[b] - m);
+          m_run[b] = m;
+          l_run[b] *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) o[db][b] *= alpha;
+          weights();
         }
-        pk[TERMS - 1][j] = pack_bf16(x, y);
+        if constexpr (TERMS == 1) psum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float x = e[2 * j], y = e[2 * j + 1];
+#pragma unroll
+          for (int t = 0; t < TERMS - 1; ++t) {              // the upper bits of what is left
+            pk[b][t][j] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
+            x -= bf16_lo(pk[b][t][j]);
+            y -= bf16_hi(pk[b][t][j]);
+          }
+          pk[b][TERMS - 1][j] = pack_bf16(x, y);
+          if constexpr (TERMS == 1) psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[b][0][j]), bf16x2{(__bf16)1.0f, (__bf16)1.0f}, psum, false);
+        }
+        l_run[b] = __builtin_fmaf(psum, inv_rest, l_run[b]);
       }
+      // ---- O^T += V^T P^T, 32 keys at a time: lane (n, g) has the keys 32 kh + 4 g + (0..3) and 16 more of P, and takes the same of V
 #pragma unroll
       for (int kh = 0; kh < 2; ++kh) {
         const int j = n >> 1;
@@ -356,16 +439,19 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
           const i32x2 t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((FLUX_LDS i32x2*)(src + 16 * db));
           const bf16x8 vf = unpack8((uint32_t)t[0], (uint32_t)t[1], v_power);
 #pragma unroll
-          for (int i = 0; i < TERMS; ++i)
-            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, u32x4{pk[i][4 * kh], pk[i][4 * kh + 1], pk[i][4 * kh + 2], pk[i][4 * kh + 3]}), o[db], 0, 0, 0);
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i)
+              o[db][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, u32x4{pk[b][i][4 * kh], pk[b][i][4 * kh + 1], pk[b][i][4 * kh + 2], pk[b][i][4 * kh + 3]}), o[db][b], 0, 0, 0);
         }
       }
     }
 
     __builtin_amdgcn_s_waitcnt(0x0F70);                     // vmcnt(0): nothing is in flight any more
     // ---- what the end of this part needs, and on to the next one: its first page is in flight meanwhile
-    const int nq = min(16, a.group - (a.qblocks == 1 ? 0 : 16 * (pair % a.qblocks)));
-    const int64_t out0 = ((int64_t)place.b * a.hq + (int64_t)(a.qblocks == 1 ? pair : pair / a.qblocks) * a.group + (a.qblocks == 1 ? 0 : 16 * (pair % a.qblocks))) * D;
+    const int nq = RUN ? run_rows : min(16, a.group - (a.qblocks == 1 ? 0 : 16 * (pair % a.qblocks)));
+    const int64_t out0 = ((int64_t)(RUN ? __builtin_amdgcn_readlane(q_begin_mine, place.b) : place.b) * a.hq +
+                          (int64_t)(a.qblocks == 1 ? pair : pair / a.qblocks) * a.group + (a.qblocks == 1 ? 0 : 16 * (pair % a.qblocks))) * D;
     const int list0 = place.begin + pair * place.nb;
     const bool empty = x0 >= x1;                            // (the range begins in what is only counted behind a list)
     const bool whole = empty || (x0 == 0 && x1 == place.real);   // the pair lies in this range
@@ -375,54 +461,66 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
     const bool more = W == 4 && at < range_end;
     if (more) {
       if (++pair == a.sp.pps) {
-        place = find_place(a.sp, cut, lanes, l, seqs, place.begin + a.sp.pps * place.nb);   // (the next one that has keys)
+        place = find_place(split, cut, lanes, l, seqs, place.begin + a.sp.pps * place.nb);   // (the next one that has keys)
         pair = 0;
       }
       set_part();
       begin_part();
     }
 
-    // ---- merge the waves through LDS: red[w][n][0..D-1] = O, ml[w][n] = (m, l); only the columns of heads that exist
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
-    __syncthreads();                                        // every wave is done with its V staging
+    // ---- merge the waves through LDS, a block of columns at a time: red[w][n][0..D-1] = O, ml[w][n] = (m, l); only the columns of
+    // rows that exist
     FLUX_LDS float* red = (FLUX_LDS float*)smem;
     FLUX_LDS f32x2* ml = (FLUX_LDS f32x2*)(red + W * 16 * RED);
-    if (n < nq) {
-      FLUX_LDS float* mine = red + (w * 16 + n) * RED + 4 * g;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) *(FLUX_LDS f32x4*)(mine + 16 * db) = o[db];
-      if (g == 0) ml[w * 16 + n] = f32x2{m_run, l_run};
-    }
-    __syncthreads();
     auto store_out = [&](int qi, int d, f32x4 r) __attribute__((always_inline)) {
-      const int64_t off = out0 + qi * D + d;
+      int64_t off = out0 + d;
+      if constexpr (RUN) {
+        const int tok = quotient(qi, a.by_group);
+        off += (int64_t)(tok * a.hq + qi - tok * a.group) * D;
+      } else {
+        off += qi * D;
+      }
       if constexpr (FP32) *(f32x4*)((float*)a.out + off) = r;
       else *(u32x2*)((__bf16*)a.out + off) = u32x2{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
     };
-    const int row0 = part_place(first, wg - first) * a.rpu;
-    for (int idx = tid; !empty && idx < nq * (D / 4); idx += 64 * W) {
-      const int qi = idx / (D / 4), d = 4 * (idx % (D / 4));
-      f32x2 x[W];
-      float m = -1e30f;
 #pragma unroll
-      for (int ww = 0; ww < W; ++ww) {
-        x[ww] = ml[ww * 16 + qi];
-        m = fmaxf(m, x[ww][0]);
-      }
-      f32x4 val = {0.f, 0.f, 0.f, 0.f};
-      float den = 0x1p-126f;                                // (no page there: 0 / this)
+    for (int b = 0; b < NB; ++b) {
+      const int in_block = min(16, nq - 16 * b), row0 = part_place(first, wg - first) * a.rpu + 16 * b;
+      if (RUN && in_block <= 0) break;                      // (uniform)
+      float l_tot = l_run[b];
+      l_tot += __shfl_xor(l_tot, 16);
+      l_tot += __shfl_xor(l_tot, 32);
+      __syncthreads();                                      // every wave is done with its V staging, or with the block before
+      if (n < in_block) {
+        FLUX_LDS float* mine = red + (w * 16 + n) * RED + 4 * g;
 #pragma unroll
-      for (int ww = 0; ww < W; ++ww) {
-        const float wgt = fast_exp2(x[ww][0] - m);          // 0 for idle waves beside others
-        val += wgt * *(FLUX_LDS f32x4*)(red + (ww * 16 + qi) * RED + d);
-        den += wgt * x[ww][1];
+        for (int db = 0; db < DB; ++db) *(FLUX_LDS f32x4*)(mine + 16 * db) = o[db][b];
+        if (g == 0) ml[w * 16 + n] = f32x2{m_run[b], l_tot};
       }
-      if (whole) {                                          // nothing to merge with
-        store_out(qi, d, f32x4{val[0] / den, val[1] / den, val[2] / den, val[3] / den});
-      } else {
-        store16_dev(a.part_o, ((row0 + qi) * D + d) * 4, val);
-        if (d == 0) __hip_atomic_store((unsigned long long*)(a.part_ml + 2 * (row0 + qi)), __builtin_bit_cast(unsigned long long, f32x2{m, den}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __syncthreads();
+      for (int idx = tid; !empty && idx < in_block * (D / 4); idx += 64 * W) {
+        const int qi = idx / (D / 4), d = 4 * (idx % (D / 4));
+        f32x2 x[W];
+        float m = -1e30f;
+#pragma unroll
+        for (int ww = 0; ww < W; ++ww) {
+          x[ww] = ml[ww * 16 + qi];
+          m = fmaxf(m, x[ww][0]);
+        }
+        f32x4 val = {0.f, 0.f, 0.f, 0.f};
+        float den = 0x1p-126f;                              // (no page there: 0 / this)
+#pragma unroll
+        for (int ww = 0; ww < W; ++ww) {
+          const float wgt = fast_exp2(x[ww][0] - m);        // 0 for idle waves beside others
+          val += wgt * *(FLUX_LDS f32x4*)(red + (ww * 16 + qi) * RED + d);
+          den += wgt * x[ww][1];
+        }
+        if (whole) {                                        // nothing to merge with
+          store_out(16 * b + qi, d, f32x4{val[0] / den, val[1] / den, val[2] / den, val[3] / den});
+        } else {
+          store16_dev(a.part_o, ((row0 + qi) * D + d) * 4, val);
+          if (d == 0) __hip_atomic_store((unsigned long long*)(a.part_ml + 2 * (row0 + qi)), __builtin_bit_cast(unsigned long long, f32x2{m, den}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
       }
     }
     if (!whole) {
@@ -444,9 +542,22 @@ __global__ __launch_bounds__(64 * W, 2) void paged_decode_kernel(PagedDecodeArgs
   zero_rows();
 }
 
-hipError_t launch_decode_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, int max_kv_len, const flux_paged_kv& kv,
-                               const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s) {
-  const DecodePlan plan = plan_decode_paged(cfg, pt.batch, max_kv_len);
+namespace {
+template <bool NT, int W, int QB>
+void launch_kernel(const PagedDecodeArgs& a, const flux_attn_cfg& cfg, int wgs, hipStream_t s) {
+  const dim3 grid(wgs), block(64 * W);
+  if (cfg.head_dim == 128) {
+    if (cfg.out_dtype != 0) hipLaunchKernelGGL((paged_decode_kernel<128, NT, W, true, QB>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_decode_kernel<128, NT, W, false, QB>), grid, block, 0, s, a);
+  } else {
+    if (cfg.out_dtype != 0) hipLaunchKernelGGL((paged_decode_kernel<64, NT, W, true, QB>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((paged_decode_kernel<64, NT, W, false, QB>), grid, block, 0, s, a);
+  }
+}
+
+// What a call of one query per sequence and one of runs have in common.  `rows` leave a part, which go to `part_rows`.
+PagedDecodeArgs decode_args(const Ctx& c, const flux_attn_cfg& cfg, const void* q, int max_kv_len, const flux_paged_kv& kv,
+                            const flux_page_table& pt, const uint8_t* mode, void* out, const DecodePlan& plan, float* part_rows) {
   PagedDecodeArgs a;
   a.q = (const __bf16*)q;
   a.k = (const char*)kv.k;
@@ -474,30 +585,50 @@ hipError_t launch_decode_paged(const Ctx& c, const flux_attn_cfg& cfg, const voi
   a.hq = cfg.n_q_heads;
   a.hkv = cfg.n_kv_heads;
   a.group = cfg.n_q_heads / cfg.n_kv_heads;
-  a.qblocks = (a.group + 15) / 16;
+  a.by_group = reciprocal((uint32_t)a.group);
+  a.qblocks = plan.pps / cfg.n_kv_heads;
   a.rpu = plan.rpu;
+  a.cu_q = nullptr;
+  a.max_q = 1;
   a.scale_log2 = (cfg.softmax_scale != 0.f ? cfg.softmax_scale : 1.0f / sqrtf((float)cfg.head_dim)) * kLog2e;
-  a.part_o = plan.in_partials ? c.partials + decode_rows_at(plan, false) : c.small;
+  a.part_o = part_rows;
   a.part_ml = a.part_o + (size_t)2 * plan.wgs * plan.rpu * cfg.head_dim;
   a.status = c.status;
   a.arrived = c.decode_counters;
   a.out = out;
-  const dim3 grid(plan.wgs);
-  // rows that are evicted before the next step are fetched with nontemporal loads (see launch_decode)
-  const bool nt = 2.0 * pt.batch * cfg.n_kv_heads * cfg.head_dim * (double)max_kv_len > 64.0 * 1024 * 1024;
-  auto launch = [&](auto d, auto fp32) {
-    constexpr int D = decltype(d)::value;
-    constexpr bool FP32 = decltype(fp32)::value;
-    if (plan.waves == 8) hipLaunchKernelGGL((paged_decode_kernel<D, false, 8, FP32>), grid, dim3(512), 0, s, a);
-    else if (nt) hipLaunchKernelGGL((paged_decode_kernel<D, true, 4, FP32>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_decode_kernel<D, false, 4, FP32>), grid, dim3(256), 0, s, a);
-  };
-  auto launch_d = [&](auto d) {
-    if (cfg.out_dtype != 0) launch(d, std::true_type());
-    else launch(d, std::false_type());
-  };
-  if (cfg.head_dim == 128) launch_d(std::integral_constant<int, 128>());
-  else launch_d(std::integral_constant<int, 64>());
+  return a;
+}
+
+// rows that are evicted before the next step are fetched with nontemporal loads (see launch_decode)
+bool nontemporal(const flux_attn_cfg& cfg, const flux_page_table& pt, int max_kv_len) {
+  return 2.0 * pt.batch * cfg.n_kv_heads * cfg.head_dim * (double)max_kv_len > 64.0 * 1024 * 1024;
+}
+}  // namespace
+
+hipError_t launch_decode_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, int max_kv_len, const flux_paged_kv& kv,
+                               const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s) {
+  const DecodePlan plan = plan_decode_paged(cfg, pt.batch, max_kv_len);
+  const PagedDecodeArgs a = decode_args(c, cfg, q, max_kv_len, kv, pt, mode, out, plan, plan.in_partials ? c.partials + decode_rows_at(plan, false) : c.small);
+  if (plan.waves == 8) launch_kernel<false, 8, 0>(a, cfg, plan.wgs, s);
+  else if (nontemporal(cfg, pt, max_kv_len)) launch_kernel<true, 4, 0>(a, cfg, plan.wgs, s);
+  else launch_kernel<false, 4, 0>(a, cfg, plan.wgs, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_runs_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
+                             const flux_paged_kv& kv, const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s) {
+  const DecodePlan plan = plan_runs_paged(cfg, pt.batch, max_q_len, max_kv_len);
+  PagedDecodeArgs a = decode_args(c, cfg, q, max_kv_len, kv, pt, mode, out, plan, c.partials);
+  a.cu_q = cu_q;
+  a.max_q = max_q_len;
+  const bool nt = nontemporal(cfg, pt, max_kv_len);
+  if (plan.rpu <= 16) {
+    if (nt) launch_kernel<true, 4, 1>(a, cfg, plan.wgs, s);
+    else launch_kernel<false, 4, 1>(a, cfg, plan.wgs, s);
+  } else {
+    if (nt) launch_kernel<true, 4, 2>(a, cfg, plan.wgs, s);
+    else launch_kernel<false, 4, 2>(a, cfg, plan.wgs, s);
+  }
   return hipGetLastError();
 }
 

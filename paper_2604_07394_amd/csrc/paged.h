@@ -43,6 +43,9 @@ inline Reciprocal reciprocal(uint32_t d) {
   while (shift < 31 && (1ull << shift) < d) ++shift;
   return {(uint32_t)(((((uint64_t)1 << shift) - d) << 32) / d + 1), shift};
 }
+#ifdef __HIP__
+__device__ __forceinline__ int quotient(int n, Reciprocal d) { return (int)(((uint32_t)(((uint64_t)(uint32_t)n * d.mul) >> 32) + (uint32_t)n) >> d.shift); }
+#endif
 struct PagedPrefillPlan {
   int bm;               // rows of a tile
   int tiles;            // of a sequence and KV head, at most
@@ -68,6 +71,30 @@ inline PagedPrefillPlan plan_prefill_paged(const flux_attn_cfg& cfg, int batch, 
   }
   return p;
 }
+// Short runs of queries behind a cached context (drafted tokens), whose rows take at most two blocks of 16 columns, are worked on like
+// decode calls, by the kernel of those: a wave has a page to itself instead of a quarter of the rows.
+constexpr int kRunRows = 32;
+constexpr int runs_per_cu(int head_dim, int blocks) { return head_dim == 128 && blocks == 2 ? 1 : 2; }   // workgroups
+inline DecodePlan plan_runs_paged(const flux_attn_cfg& cfg, int batch, int max_q_len, int max_kv_len) {
+  flux_attn_cfg one = cfg;
+  one.n_q_heads = cfg.n_kv_heads;                            // one pair per KV head
+  DecodePlan p = plan_decode_paged(one, batch, max_kv_len);
+  const long long by_four = (long long)batch * p.pps * ((pages_of(max_kv_len) + 3) / 4);
+  p.rpu = max_q_len * (cfg.n_q_heads / cfg.n_kv_heads);
+  p.waves = 4;
+  p.aligned_shift = runs_per_cu(cfg.head_dim, (p.rpu + 15) / 16) == 1 ? kDecodeWgsShift : kDecodeAlignedShift;
+  p.wgs = (int)(by_four < (1 << p.aligned_shift) ? by_four : (1 << p.aligned_shift));
+  return p;
+}
+inline bool runs_paged(const Ctx& c, const flux_attn_cfg& cfg, int batch, int max_q_len, int max_kv_len) {
+  const int group = cfg.n_q_heads / cfg.n_kv_heads;
+  if (batch > 64 || max_q_len > kRunRows / group || pages_of(max_kv_len) < kPagedMinPages) return false;
+  if ((long long)batch * cfg.n_kv_heads > 0x7FFFFFFFll / (pages_of(max_kv_len) + 16)) return false;   // pages are counted in 32 bits
+  const DecodePlan p = plan_runs_paged(cfg, batch, max_q_len, max_kv_len);
+  return c.decode_counters && (size_t)2 * p.wgs * p.rpu * (cfg.head_dim + 2) * sizeof(float) <= c.partials_bytes;
+}
+hipError_t launch_runs_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
+                             const flux_paged_kv& kv, const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s);
 hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
                                 const flux_paged_kv& kv, const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s);
 

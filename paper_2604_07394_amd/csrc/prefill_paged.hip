@@ -34,6 +34,7 @@ struct PagedPrefillArgs {
   int table_pages, n_pages;
   const int32_t* kv_len;
   const uint8_t* mode;
+  int max_kv_len;
   int hq, hkv, group, batch;
   Reciprocal by_group;
   int sink_lim, win_blocks, blk_shift;   // SA geometry (see sa_geom)
@@ -51,8 +52,6 @@ struct PagedPrefillArgs {
 
 constexpr int kPagedNoSplit = 0x3FFFFFFF;
 
-__device__ __forceinline__ int quotient(int n, Reciprocal d) { return (int)(((uint32_t)(((uint64_t)(uint32_t)n * d.mul) >> 32) + (uint32_t)n) >> d.shift); }
-
 struct PagedSeq {
   int q_begin, n_q, len, tiles, pages;   // pages: of its longest tile (an upper bound for SA)
   bool sa, bad;
@@ -65,7 +64,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedPrefillArgs& a, int b, 
   s.len = a.kv_len[b];
   s.sa = a.mode[b] == 0;
   const int cap = a.table_pages * kPageTokens;
-  s.bad = s.n_q < 0 || s.len < 0 || s.len > cap || s.n_q > s.len || s.q_begin < 0;
+  s.bad = s.n_q < 0 || s.len < 0 || s.len > cap || s.n_q > s.len || s.q_begin < 0 || s.len > a.max_kv_len;
   s.len = s.len < 0 ? 0 : min(s.len, cap);
   s.n_q = s.n_q < 0 || s.q_begin < 0 ? 0 : min(s.n_q, s.len);
   s.tiles = (int)min(((int64_t)s.n_q * a.group + bm - 1) / bm, (int64_t)a.n_qtiles);
@@ -670,8 +669,9 @@ __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
 
 hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
                                 const flux_paged_kv& kv, const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s) {
+  if (max_q_len == 0) return hipSuccess;
+  if (runs_paged(c, cfg, pt.batch, max_q_len, max_kv_len)) return launch_runs_paged(c, cfg, q, cu_q, max_q_len, max_kv_len, kv, pt, mode, out, s);
   const PagedPrefillPlan plan = plan_prefill_paged(cfg, pt.batch, max_q_len, max_kv_len, c.partials_bytes);
-  if (plan.tiles == 0) return hipSuccess;
   PagedPrefillArgs a;
   a.q = (const __bf16*)q;
   a.cu_q = cu_q;
@@ -687,6 +687,7 @@ hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const vo
   a.n_pages = kv.n_pages;
   a.kv_len = pt.kv_len;
   a.mode = mode;
+  a.max_kv_len = max_kv_len;
   a.hq = cfg.n_q_heads;
   a.hkv = cfg.n_kv_heads;
   a.group = cfg.n_q_heads / cfg.n_kv_heads;

@@ -45,6 +45,11 @@ CASES = [
     ([40, 500], [1000, 0], [SA, SA], 4, 4, 64, 130, 70, 16),                  # group 1; sinks of two pages and two positions
     ([5] * 6, [300, 2000, 64, 63, 4000, 1], [FA, SA, FA, FA, FA, SA], 32, 8, 128, 128, 512, 0),   # drafts: pages are shared out
     ([3], [6000], [FA], 16, 1, 128, 0, 1, 0),                                 # one KV head, group 16
+    ([2], [6000], [SA], 16, 1, 128, 70, 300, 0),                              # ... two blocks of columns
+    ([4, 0, 1, 3], [700, 500, 20000, 64], [FA, FA, SA, SA], 8, 2, 64, 5, 100, 0),     # runs of uneven length, one block
+    ([1, 8, 2, 7, 8], [64, 511, 448, 3000, 62], [SA, SA, FA, SA, FA], 8, 2, 128, 3, 64, 64),   # runs across page borders
+    ([8, 8], [100000, 3], [FA, FA], 4, 1, 64, 0, 1, 0),
+    ([1 + i % 5 for i in range(64)], [(i * 97) % 900 + 1 for i in range(64)], [i % 2 for i in range(64)], 12, 2, 128, 3, 70, 0),
     ([17, 1], [5000, 9000], [FA, SA], 40, 2, 64, 64, 3000, 0),                # group 20
     ([600], [1500], [FA], 8, 2, 128, 0, 1, 0),
     ([900], [0], [SA], 8, 1, 64, 2 ** 31 - 1, 2 ** 31 - 1, 64),               # the sparse rule sees everything
@@ -140,6 +145,22 @@ def test_prefill_where_pages_are_missing_and_lengths_do_not_fit(F, ctx):
     kv.v_scale.fill_(1)
     F.flux_attn_prefill_paged(ctx, cfg, q, i32([0, -3, 9]), 40, 40, kv, pt, torch.ones(2, dtype=torch.uint8, device="cuda"), out)
     assert F.flux_last_device_status(ctx) & F.FLUX_DEV_BAD_LENGTH
+
+
+@pytest.mark.parametrize("n", [2, 60])
+def test_prefill_says_when_a_bound_is_too_low(F, ctx, n):
+    hq, hkv, d = 8, 2, 64
+    kv, pt, q, qf, seqs = attention_case(F, [1000, 640], hq, hkv, d, seed=9, rows=[n, n])
+    out = torch.full((2 * n, hq, d), 7.0, dtype=torch.float32, device="cuda")
+    F.flux_attn_prefill_paged(ctx, F.attn_cfg(hq, hkv, d, 0, 1, 0.0, 1), q, cu_of([n, n]), n, 640, kv, pt, torch.ones(2, dtype=torch.uint8, device="cuda"), out)
+    assert F.flux_last_device_status(ctx) == F.FLUX_DEV_BAD_LENGTH
+    check(out[n:], prefill_ref(qf[n:], seqs[1:], [n], [FA], 0, 1), tolerance(qf, seqs, d), seqs)
+    assert torch.isfinite(out).all()
+    out.fill_(7.0)                                           # rows beyond max_q_len are not computed, whatever tile they share
+    F.flux_attn_prefill_paged(ctx, F.attn_cfg(hq, hkv, d, 0, 1, 0.0, 1), q, cu_of([n, n]), 1, 1000, kv, pt, torch.ones(2, dtype=torch.uint8, device="cuda"), out)
+    assert F.flux_last_device_status(ctx) == 0
+    ref = prefill_ref(qf, seqs, [n, n], [FA, FA], 0, 1)
+    check(out[[0, n]], ref[[0, n]], tolerance(qf, seqs, d), seqs)
 
 
 def test_prefill_rows_are_those_of_decode(F, ctx):
