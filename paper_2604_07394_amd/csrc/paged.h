@@ -56,7 +56,13 @@ struct PagedPrefillPlan {
 inline PagedPrefillPlan plan_prefill_paged(const flux_attn_cfg& cfg, int batch, int max_q_len, int max_kv_len, size_t partials_bytes) {
   PagedPrefillPlan p;
   const long long rows = (long long)max_q_len * (cfg.n_q_heads / cfg.n_kv_heads);
-  p.bm = rows <= 64 ? 64 : 128;
+  // Tiles of 64 rows where they run side by side and walk little more than their own queries: a page takes a wave half the MFMAs, and
+  // nothing waits for a second round.  Behind a long context a tile of 128 rows converts and stages half as much.  us with 64 / 128
+  // rows, 32/8 heads of 128 (512 workgroups of 64 rows side by side) unless said: 40 tokens 6.1 / 7.7, 100 6.9 / 8.9, 1000 23.8 / 32.8, 4 x
+  // 100 7.5 / 9.5, 16 x 60 to 140 (1024 tiles of 64) 16.8 / 14.1, 512 at 8/2 heads of 64 (1024 side by side) 10.0 / 12.7, 4 x 300 to 700
+  // of 64 15.6 / 17.1; 64 tokens behind 8000 28.3 / 28.4, 128 behind 16000 54.5 / 46.9, 512 behind 32000 326 / 235.
+  const long long tiles64 = (long long)batch * cfg.n_kv_heads * ((rows + 63) / 64);
+  p.bm = rows <= 64 || (tiles64 <= (cfg.head_dim == 128 ? 512 : 1024) && max_kv_len <= 2ll * max_q_len) ? 64 : 128;
   p.tiles = (int)((rows + p.bm - 1) / p.bm);
   p.wgs = (long long)batch * unit_count(cfg.n_kv_heads, p.tiles);
   p.part_units = 0;
