@@ -47,6 +47,7 @@ struct SplitArgs {
   int block_shift;        // lists are cut into blocks of 2^block_shift keys
   int most_by_four;       // calls of eight waves: workgroups up to which they take four blocks of a list where lists are merged
   int aligned_shift;      // few blocks: one workgroup per 4, 8 or 16 of a list while that takes at most 2^aligned_shift (see Cut); < 0: not
+  static constexpr int seam_blocks(int head_dim) { return 512 / head_dim; }   // see find_cut
 };
 
 struct DecodeArgs {

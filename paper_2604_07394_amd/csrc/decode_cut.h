@@ -1,7 +1,7 @@
 // How a decode call is shared out over the chip, and how the parts of a list are merged: what the decode kernels of the
 // contiguous and of the paged cache have in common.  A call is described by a struct `s` with the members batch, pps,
 // most_by_four and aligned_shift (see SplitArgs in decode.hip), for which load_counted(s, b, bad) says how many blocks
-// sequence b has: 32 keys of a bf16 cache or a page of 64 keys of an 8-bit one, the same bytes either way.
+// sequence b has, and S::seam_blocks(head_dim) what going on to the next list counts: 32 keys of a bf16 cache or a page of 64 keys of an 8-bit one, the same bytes either way.
 #pragma once
 
 #include <utility>
@@ -80,7 +80,8 @@ __device__ __forceinline__ Cut find_cut(const S& s, int lane, int w, SeqTable* t
   // dimension 128 is a multiple of two and two blocks more then.  us with four and four / so: 104 lists of 1 to 4 keys among 24 of 2000
   // 53.0 / 48.7, 128 of 50 to 299 31.2 / 30.4, 1000 of 20 to 199 at 28/4 heads 73.4 / 72.1, 53 of 36 to 1044 at 16/8 36.3 / 35.5.
   // At head dimension 64 there is nothing in it: 136 of 6 to 200 18.9 / 20.4, 122 of 39 to 1278 45.9 / 44.9.
-  constexpr int kSeam = 512 / D;
+  // (Over pages the next list's page numbers are a memory latency more: S says how many blocks a seam counts.)
+  constexpr int kSeam = S::seam_blocks(D);
   // Two workgroups per CU where there are as many lists as CUs, since at most seams the other one goes on (us with one / two,
   // 32/8 heads of 128: 128 lists of 300 keys 39.9 / 34.5, 128 of 100 to 3000 61.8 / 52.6, 1000 of 20 to 200 at 28/4 heads 107 /
   // 82; but 16 lists of 2112, 128 in all, 29.4 / 31.0, 8 x 131072 629 / 665).  At head dimension 64 from a quarter of that on:

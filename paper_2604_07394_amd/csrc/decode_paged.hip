@@ -30,6 +30,9 @@ struct PagedSplit {
   int sink_lim, win_blocks, blk_shift;   // SA geometry (see sa_geom)
   int max_pages;          // the host's bound on the pages of a list
   int pps, most_by_four, aligned_shift;  // see SplitArgs
+  // us with 4 / 6 / 8 blocks of head dimension 128: 128 lists of 2 to 32 pages 64.4 / 60.2 / 60.5, 16 of 8 to 125 32.1 / 31.7 / 31.6, 32 ragged
+  // ones of 28/4 heads 25.7 / 25.1 / 25.2
+  static constexpr int seam_blocks(int head_dim) { return 768 / head_dim; }
 };
 
 // The pages of a list: all up to the query's, or, where `skip` > 0, the first `seam` (the sinks) and those from seam + skip on.

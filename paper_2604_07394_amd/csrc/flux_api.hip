@@ -466,8 +466,9 @@ int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* 
   if (!ctx || !q || !mode || !out) return FLUX_EINVAL;
   const int rc = check_paged_attention(cfg, q, max_kv_len, kv, pt, out);
   if (rc != FLUX_OK) return rc;
+  const int group = cfg->n_q_heads / cfg->n_kv_heads;
+  if ((long long)pt->batch * cfg->n_kv_heads * ((group + 15) / 16) > 0x7FFFFFFFll / (pages_of(max_kv_len) + 16)) return FLUX_EINVAL;   // pages are counted in 32 bits
   const DecodePlan p = plan_decode_paged(*cfg, pt->batch, max_kv_len);
-  if ((long long)pt->batch * p.pps > 0x7FFFFFFFll / (pages_of(max_kv_len) + 16)) return FLUX_EINVAL;   // pages are counted in 32 bits
   if (ctx->c.device >= 0 && decode_partials_bytes(*cfg, p) > ctx->c.partials_bytes) return FLUX_EWORKSPACE;
   if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
   const hipError_t e = launch_decode_paged(ctx->c, *cfg, q, max_kv_len, *kv, *pt, mode, out, (hipStream_t)stream);

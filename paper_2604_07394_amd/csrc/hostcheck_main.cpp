@@ -16,6 +16,7 @@ extern "C" int hostcheck_decode_wgs(const flux_attn_cfg* cfg, int batch, int max
 extern "C" int hostcheck_decode_in_partials(const flux_attn_cfg* cfg, int batch, int max_kv_len);
 extern "C" int hostcheck_decode_blocks_fit(const flux_attn_cfg* cfg, int batch, int max_kv_len);
 extern "C" int hostcheck_decode_rows_fit(const flux_attn_cfg* cfg, int batch, int max_kv_len);
+extern "C" int hostcheck_paged_rows_fit(const flux_attn_cfg* cfg, int batch, int max_q_len, int max_kv_len, int* wgs, int* waves);
 extern "C" int hostcheck_append(int batch, int hkv, int d, int total_new, int max_new, int ring, int window, unsigned* wgs);
 
 static int failures = 0;
@@ -186,6 +187,47 @@ int main() {
   // ---- status and teardown
   EXPECT(flux_last_device_status(ctx, nullptr), FLUX_EHIP);
   EXPECT(flux_last_device_status(nullptr, nullptr), FLUX_EINVAL);
+  // ---- paged caches: every entry point, and the arithmetic of launches and workspaces at ordinary and extreme sizes
+  {
+    flux_page_table pt = {pi, pi, pi, pi, 2, 4, 8};
+    flux_paged_kv kv = {p, p, (float*)buf, (float*)buf, 2 * 64 * 128, 64 * 128, 128, 8};
+    EXPECT(flux_page_plan(ctx, &pt, pi, 5, pi, nullptr), FLUX_EHIP);
+    EXPECT(flux_page_plan(ctx, &pt, pi, INT_MAX, pi, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_plan(ctx, nullptr, pi, 5, pi, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_release(ctx, &pt, pi, nullptr), FLUX_EHIP);
+    EXPECT(flux_page_release(ctx, &pt, nullptr, nullptr), FLUX_EINVAL);
+    EXPECT(flux_kv_append_paged(ctx, &kv, 2, 128, p, p, pi, 7, nullptr), FLUX_EHIP);
+    EXPECT(flux_kv_append_paged(ctx, &kv, 2, 128, p, buf + 8, pi, 7, nullptr), FLUX_EINVAL);
+    EXPECT(flux_kv_append_paged(ctx, nullptr, 2, 128, p, p, pi, 7, nullptr), FLUX_EINVAL);
+    for (int w : big)
+      for (int b : blocks) {
+        flux_attn_cfg c2 = {8, 2, 128, w, w, 0.f, 1, b};
+        EXPECT(flux_attn_decode_paged(ctx, &c2, p, 200, &kv, &pt, pb, p, nullptr), FLUX_EHIP);
+        EXPECT(flux_attn_prefill_paged(ctx, &c2, p, pi, 8, 200, &kv, &pt, pb, p, nullptr), FLUX_EHIP);
+      }
+    pt.table_pages = 1 << 24;
+    EXPECT(flux_attn_decode_paged(ctx, &cfg, p, 1 << 30, &kv, &pt, pb, p, nullptr), FLUX_EHIP);
+    EXPECT(flux_attn_decode_paged(ctx, &cfg, p, INT_MAX, &kv, &pt, pb, p, nullptr), FLUX_ECAPACITY);
+    EXPECT(flux_attn_prefill_paged(ctx, &cfg, p, pi, 1 << 28, 1 << 30, &kv, &pt, pb, p, nullptr), FLUX_EINVAL);   // (workgroups)
+    pt.batch = INT_MAX;
+    EXPECT(flux_attn_decode_paged(ctx, &cfg, p, 1 << 30, &kv, &pt, pb, p, nullptr), FLUX_EINVAL);
+    EXPECT(flux_attn_prefill_paged(ctx, &cfg, p, pi, 8, 1 << 30, &kv, &pt, pb, p, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_plan(ctx, &pt, pi, 5, pi, nullptr), FLUX_EINVAL);
+    int wgs, waves;
+    const int heads[][2] = {{32, 8}, {28, 4}, {8, 2}, {1, 1}, {16, 1}, {40, 2}, {64, 64}, {96, 1}, {256, 2}};
+    const int batches[] = {1, 2, 3, 13, 31, 32, 33, 64, 65, 500, 3000, 70000};
+    const int keys[] = {0, 1, 63, 64, 65, 200, 511, 513, 2001, 8000, 20000, 131072, 1 << 20, 1 << 30};
+    for (int d : {64, 128})
+      for (const auto& h : heads)
+        for (int batch : batches)
+          for (int k : keys)
+            for (int q : {1, 2, 5, 8, 31, 300, 40000}) {
+              if (q > k || (long long)batch * h[1] * (k / 64 + 16) > INT_MAX / ((h[0] / h[1] + 15) / 16)) continue;
+              flux_attn_cfg c = {h[0], h[1], d, 4, 16, 0.f, 0, 0};
+              EXPECT(hostcheck_paged_rows_fit(&c, batch, q, k, &wgs, &waves), 1);
+              EXPECT(wgs >= 1 && wgs <= (waves == 8 ? 256 : 512), 1);
+            }
+  }
   EXPECT(flux_destroy(ctx), FLUX_OK);
   EXPECT(flux_destroy(nullptr), FLUX_EINVAL);
   if (failures == 0) printf("hostcheck ok\n");

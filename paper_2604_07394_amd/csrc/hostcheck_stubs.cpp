@@ -26,6 +26,31 @@ int hostcheck_append(int batch, int hkv, int d, int total_new, int max_new, int 
   *wgs = p.wgs;
   return p.form;
 }
+// a decode call over pages: whether the rows of its parts end within what holds them (nothing but the call's own checks bounds the
+// workspace), and the same of a run of queries in the partials that it asks for; workgroups, waves
+int hostcheck_paged_rows_fit(const flux_attn_cfg* cfg, int batch, int max_q_len, int max_kv_len, int* wgs, int* waves) {
+  const flux::DecodePlan p = flux::plan_decode_paged(*cfg, batch, max_kv_len);
+  *wgs = p.wgs;
+  *waves = p.waves;
+  const size_t rows = (size_t)2 * p.wgs * p.rpu * (cfg->head_dim + 2) * sizeof(float);
+  const size_t needed = flux_workspace_needed(cfg, batch, max_kv_len) - flux::kHeaderBytes - flux::kSmallBytes;
+  bool fits = p.in_partials ? rows <= needed : rows <= flux::kSmallBytes;
+  fits = fits && flux::decode_partials_bytes(*cfg, p) <= needed;
+  flux::Ctx c = {};
+  uint32_t counters;
+  c.decode_counters = &counters;
+  for (size_t room = 4096; room <= (size_t)1 << 28; room *= 4) {
+    c.partials_bytes = room;
+    if (flux::runs_paged(c, *cfg, batch, max_q_len, max_kv_len)) {
+      const flux::DecodePlan r = flux::plan_runs_paged(*cfg, batch, max_q_len, max_kv_len);
+      fits = fits && r.waves == 4 && r.pps == cfg->n_kv_heads && (size_t)2 * r.wgs * r.rpu * (cfg->head_dim + 2) * sizeof(float) <= room;
+    }
+    const flux::PagedPrefillPlan f = flux::plan_prefill_paged(*cfg, batch, max_q_len, max_kv_len, room);
+    fits = fits && f.info_bytes % 16 == 0 && f.wgs >= f.part_units;
+    if (f.part_units > 0) fits = fits && f.info_bytes + (size_t)f.part_units * f.bm * (cfg->head_dim + 2) * sizeof(float) <= room && batch <= 64;
+  }
+  return fits;
+}
 int hostcheck_decode_rows_fit(const flux_attn_cfg* cfg, int batch, int max_kv_len) {
   const flux::DecodePlan p = flux::plan_decode(*cfg, batch, max_kv_len);
   const size_t rows = (size_t)2 * p.wgs * p.rpu * (cfg->head_dim + 2) * sizeof(float);

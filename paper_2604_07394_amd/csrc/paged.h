@@ -9,6 +9,7 @@ constexpr int kPageTokens = FLUX_PAGE_TOKENS;
 constexpr int kPlanRows = 1024;               // slots that a workgroup of flux_page_plan writes
 constexpr float kPagedGuard = 1073741824.0f;  // 2^30: a page whose weights sum past this moves the softmax reference
 constexpr long long kAppendPagedWaves = 4096; // an append takes as many as that where blocks may be many (see kv_append_paged_kernel)
+constexpr int kPagedFewWgs = 256;            // workgroups of eight waves that a decode call takes at most
 constexpr int kMinScaleExp = -100;            // of the scale of a block; its codes reach down to 2^-109
 
 hipError_t launch_page_plan(const Ctx& c, const flux_page_table& pt, const int32_t* cu_new, int total_new, int32_t* slots, hipStream_t s);
@@ -18,8 +19,20 @@ hipError_t launch_kv_append_paged(const Ctx& c, const flux_paged_kv& kv, int hkv
 
 inline int pages_of(int tokens) { return tokens / kPageTokens + (tokens % kPageTokens != 0 ? 1 : 0); }
 // A page of 8-bit codes has the bytes of 32 rows of a bf16 cache, the block that the plan of a decode call counts in.
-inline DecodePlan plan_decode_paged(const flux_attn_cfg& cfg, int batch, int max_kv_len) {
-  return plan_decode(cfg, batch, 32 * pages_of(max_kv_len));
+// `one_each`: calls of few pages take workgroups of eight waves with a page each (see DecodePlan), of which a CU holds one at a time: up
+// to kPagedFewWgs of them.  us of the kernel with at most 0 / 128 / 256 / 512, 32/8 heads of 128: 3 lists of 144 keys 7.4 / 7.3 / 6.9 /
+// 7.2, 1 x 2000 9.0 / 8.9 / 8.7 / 8.8, 1 x 8000 11.6 / 11.8 / 10.2 / 10.5, 2 x 5000 12.0 / 12.0 / 10.9 / 11.1, 16 x 250 at 16/8 heads 7.5 /
+// 7.6 / 6.9 / 7.6.
+inline DecodePlan plan_decode_paged(const flux_attn_cfg& cfg, int batch, int max_kv_len, bool one_each = true) {
+  DecodePlan p = plan_decode(cfg, batch, 32 * pages_of(max_kv_len));
+  if (p.waves == 8 && !(one_each && p.wgs <= kPagedFewWgs)) {
+    const long long by_four = (long long)batch * p.pps * ((pages_of(max_kv_len) + 3) / 4);
+    p.waves = 4;
+    // (the rows of parts go to the small region, which holds those of 512 workgroups up to 15 per part)
+    if (2ll * (by_four < (1 << p.aligned_shift) ? by_four : (1 << p.aligned_shift)) * p.rpu * (cfg.head_dim + 2) * (long long)sizeof(float) > (long long)kSmallBytes) --p.aligned_shift;
+    p.wgs = (int)(by_four < (1 << p.aligned_shift) ? by_four : (1 << p.aligned_shift));
+  }
+  return p;
 }
 hipError_t launch_decode_paged(const Ctx& c, const flux_attn_cfg& cfg, const void* q, int max_kv_len, const flux_paged_kv& kv,
                                const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s);
@@ -84,10 +97,9 @@ constexpr int runs_per_cu(int head_dim, int blocks) { return head_dim == 128 && 
 inline DecodePlan plan_runs_paged(const flux_attn_cfg& cfg, int batch, int max_q_len, int max_kv_len) {
   flux_attn_cfg one = cfg;
   one.n_q_heads = cfg.n_kv_heads;                            // one pair per KV head
-  DecodePlan p = plan_decode_paged(one, batch, max_kv_len);
+  DecodePlan p = plan_decode_paged(one, batch, max_kv_len, false);
   const long long by_four = (long long)batch * p.pps * ((pages_of(max_kv_len) + 3) / 4);
   p.rpu = max_q_len * (cfg.n_q_heads / cfg.n_kv_heads);
-  p.waves = 4;
   p.aligned_shift = runs_per_cu(cfg.head_dim, (p.rpu + 15) / 16) == 1 ? kDecodeWgsShift : kDecodeAlignedShift;
   p.wgs = (int)(by_four < (1 << p.aligned_shift) ? by_four : (1 << p.aligned_shift));
   return p;
