@@ -336,7 +336,8 @@ int flux_page_release(flux_ctx* ctx, const flux_page_table* pt, const int32_t* k
  * Powers of two cost a code of 4 exponent bits nothing (values below 2^-14 of the block's largest one at most) and make that
  * second rounding exact but for such values.  Rounding is to nearest even.  Values that are not finite are
  * stored as NaN and do not count towards the scale; an attention result over such a row is NaN (prefill: also of earlier queries that share a tile of 64 keys
- * with it).  A slot outside the pool raises FLUX_DEV_BAD_PAGE and its row is left out. */
+ * with it).  A slot outside the pool raises FLUX_DEV_BAD_PAGE and its row is left out.
+ * total_new <= 2^30, (total_new / 64 + 1) * n_kv_heads <= 2^30. */
 int flux_kv_append_paged(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int head_dim, const void* k_new, const void* v_new,
                          const int32_t* slots, int total_new, void* stream);
 

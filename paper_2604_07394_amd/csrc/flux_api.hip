@@ -452,6 +452,7 @@ int flux_kv_append_paged(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads,
   if (!ctx || !k_new || !v_new || !slots) return FLUX_EINVAL;
   if (head_dim != 64 && head_dim != 128) return FLUX_EINVAL;
   if (n_kv_heads <= 0 || total_new < 0 || total_new > (1 << 30)) return FLUX_EINVAL;
+  if ((total_new / 64 + 1ll) * n_kv_heads > (1 << 30)) return FLUX_EINVAL;   // (tile of rows, head) pairs are counted in 32 bits
   const int rc = check_paged_kv(kv, head_dim);
   if (rc != FLUX_OK) return rc;
   if (!aligned16(k_new) || !aligned16(v_new)) return FLUX_EINVAL;

@@ -19,7 +19,7 @@ struct PagedAppendArgs {
   int64_t stride_p, stride_h, stride_t;
   const int32_t* slots;
   int hkv, total, n_pages;
-  long long units;                // (tile of 64 token rows, head, K or V, 2^share)
+  uint32_t units;                 // (tile of 64 token rows, head, K or V, 2^share)
   int share;
   uint32_t* status;
 };
@@ -57,9 +57,9 @@ __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a)
   constexpr int STEPS = 64 / RPS;
   const int l = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per_tile = (2 * a.hkv) << a.share;
-  for (long long u = (long long)blockIdx.x * 4 + w; u < a.units; u += (long long)gridDim.x * 4) {
-    const int tile = (int)(u / per_tile), rest = (int)(u - (long long)tile * per_tile);
+  const uint32_t per_tile = (2u * a.hkv) << a.share;
+  for (uint32_t u = blockIdx.x * 4 + w; u < a.units; u += gridDim.x * 4) {   // (units < 2^31, a launch below 2^25)
+    const int tile = (int)(u / per_tile), rest = (int)(u - tile * per_tile);
     const int turn = rest & ((1 << a.share) - 1), h = rest >> (a.share + 1);
     const bool is_v = (rest >> a.share) & 1;
     const int t0 = tile * 64;
@@ -174,8 +174,8 @@ hipError_t launch_kv_append_paged(const Ctx& c, const flux_paged_kv& kv, int hkv
   const long long tiles = ((long long)total_new + 63) / 64 * 2 * hkv;
   a.share = 6;
   while (a.share > 0 && (tiles << a.share) > kAppendPagedWaves) --a.share;
-  a.units = tiles << a.share;
-  const long long wgs = (a.units + 3) / 4;
+  a.units = (uint32_t)(tiles << a.share);
+  const long long wgs = ((long long)a.units + 3) / 4;
   const dim3 grid((unsigned)(wgs < kAppendMost ? wgs : kAppendMost)), block(256);
   if (d == 128) hipLaunchKernelGGL((kv_append_paged_kernel<128>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((kv_append_paged_kernel<64>), grid, block, 0, s, a);
