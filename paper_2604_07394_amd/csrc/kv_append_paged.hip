@@ -52,7 +52,7 @@ __device__ __forceinline__ float finite_or_nan(float x) { return x - x == 0.f ? 
 // read and written; a plain copy of 1 GB reaches 5.2.)
 template <int D>
 __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a) {
-  constexpr int LPR = D / 8;                                 // lanes per row, 16 bytes each
+  constexpr int LPR = D / 16;                                // lanes per row, 16 values each
   constexpr int RPS = 64 / LPR;                              // rows per step
   constexpr int STEPS = 64 / RPS;
   const int l = threadIdx.x & 63;
@@ -81,17 +81,20 @@ __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a)
       }
       const uint64_t others = ~__builtin_amdgcn_ballot_w64(first + l < 64 && mine == slot + l);
       const int rows = others == 0 ? 64 : __builtin_ctzll(others);
-      const char* src = (is_v ? a.v_new : a.k_new) + (((int64_t)t * a.hkv + h) * D + (l % LPR) * 8) * 2;
+      const char* src = (is_v ? a.v_new : a.k_new) + (((int64_t)t * a.hkv + h) * D + (l % LPR) * 16) * 2;
       const int64_t src_step = (int64_t)a.hkv * D * 2;
       float* const scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.hkv + h;
-      char* const dst = (is_v ? a.v : a.k) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h + (l % LPR) * 8;
-      u32x4 x[STEPS];
+      char* const dst = (is_v ? a.v : a.k) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h + (l % LPR) * 16;
+      u32x4 x[STEPS][2];
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
-        x[i] = u32x4{0, 0, 0, 0};
+        x[i][0] = x[i][1] = u32x4{0, 0, 0, 0};
         if (i * RPS < rows) {                                // (uniform)
           const int r = i * RPS + l / LPR;
-          if (r < rows) x[i] = *(const u32x4*)(src + r * src_step);
+          if (r < rows) {
+            x[i][0] = *(const u32x4*)(src + r * src_step);
+            x[i][1] = *(const u32x4*)(src + r * src_step + 16);
+          }
         }
       }
       const float old = first != 0 ? *scale_at : 0.f;
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a)
 #pragma unroll
       for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = pk_max(top, x[i][j] & 0x7FFF7FFFu);
+        for (int j = 0; j < 8; ++j) top = pk_max(top, x[i][j >> 2][j & 3] & 0x7FFF7FFFu);
       bool odd = (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u;
       odd = __builtin_amdgcn_ballot_w64(odd) != 0;           // some value is not finite
       if (odd) {
@@ -107,7 +110,7 @@ __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a)
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) top = pk_max(top, finite_bits(x[i][j]));
+          for (int j = 0; j < 8; ++j) top = pk_max(top, finite_bits(x[i][j >> 2][j & 3]));
       }
       int amax = max((int)(top & 0xFFFFu), (int)(top >> 16));
 #pragma unroll
@@ -122,27 +125,28 @@ __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a)
       for (int i = 0; i < STEPS; ++i) {
         if (i * RPS >= rows) continue;
         const int r = i * RPS + l / LPR;
-        float f[8];
+        uint32_t codes[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          f[2 * j] = bf16_lo(x[i][j]);
-          f[2 * j + 1] = bf16_hi(x[i][j]);
-        }
-        if (odd) {
+          const uint32_t lo = x[i][j >> 1][2 * (j & 1)], hi = x[i][j >> 1][2 * (j & 1) + 1];
+          float f[4] = {bf16_lo(lo), bf16_hi(lo), bf16_lo(hi), bf16_hi(hi)};
+          if (odd) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = finite_or_nan(f[j]);
+            for (int k = 0; k < 4; ++k) f[k] = finite_or_nan(f[k]);
+          }
+          codes[j] = codes4(f[0], f[1], f[2], f[3], inv);
         }
-        if (r < rows) *(u32x2*)(dst + (first + r) * a.stride_t) = u32x2{codes4(f[0], f[1], f[2], f[3], inv), codes4(f[4], f[5], f[6], f[7], inv)};
+        if (r < rows) *(u32x4*)(dst + (first + r) * a.stride_t) = u32x4{codes[0], codes[1], codes[2], codes[3]};
       }
       if (first != 0 && scale > old) {                       // the rows that the page holds take the new scale too
         const float down = old * inv;
         for (int r0 = 0; r0 < first; r0 += RPS) {
           const int r = r0 + l / LPR;
           if (r >= first) continue;
-          u32x2* const at = (u32x2*)(dst + r * a.stride_t);
-          u32x2 c = *at;
+          u32x4* const at = (u32x4*)(dst + r * a.stride_t);
+          u32x4 c = *at;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
+          for (int j = 0; j < 4; ++j) {
             const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[j], true);
             c[j] = codes4(lo[0], lo[1], hi[0], hi[1], down);
           }
