@@ -38,7 +38,10 @@ hipError_t launch_decode_paged(const Ctx& c, const flux_attn_cfg& cfg, const voi
                                const flux_page_table& pt, const uint8_t* mode, void* out, hipStream_t s);
 
 // ---- prefill over pages: what its launch is bounded by (the plan itself is taken on the device, see paged_plan)
-constexpr int kPagedResident = 512;           // workgroups that the chip holds at once, two per CU
+// Workgroups that the chip holds at once, per CU two at head dimension 128, three and (tiles of 64 rows) four at 64.  (With one
+// register more than three of them have, 8192 tokens of 32/8 heads of 64 took 332 us, now 287.)
+constexpr int paged_per_cu(int head_dim, int bm) { return head_dim == 128 ? 2 : (bm == 64 ? 4 : 3); }
+constexpr int paged_resident(int head_dim, int bm) { return 256 * paged_per_cu(head_dim, bm); }
 constexpr int kPagedMinPages = 8;             // a unit that shares a tile with others has at least so many pages
 // Units of one (KV head, part) have ids of one residue mod 8, or of 8 / groups residues: units that `groups` of them take, some of
 // them padding.
@@ -75,16 +78,16 @@ inline PagedPrefillPlan plan_prefill_paged(const flux_attn_cfg& cfg, int batch, 
   // 100 7.5 / 9.5, 16 x 60 to 140 (1024 tiles of 64) 16.8 / 14.1, 512 at 8/2 heads of 64 (1024 side by side) 10.0 / 12.7, 4 x 300 to 700
   // of 64 15.6 / 17.1; 64 tokens behind 8000 28.3 / 28.4, 128 behind 16000 54.5 / 46.9, 512 behind 32000 326 / 235.
   const long long tiles64 = (long long)batch * cfg.n_kv_heads * ((rows + 63) / 64);
-  p.bm = rows <= 64 || (tiles64 <= (cfg.head_dim == 128 ? 512 : 1024) && max_kv_len <= 2ll * max_q_len) ? 64 : 128;
+  p.bm = rows <= 64 || (tiles64 <= paged_resident(cfg.head_dim, 64) && max_kv_len <= 2ll * max_q_len) ? 64 : 128;
   p.tiles = (int)((rows + p.bm - 1) / p.bm);
   p.wgs = (long long)batch * unit_count(cfg.n_kv_heads, p.tiles);
   p.part_units = 0;
   p.info_bytes = (((size_t)batch * cfg.n_kv_heads * p.tiles + 1) * 16 + 255) / 256 * 256;
   // worth a second launch where lists may be long and tiles few (the tiles of the longest run of queries are, and the device knows
   // the others)
-  if (batch <= 64 && pages_of(max_kv_len) >= 2 * kPagedMinPages && 3ll * cfg.n_kv_heads * p.tiles <= 2 * kPagedResident && p.info_bytes <= partials_bytes / 4) {
+  if (batch <= 64 && pages_of(max_kv_len) >= 2 * kPagedMinPages && 3ll * cfg.n_kv_heads * p.tiles < 2 * paged_resident(cfg.head_dim, p.bm) && p.info_bytes <= partials_bytes / 4) {
     const size_t fit = (partials_bytes - p.info_bytes) / ((size_t)p.bm * (cfg.head_dim + 2) * sizeof(float));
-    const size_t want = 2 * kPagedResident + (size_t)8 * batch;
+    const size_t want = 2 * (size_t)paged_resident(cfg.head_dim, p.bm) + (size_t)8 * batch;
     p.part_units = (int)(fit < want ? fit : want);
     if (p.wgs < p.part_units) p.wgs = p.part_units;
   }

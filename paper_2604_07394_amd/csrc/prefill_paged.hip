@@ -111,13 +111,13 @@ __device__ __forceinline__ int wave_min(int x) {
 // all pages upwards, by a model in units of one page: the longest part, or, where the units take more than one round, that
 // share and half a part of unevenness; and 0.02 for writing and merging the rows of a part.  (With the share alone a call of 16 x 8
 // lists took 576 units, the last 64 of them by themselves: 16 x 5 queries 62 us, now 36.)
-__device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, const PagedSeq& mine) {
+__device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, const PagedSeq& mine, int resident) {
   if (a.part_units == 0) return kPagedNoSplit;               // (the batch has at most 64 sequences otherwise)
   float tiles = (float)mine.tiles, pages = (float)mine.tiles * (float)mine.pages;
   tiles = wave_sum(tiles) * (float)a.hkv;
   pages = wave_sum(pages) * (float)a.hkv;
-  if (3.f * tiles > 2.f * kPagedResident) return kPagedNoSplit;
-  const float share = pages * (1.0f / kPagedResident);
+  if (3.f * tiles >= 2.f * (float)resident) return kPagedNoSplit;
+  const float share = pages / (float)resident;
   const int cand = l == 63 ? kPagedNoSplit : max(kPagedMinPages, (int)(share * (float)(l + 32) * (1.0f / 32.0f)) + 1);   // (1 to 3 shares)
   const float inv = 1.0f / (float)cand;
   int units = 0, rows = 0;
@@ -132,7 +132,7 @@ __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, con
     rows += n > 1 ? a.hkv * n * t : 0;
     longest = fmaxf(longest, (float)p / (float)n);
   }
-  float cost = (units <= kPagedResident ? longest : fmaxf(longest, share + 0.5f * longest)) + 0.02f * (float)rows;
+  float cost = (units <= resident ? longest : fmaxf(longest, share + 0.5f * longest)) + 0.02f * (float)rows;
   if (units > a.n_wg || units > a.part_units) cost = 1e30f;
   if (l == 63) cost = fminf(cost, 1e29f);                    // (splits nothing, and always fits)
   return __builtin_amdgcn_readlane(cand, wave_min((__builtin_bit_cast(int, cost) & ~63) | l) & 63);   // (positive floats order like their bits)
@@ -148,12 +148,12 @@ __device__ __forceinline__ PagedSeq seq_from_lane(const PagedSeq& s, int i) {
   r.bad = false;
   return r;
 }
-__device__ __forceinline__ PagedUnit paged_plan(const PagedPrefillArgs& a, int wg, int l, int bm) {
+__device__ __forceinline__ PagedUnit paged_plan(const PagedPrefillArgs& a, int wg, int l, int bm, int resident) {
   const PagedSeq first = paged_seq(a, l, bm);
   PagedUnit u;
   u.b = -1;
   u.chunk = kPagedNoSplit;
-  const int chunk = paged_chunk(a, l, first);
+  const int chunk = paged_chunk(a, l, first, resident);
   u.shared = chunk < kPagedNoSplit;
   int base = 0;
   bool bad = false;
@@ -220,7 +220,7 @@ __device__ __forceinline__ u32x4 unpack8_scaled(uint32_t lo, uint32_t hi, float 
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true))};
 }
 template <int D, int QB>
-__global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a) {
+__global__ __launch_bounds__(256, paged_per_cu(D, 64 * QB)) void paged_prompt_kernel(PagedPrefillArgs a) {
   constexpr int WR = 16 * QB;             // query rows per wave
   constexpr int BM = 4 * WR;              // query rows per workgroup
   constexpr int KC = D / 32;              // MFMA k-steps over the head dimension (QK^T)
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedPrefillArgs a
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = tid & 63;
   const int g = l >> 4, n = l & 15;
-  const PagedUnit u = paged_plan(a, blockIdx.x, l, BM);
+  const PagedUnit u = paged_plan(a, blockIdx.x, l, BM, paged_resident(D, BM));
   if (a.part_units > 0 && blockIdx.x == 0 && tid == 0) a.tile_info[0] = i32x4{u.shared, 0, 0, 0};
   if (u.b < 0) return;                                       // uniform for the workgroup
 
@@ -620,7 +620,7 @@ __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
   constexpr int TPR = D / 4, RPW = 256 / TPR;                // rows that a workgroup has in work
   if (a.tile_info[0][0] == 0) return;
   const int groups = a.bm / RPW;
-  const int items = a.batch * a.hkv * a.n_qtiles * groups;   // (64 sequences and two thirds of kPagedResident tiles of one at most)
+  const int items = a.batch * a.hkv * a.n_qtiles * groups;   // (64 sequences and two thirds of paged_resident tiles of one at most)
   for (int it = blockIdx.x; it < items; it += gridDim.x) {
     const int t = it / groups, rg = it - t * groups;
     const int pair = t / a.n_qtiles, tile = t - pair * a.n_qtiles, b = pair / a.hkv, kvh = pair - b * a.hkv;
