@@ -483,7 +483,8 @@ int flux_attn_prefill_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void*
   if (rc != FLUX_OK) return rc;
   if (max_q_len < 0 || max_q_len > max_kv_len) return FLUX_EINVAL;
   // rows of a group and workgroups are counted in 32 bits
-  if ((long long)max_q_len * (cfg->n_q_heads / cfg->n_kv_heads) > (1 << 30)) return FLUX_EINVAL;
+  const long long rows = (long long)max_q_len * (cfg->n_q_heads / cfg->n_kv_heads);
+  if (rows > (1 << 30) || (rows + 63) / 64 > kAppendMost / cfg->n_kv_heads) return FLUX_EINVAL;
   const PagedPrefillPlan p = plan_prefill_paged(*cfg, pt->batch, max_q_len, max_kv_len, ctx->c.partials_bytes);
   if (p.wgs > kAppendMost) return FLUX_EINVAL;
   if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);

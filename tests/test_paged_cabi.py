@@ -105,3 +105,13 @@ def test_the_binding_checks_shapes_and_layouts(F):
             F.PageTable(*t[:i], bad, *t[i + 1:])
     with pytest.raises(AttributeError):                      # a handle's tensors stay its own
         pt.table = pt.table.clone()
+
+
+def test_prefill_refuses_more_tiles_than_it_counts(F, nodev):
+    """Tiles times KV heads that pass 31 bits, by one and by far."""
+    for hkv, mq in ((128, 1 << 30), (1 << 20, 1 << 30), (2 ** 31 - 1, 1 << 30), (1 << 22, 65), (257, 1 << 20)):
+        cfg = F.attn_cfg(hkv, hkv, 64, 4, 16)
+        pt = table(F, batch=1, table_pages=1 << 24)
+        assert rc_of(F, F.flux_attn_prefill_paged, nodev, cfg, 4096, 768, mq, 1 << 30, pool(F), pt, 512, 1024) == F.FLUX_EINVAL, (hkv, mq)
+    cfg = F.attn_cfg(128, 128, 64, 4, 16)
+    assert rc_of(F, F.flux_attn_prefill_paged, nodev, cfg, 4096, 768, 1 << 20, 1 << 20, pool(F), table(F, batch=1, table_pages=1 << 24), 512, 1024) == F.FLUX_EHIP
