@@ -324,29 +324,32 @@ int flux_page_plan(flux_ctx* ctx, const flux_page_table* pt, const int32_t* cu_n
 /* Cut every sequence to its first keep_len[b] positions (dev int32 [batch]; 0: the request is done; kv_len[b] or more: nothing
  * changes; fewer: rejected tokens are taken back) and return the pages behind them, so that the next flux_page_plan takes the
  * page of the first sequence's first returned place first (a plan is taken back exactly).  Returned table entries become -1.
- * batch <= FLUX_MAX_PAGED_BATCH, batch * table_pages < 2^31.  Pages that stand in several tables must not be returned.  If the list of free pages would grow past n_pages, or an entry
- * lies outside the pool, FLUX_DEV_BAD_PAGE is raised and the page is not listed. */
+ * batch <= FLUX_MAX_PAGED_BATCH, batch * table_pages < 2^31.  Pages that stand in several tables must not be returned.  If the list
+ * of free pages would grow past n_pages, or an entry lies outside the pool, FLUX_DEV_BAD_PAGE is raised and the page is not listed. */
 int flux_page_release(flux_ctx* ctx, const flux_page_table* pt, const int32_t* keep_len, void* stream);
 
 /* Quantise new K/V rows of one layer into their slots.  k_new, v_new: dev bf16 [total_new, n_kv_heads, head_dim]; slots: dev
  * int32 [total_new] as flux_page_plan writes them (rows of one page lie next to each other, in the order of their positions;
- * no two rows have the same slot); rows with a negative slot, which stand before or behind those of a page, are left out.  The scale of a (page, head) is 2^e with the smallest
- * e >= -100 for which no value of its block exceeds 448 * 2^e, the largest code; a page that holds rows already (slot % 64 of its
+ * no two rows have the same slot); rows with a negative slot, which stand before or behind those of a page, are left out.  The
+ * scale of a (page, head) is 2^e with the smallest e >= -100 for which no value of its block exceeds 448 * 2^e, the largest code; a page that holds rows already (slot % 64 of its
  * first new row is not 0) keeps its scale unless a new row needs a larger one: then the codes it holds are rounded to that.
  * Powers of two cost a code of 4 exponent bits nothing (values below 2^-14 of the block's largest one at most) and make that
  * second rounding exact but for such values.  Rounding is to nearest even.  Values that are not finite are
- * stored as NaN and do not count towards the scale; an attention result over such a row is NaN (prefill: also of earlier queries that share a tile of 64 keys
- * with it).  A slot outside the pool raises FLUX_DEV_BAD_PAGE and its row is left out.
+ * stored as NaN and do not count towards the scale; an attention result over such a row is NaN (prefill: also of earlier
+ * queries that share a tile of 64 keys with it).  A slot outside the pool raises FLUX_DEV_BAD_PAGE and its row is left out.
  * total_new <= 2^30, (total_new / 64 + 1) * n_kv_heads <= 2^30. */
 int flux_kv_append_paged(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int head_dim, const void* k_new, const void* v_new,
                          const int32_t* slots, int total_new, void* stream);
 
 /* flux_attn_decode over a paged 8-bit cache: one query per sequence at position kv_len[b] - 1, mode bytes, SA rule, outputs and
- * determinism as there; keys and values are code * scale (any finite scale >= 0).  max_kv_len: host upper bound on kv_len[b],
+ * determinism as there; keys and values are code * scale (any finite scale >= 0;
+ * one of V below 2^-126 counts as that).  max_kv_len: host upper bound on kv_len[b],
  * at most 64 * table_pages (which is always valid); pages of a longer list are left out, the oldest kept, and FLUX_DEV_BAD_LENGTH
  * is raised.  Where all sequences are SA, 64 * (ceil(n_sink / 64) + ceil(window / 64) + 1) is enough (n_sink and window rounded
  * up to multiples of sa_block).  The workspace that flux_workspace_needed names for these arguments is enough.
  * batch * n_kv_heads * ceil(group / 16) * (ceil(max_kv_len / 64) + 16) must be below 2^31 (FLUX_EINVAL).
+ * A score scale * sk * (q . ck) is an fp32 number and may be of either sign, up to 2^24 in magnitude: beyond that fp32 does not tell
+ * scores that are one apart from each other, and the row may be anything.
  * What lies behind kv_len[b] in a page is never used.  A table entry outside the pool counts as a page that is not there, and
  * raises FLUX_DEV_BAD_PAGE; rows without any key are zero. */
 int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, int max_kv_len, const flux_paged_kv* kv,
@@ -354,7 +357,7 @@ int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* 
 
 /* flux_attn_prefill over a paged 8-bit cache: q, cu_q, max_q_len, max_kv_len, mode, out as there (the queries of sequence b are the
  * last n_q(b) positions of its pages: flux_page_plan and flux_kv_append_paged first); keys and values are code * scale (any
- * finite scale >= 0; one of V below 2^-126 counts as that).  A tile of query rows holds all heads
+ * finite scale >= 0; one of V below 2^-126 counts as that; scores as in flux_attn_decode_paged).  A tile of query rows holds all heads
  * of a group, token by token, and walks only pages of which a row sees something; pages of a tile may be shared out over several
  * workgroups where max_kv_len >= 1024, as far as the workspace has room for their results (any context will do), in a way that
  * depends on the bounds, lengths and modes of the whole batch.  Where max_q_len * group <= 32 the rows of a sequence are worked on

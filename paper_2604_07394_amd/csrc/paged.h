@@ -26,7 +26,7 @@ inline int pages_of(int tokens) { return tokens / kPageTokens + (tokens % kPageT
 inline DecodePlan plan_decode_paged(const flux_attn_cfg& cfg, int batch, int max_kv_len, bool one_each = true) {
   DecodePlan p = plan_decode(cfg, batch, 32 * pages_of(max_kv_len));
   if (p.waves == 8 && !(one_each && p.wgs <= kPagedFewWgs)) {
-    const long long by_four = (long long)batch * p.pps * ((pages_of(max_kv_len) + 3) / 4);
+    const long long by_four = (long long)batch * p.pps * (pages_of(max_kv_len) / 4 + (pages_of(max_kv_len) % 4 != 0 || max_kv_len == 0 ? 1 : 0));   // (one at least)
     p.waves = 4;
     // (the rows of parts go to the small region, which holds those of 512 workgroups up to 15 per part)
     if (2ll * (by_four < (1 << p.aligned_shift) ? by_four : (1 << p.aligned_shift)) * p.rpu * (cfg.head_dim + 2) * (long long)sizeof(float) > (long long)kSmallBytes) --p.aligned_shift;

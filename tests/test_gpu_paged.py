@@ -404,3 +404,53 @@ def test_nan_is_seen_only_by_those_who_look(F, ctx):
     assert torch.isnan(out[0, :2]).all() and torch.isfinite(out[0, 2:]).all()
     ref = decode_ref(qf[1:], seqs[1:], [SA], 16, 200)
     check(out[1:], ref, tolerance(qf, seqs, d), seqs)
+
+
+@pytest.mark.parametrize("batch,hq,hkv", [(1, 4, 2), (40, 16, 8), (300, 16, 8)])   # launches of 2, 320 and 2400 lists
+@pytest.mark.parametrize("cached", [0, 70])
+def test_decode_with_a_bound_of_zero(F, ctx, batch, hq, hkv, cached):
+    """No page may be read then: rows of zeros, and a word of warning where there are some."""
+    kv, pt, q, _, _ = attention_case(F, [cached] * batch, hq, hkv, 64, seed=batch)
+    out = torch.full((batch, hq, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    F.flux_attn_decode_paged(ctx, F.attn_cfg(hq, hkv, 64, 4, 16), q, 0, kv, pt, torch.ones(batch, dtype=torch.uint8, device="cuda"), out)
+    assert (out == 0).all()
+    assert F.flux_last_device_status(ctx) == (F.FLUX_DEV_BAD_LENGTH if cached else 0)
+
+
+@pytest.mark.parametrize("lens", [[3], [200], [2000, 64], [30000]])   # one wave, waves without a page, parts
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_far_below_zero(F, ctx, lens, d):
+    """Scores of -2^17 d^0.5 for every key but some of twice that: the weights are relative to the largest one however low it lies,
+    and the result is the mean of V over the first ones.  (q and the keys are powers of two and so are the scales: the scores are
+    exact, and what the exponent's rounding leaves of a weight is the same for all keys.)"""
+    hq, hkv = 4, 2
+    rng = np.random.default_rng(d)
+    kv, pt, q, qf, seqs = attention_case(F, lens, hq, hkv, d, seed=5)
+    q.fill_(-2.0 ** 17)
+    low = torch.from_numpy(rng.random(tuple(kv.k.shape[:3])) < 0.3).cuda()
+    one = [int(torch.tensor([x], dtype=torch.float32).to(torch.float8_e4m3fn).view(torch.uint8)) for x in (1.0, 2.0)]
+    kv.k.copy_(torch.where(low, one[1], one[0])[..., None].expand(kv.k.shape).to(torch.uint8))
+    kv.k_scale.fill_(1.0)
+    kv.v_scale.copy_(torch.exp2(torch.floor(torch.log2(kv.v_scale))))
+    table, codes, scale = pt.table.cpu().numpy(), kv.v.cpu().numpy(), kv.v_scale.cpu().numpy()
+    seqs = [[None, P.gather(codes, scale, table[b], n)] for b, n in enumerate(lens)]
+    ref = np.zeros((len(lens), hq, d))
+    for b, n in enumerate(lens):
+        flag = low.cpu().numpy()[table[b, :-(-n // 64)]].transpose(0, 2, 1).reshape(-1, hkv)[:n]
+        for h in range(hq):
+            keep = ~flag[:, h // 2] if not flag[:, h // 2].all() else flag[:, h // 2]
+            ref[b, h] = seqs[b][1][keep, h // 2].mean(0)
+    out = torch.empty(len(lens), hq, d, dtype=torch.float32, device="cuda")
+    cfg = F.attn_cfg(hq, hkv, d, 0, 1, 0.0, 1)
+    mode = torch.ones(len(lens), dtype=torch.uint8, device="cuda")
+    v = max(float(np.abs(s[1]).max()) for s in seqs)
+    F.flux_attn_decode_paged(ctx, cfg, q, max(lens), kv, pt, mode, out)
+    # all weights are alike: sums of n terms in fp32, 2^-24 of the sum of the magnitudes a term and as much for the denominator; two
+    # terms leave 2^-16 of a weight
+    assert np.abs(H.torch_to_f64(out) - ref).max() <= (2 * (max(lens) + 8) * 2.0 ** -24 + 2 * 2.0 ** -16) * v
+    # the same as a run of one query, and as a tile (the bound on the queries says which)
+    for most in (1, max(lens)):
+        F.flux_attn_prefill_paged(ctx, cfg, q, cu_of([1] * len(lens)), most, max(lens), kv, pt, mode, out)
+        # (the denominator sums the rounded weights)
+        assert np.abs(H.torch_to_f64(out) - ref).max() <= (2 * (max(lens) + 8) * 2.0 ** -24 + 2 * 2.0 ** -16) * v
+    assert F.flux_last_device_status(ctx) == 0
