@@ -1,7 +1,8 @@
 // How a decode call is shared out over the chip, and how the parts of a list are merged: what the decode kernels of the
 // contiguous and of the paged cache have in common.  A call is described by a struct `s` with the members batch, pps,
 // most_by_four and aligned_shift (see SplitArgs in decode.hip), for which load_counted(s, b, bad) says how many blocks
-// sequence b has, and S::seam_blocks(head_dim) what going on to the next list counts: 32 keys of a bf16 cache or a page of 64 keys of an 8-bit one, the same bytes either way.
+// sequence b has (32 keys of a bf16 cache or a page of 64 keys of an 8-bit one, the same bytes either way), and
+// S::seam_blocks(head_dim) how many of them going on to the next list counts.
 #pragma once
 
 #include <utility>

@@ -47,9 +47,12 @@ __device__ __forceinline__ float finite_or_nan(float x) { return x - x == 0.f ? 
 // A wave looks at 64 token rows, where blocks begin in them, and does one block in 2^share for one head, K or V: in a decode step
 // every row begins a block, in a long prompt one or two of 64 do, and only the slots tell which it is.  So short calls have as many
 // waves as there may be blocks, and long ones about kAppendPagedWaves at least, most of which leave at once: us with 1024 / 2048 / 4096
-// / 8192 of them, 8 heads of 128, one row of 256 sequences 9.4 / 6.8 / 7.1 / 7.0, five of each 16.4 / 11.3 / 8.2 / 8.3, 512 rows of one
-// 6.0 / 7.0 / 7.8 / 10.8, 2100 rows of three 6.4 / 7.0 / 8.1 / 12.0, 8000 of four 13.4 / 13.5 / 12.3 / 13.1.  (32768 rows 42.4: 4.75 TB/s
-// read and written; a plain copy of 1 GB reaches 5.2.)
+// / 8192 of them, 8 heads of 128, one row of 256 sequences 8.6 / 6.6 / 5.8 / 5.7, five of each 14.1 / 9.4 / 7.5 / 7.1, 512 rows of one
+// 5.4 / 6.2 / 6.5 / 8.9, 2100 rows of three 5.8 / 6.4 / 7.0 / 10.1, 8000 of four 13.2 / 13.2 / 12.0 / 12.0.  (32768 rows take 41.5 with
+// any: 4.9 TB/s read and written, where a plain copy of 1 GB reaches 5.2.  64 sequences with a row each: 4.0, a launch, the slots,
+// the scale and the row one behind the other.)
+// A lane has 16 values of a row, two loads and one store of 16 bytes: with 8 values each a store of codes is 8 bytes, and 32768 rows
+// took 42.4.
 template <int D>
 __global__ __launch_bounds__(256) void kv_append_paged_kernel(PagedAppendArgs a) {
   constexpr int LPR = D / 16;                                // lanes per row, 16 values each

@@ -74,20 +74,25 @@ inline PagedPrefillPlan plan_prefill_paged(const flux_attn_cfg& cfg, int batch, 
   const long long rows = (long long)max_q_len * (cfg.n_q_heads / cfg.n_kv_heads);
   // Tiles of 64 rows where they run side by side and walk little more than their own queries: a page takes a wave half the MFMAs, and
   // nothing waits for a second round.  Behind a long context a tile of 128 rows converts and stages half as much.  us with 64 / 128
-  // rows, 32/8 heads of 128 (512 workgroups of 64 rows side by side) unless said: 40 tokens 6.1 / 7.7, 100 6.9 / 8.9, 1000 23.8 / 32.8, 4 x
-  // 100 7.5 / 9.5, 16 x 60 to 140 (1024 tiles of 64) 16.8 / 14.1, 512 at 8/2 heads of 64 (1024 side by side) 10.0 / 12.7, 4 x 300 to 700
-  // of 64 15.6 / 17.1; 64 tokens behind 8000 28.3 / 28.4, 128 behind 16000 54.5 / 46.9, 512 behind 32000 326 / 235.
+  // rows, 32/8 heads of 128 (512 workgroups of 64 rows side by side) unless said: 40 tokens 6.6 / 8.2, 100 7.6 / 9.6, 1000 25.4 / 29.0 and
+  // a launch for shared tiles, 4 x 100 8.1 / 10.0, 16 x 60 to 140 (1024 tiles of 64) 17.2 / 14.4, at 8/2 heads of 64 (1024 side by side)
+  // 512 tokens 10.5 / 12.8, 16 x 60 to 140 7.3 / 8.6; with the merge 64 tokens behind 8000 30.1 / 29.6, 128 behind 16000 61.2 / 51.8,
+  // 512 behind 32000 382 / 274.  (What the bounds say counts: 4 x 300 to 700 tokens at 32/8 heads of 64 take 128 rows and 18.0 where 64
+  // would be 16.8, as 1408 tiles of 64 are possible.)
   const long long tiles64 = (long long)batch * cfg.n_kv_heads * ((rows + 63) / 64);
   p.bm = rows <= 64 || (tiles64 <= paged_resident(cfg.head_dim, 64) && max_kv_len <= 2ll * max_q_len) ? 64 : 128;
   p.tiles = (int)((rows + p.bm - 1) / p.bm);
   p.wgs = (long long)batch * unit_count(cfg.n_kv_heads, p.tiles);
   p.part_units = 0;
   p.info_bytes = (((size_t)batch * cfg.n_kv_heads * p.tiles + 1) * 16 + 255) / 256 * 256;
-  // worth a second launch where lists may be long and tiles few (the tiles of the longest run of queries are, and the device knows
-  // the others)
-  if (batch <= 64 && pages_of(max_kv_len) >= 2 * kPagedMinPages && 3ll * cfg.n_kv_heads * p.tiles < 2 * paged_resident(cfg.head_dim, p.bm) && p.info_bytes <= partials_bytes / 4) {
+  // worth a second launch (4 us where it finds nothing to do) where lists may be long and tiles few, or lists long and tiles no more than
+  // two rounds: the tiles of the longest run of queries, and the device knows the others.  (From 64 pages on 3000 tokens behind 3000 took
+  // 221 us, now 217 as without it; 5000 tokens at 8/2 heads of 64 64.)
+  const long long longest = (long long)cfg.n_kv_heads * p.tiles, side_by_side = paged_resident(cfg.head_dim, p.bm);
+  const bool few = 3 * longest < 2 * side_by_side;
+  if (batch <= 64 && pages_of(max_kv_len) >= (few ? 2 : 16) * kPagedMinPages && longest <= 2 * side_by_side && p.info_bytes <= partials_bytes / 4) {
     const size_t fit = (partials_bytes - p.info_bytes) / ((size_t)p.bm * (cfg.head_dim + 2) * sizeof(float));
-    const size_t want = 2 * (size_t)paged_resident(cfg.head_dim, p.bm) + (size_t)8 * batch;
+    const size_t want = (size_t)((few ? 2 : 3) * side_by_side + 8 * batch);
     p.part_units = (int)(fit < want ? fit : want);
     if (p.wgs < p.part_units) p.wgs = p.part_units;
   }

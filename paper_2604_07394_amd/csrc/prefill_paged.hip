@@ -77,8 +77,8 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedPrefillArgs& a, int b, 
 }
 
 // ---- the plan of a launch, taken on the device by every wave: which unit of work a workgroup is.  A unit is (sequence, KV head,
-// part, tile): part i of a tile has its pages [i * chunk, (i + 1) * chunk).  Where the tiles by themselves fill two thirds of
-// the chip or more, there is one part; otherwise see paged_chunk.
+// part, tile): part i of a tile has its pages [i * chunk, (i + 1) * chunk).  Where the tiles by themselves fill the chip
+// more than twice, there is one part; otherwise see paged_chunk.
 // Units of one (KV head, part) walk the same pages; workgroups go to the 8 XCDs by id mod 8, each with an L2 of its own, so these
 // units get ids of one residue (or of 8 / groups residues).
 struct PagedUnit {
@@ -107,18 +107,22 @@ __device__ __forceinline__ int wave_min(int x) {
   x = min(x, moved<0x143, 0xc>(x, x));
   return __builtin_amdgcn_readlane(x, 63);
 }
-// Pages that a part has at most: every lane works out one candidate, from the share that one of the resident workgroups has of
-// all pages upwards, by a model in units of one page: the longest part, or, where the units take more than one round, that
-// share and half a part of unevenness; and 0.02 for writing and merging the rows of a part.  (With the share alone a call of 16 x 8
-// lists took 576 units, the last 64 of them by themselves: 16 x 5 queries 62 us, now 36.)
+// Pages that a part has at most: every lane works out one candidate, from a fifth of the share that one of the resident workgroups has
+// of all pages to three of them, by a model in units of one page, in which a part takes five pages more than it has, for its start
+// and its end.  One round takes the longest part; more of them as many times the mean part, or what is shared out evenly and half of the
+// longest part, whichever is less; and 0.03 for writing and merging the rows of a part.
+// Calls of up to two rounds of tiles may be shared out.  us with none of more than two thirds of a round / so, 32/8 heads of 128 unless
+// said: 3000 tokens behind 32000 (752 tiles where 512 run side by side) 1650 / 1380, six lists of 40 to 900 behind 500 to 20000 437 /
+// 330, two of 600 to 2400 behind 6000 to 30000 660 / 549, three of 1000 to 3000 behind 100 to 60000 at 16/8 heads 1018 / 860, 4096
+// behind 28672 at 32/8 heads of 64 1127 / 1070; but four of 500 to 1200 behind 1000 to 9000 230 / 241.
 __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, const PagedSeq& mine, int resident) {
   if (a.part_units == 0) return kPagedNoSplit;               // (the batch has at most 64 sequences otherwise)
-  float tiles = (float)mine.tiles, pages = (float)mine.tiles * (float)mine.pages;
+  float tiles = (float)mine.tiles, pages = tiles * 0.5f * (float)(mine.pages + min(((mine.len - mine.n_q) >> 6) + 1, mine.pages));
   tiles = wave_sum(tiles) * (float)a.hkv;
   pages = wave_sum(pages) * (float)a.hkv;
-  if (3.f * tiles >= 2.f * (float)resident) return kPagedNoSplit;
+  if (tiles > 2.f * (float)resident) return kPagedNoSplit;
   const float share = pages / (float)resident;
-  const int cand = l == 63 ? kPagedNoSplit : max(kPagedMinPages, (int)(share * (float)(l + 32) * (1.0f / 32.0f)) + 1);   // (1 to 3 shares)
+  const int cand = l == 63 ? kPagedNoSplit : max(kPagedMinPages, (int)(share * fast_exp2((float)l * (4.f / 62.f) - 2.3f)) + 1);
   const float inv = 1.0f / (float)cand;
   int units = 0, rows = 0;
   float longest = 0.f;
@@ -132,10 +136,14 @@ __device__ __forceinline__ int paged_chunk(const PagedPrefillArgs& a, int l, con
     rows += n > 1 ? a.hkv * n * t : 0;
     longest = fmaxf(longest, (float)p / (float)n);
   }
-  float cost = (units <= resident ? longest : fmaxf(longest, share + 0.5f * longest)) + 0.02f * (float)rows;
+  const int rounds = (units + resident - 1) / resident;
+  const float all = pages + 5.f * (float)units;
+  longest += 5.f;
+  float cost = (rounds <= 1 ? longest : fmaxf(longest, fminf((float)rounds * (all / (float)max(units, 1)), all / (float)resident + 0.5f * longest))) + 0.03f * (float)rows;
   if (units > a.n_wg || units > a.part_units) cost = 1e30f;
   if (l == 63) cost = fminf(cost, 1e29f);                    // (splits nothing, and always fits)
-  return __builtin_amdgcn_readlane(cand, wave_min((__builtin_bit_cast(int, cost) & ~63) | l) & 63);   // (positive floats order like their bits)
+  const int best = wave_min((__builtin_bit_cast(int, cost) & ~63) | l) & 63;   // (positive floats order like their bits)
+  return __builtin_amdgcn_readlane(rows, best) == 0 ? kPagedNoSplit : __builtin_amdgcn_readlane(cand, best);
 }
 __device__ __forceinline__ PagedSeq seq_from_lane(const PagedSeq& s, int i) {
   PagedSeq r;
@@ -620,7 +628,7 @@ __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
   constexpr int TPR = D / 4, RPW = 256 / TPR;                // rows that a workgroup has in work
   if (a.tile_info[0][0] == 0) return;
   const int groups = a.bm / RPW;
-  const int items = a.batch * a.hkv * a.n_qtiles * groups;   // (64 sequences and two thirds of paged_resident tiles of one at most)
+  const int items = a.batch * a.hkv * a.n_qtiles * groups;   // (64 sequences and twice paged_resident tiles of one at most)
   for (int it = blockIdx.x; it < items; it += gridDim.x) {
     const int t = it / groups, rg = it - t * groups;
     const int pair = t / a.n_qtiles, tile = t - pair * a.n_qtiles, b = pair / a.hkv, kvh = pair - b * a.hkv;

@@ -163,6 +163,33 @@ def test_prefill_says_when_a_bound_is_too_low(F, ctx, n):
     check(out[[0, n]], ref[[0, n]], tolerance(qf, seqs, d), seqs)
 
 
+@pytest.mark.parametrize("mode", [FA, SA])
+def test_long_lists_of_many_tiles_are_shared_out(F, ctx, mode):
+    """512 tiles of 128 to 160 pages, of which 768 run side by side, and the last tile of three tokens."""
+    n, past, heads, d, sink, window = 4096 + 3, 6000, 16, 64, 70, 5000
+    kv, pt, q, qf, seqs = attention_case(F, [past + n], heads, heads, d, seed=4, rows=[n])
+    cfg, modes = F.attn_cfg(heads, heads, d, sink, window), torch.tensor([mode], dtype=torch.uint8, device="cuda")
+    out = torch.full((n, heads, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    F.flux_attn_prefill_paged(ctx, cfg, q, cu_of([n]), n, past + n, kv, pt, modes, out)
+    k, v = seqs[0]
+    i, j = past + torch.arange(n, device="cuda")[:, None], torch.arange(past + n, device="cuda")[None]
+    seen = (j <= i) & ((j < sink) | (i - j < window) | (mode == FA))
+    bound = tolerance(qf, seqs, d)
+    for h in (0, 9):                                         # the definition in float64, a head at a time
+        kh, vh = (torch.from_numpy(np.ascontiguousarray(x[:, h])).cuda() for x in (k, v))
+        s = (q[:, h].double() @ kh.T.contiguous() / d ** 0.5).masked_fill_(~seen, -torch.inf)
+        ref = (torch.softmax(s, 1) @ vh).cpu().numpy()
+        check(out[:, h], ref, bound, seqs)
+    small = F.flux_create(0, 1)                              # without room for shared tiles: the same but for roundings
+    again = torch.empty_like(out)
+    F.flux_attn_prefill_paged(small, cfg, q, cu_of([n]), n, past + n, kv, pt, modes, again)
+    v_max = float(np.abs(v).max())
+    assert float((again.float() - out.float()).abs().max()) <= 2 * (bound + 3 * 2.0 ** -8 + 2.0 ** -8) * v_max
+    assert F.flux_last_device_status(ctx) == 0
+    torch.cuda.synchronize()
+    F.flux_destroy(small)
+
+
 def test_prefill_rows_are_those_of_decode(F, ctx):
     """The last query of a prefill call is the query of a decode call: the same to what the weights' rounding leaves."""
     hq, hkv, d = 16, 4, 128
