@@ -556,7 +556,7 @@ def main():
         }
         if not args.small:
             decode["roofline"]["traffic"], decode["roofline"]["traffic_note"] = measured_traffic(
-                "decode_fa_long_context_131072", ["decode.hip", "flux_internal.h"])
+                "decode_fa_long_context_131072", ["decode.hip", "decode_cut.h", "flux_internal.h"])
         del kc, vc, dcaches
         torch.cuda.empty_cache()
 

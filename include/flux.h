@@ -5,7 +5,8 @@
  * Full-Attention / Sparse-Attention decision (paper Sec. 3.1), the decision is cached
  * (Sec. 3.3), and each layer then runs causal grouped-query Full Attention (Eq. 1) or
  * Sparse Attention (Eq. 2; the streaming variant of Sec. 4.1 / App. C.3: sink tokens plus a
- * causal local window) over ONE contiguous bf16 KV cache, in prefill and in decode.
+ * causal local window) over ONE contiguous bf16 KV cache, in prefill and in decode, or over
+ * pages of 8-bit codes that all sequences take from one pool.
  *
  * General rules
  *  - Every pointer is a raw address.  "dev" = device memory of the context's GPU, "host" =

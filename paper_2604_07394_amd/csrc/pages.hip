@@ -1,5 +1,7 @@
 // flux_page_plan and flux_page_release: the block tables, slots and free pages of a paged KV cache, from the lengths that the
 // device holds.  What bounds both: latencies (a step of some hundred sequences moves a few KB).
+// Traced, us: 256 sequences with a token each and three of them replaced by prompts of up to 500, plan 6.0 and release 2.7; 64
+// sequences of which 16 are replaced by prompts of 1000 to 16384, 7.6 and 5.4.  An empty launch is about 2.
 //
 // Plan.  Sequence b of length L with n new rows lacks need(b) = ceil((L + n) / 64) - ceil(L / 64) pages; with start(b) the sum of
 // need over the sequences before it, its j-th new page is free_pages[n_free - 1 - start(b) - j].  So everything follows from
