@@ -339,3 +339,54 @@ def test_a_step_replays_from_a_graph(F, ctx):
         torch.cuda.synchronize()
         verify(*f)
     assert F.flux_last_device_status(ctx) == 0
+
+
+def test_lists_in_parts_from_a_graph_and_on_two_streams(F):
+    """Calls whose lists are shared out and merged (tiles, runs of drafts, decode) give the same bits eagerly, replayed from a graph with other
+    lengths than it was captured with, and with another context's calls on another stream beside them."""
+    hq, hkv, d, rows = 8, 2, 128, [20, 3, 9]
+    lens = [7000, 900, 3100]
+    kv, pt, q, _, _ = attention_case(F, lens, hq, hkv, d, seed=21, rows=rows)
+    cfg, wide = F.attn_cfg(hq, hkv, d, 16, 500), 64 * pt.table.shape[1]
+    mode = torch.tensor([FA, SA, FA], dtype=torch.uint8, device="cuda")
+    cu, cu_few = cu_of(rows), cu_of([4, 3, 4])
+
+    def outputs():
+        return [torch.zeros(sum(rows), hq, d, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+
+    def calls(ctx, out):
+        F.flux_attn_prefill_paged(ctx, cfg, q, cu, 20, wide, kv, pt, mode, out[0])
+        F.flux_attn_prefill_paged(ctx, cfg, q, cu_few, 4, wide, kv, pt, mode, out[1])
+        F.flux_attn_decode_paged(ctx, cfg, q, wide, kv, pt, mode, out[2])
+
+    states = [lens, [64, 900, 20], [6500, 7, 3000], [1, 0, 9]]   # (runs longer than their lists are cut)
+    a, b = F.flux_create(0, 0), F.flux_create(0, 0)
+    want = []
+    for s in states:
+        pt.kv_len.copy_(i32(s))
+        out = outputs()
+        calls(a, out)
+        torch.cuda.synchronize()
+        want.append(out)
+    F.flux_last_device_status(a)
+    out = outputs()
+    graph = torch.cuda.CUDAGraph()
+    pt.kv_len.copy_(i32(states[1]))
+    with torch.cuda.graph(graph):
+        calls(a, out)
+    for turn in (0, 1, 2, 3, 0, 2):
+        pt.kv_len.copy_(i32(states[turn]))
+        for x in out:
+            x.zero_()
+        other = outputs()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(3):
+                calls(b, other)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y, z in zip(out, want[turn], other):
+            assert torch.equal(x, y) and torch.equal(z, y), turn
+    for c in (a, b):
+        F.flux_destroy(c)
