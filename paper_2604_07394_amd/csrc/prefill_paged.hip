@@ -394,8 +394,6 @@ __global__ __launch_bounds__(256, paged_per_cu(D, 64 * QB)) void paged_prompt_ke
     for (int db = 0; db < DB; ++db) o[db][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  ids = load_ids(0);
-  ids_next = load_ids(64);
   typedef std::integral_constant<int, 0> Even;
   typedef std::integral_constant<int, 1> Odd;
   load_page(0, Even());
