@@ -15,7 +15,7 @@
 // nothing of K and V is rounded.
 //
 // What bounds it: the matrix pipe and the vector instructions beside it, at the clock that both leave (4096 tokens behind 28672 at 32/8
-// heads of 128: pipe 57 % busy, no LDS bank conflicts, 1635 to 1670 us, 1.23 to 1.26 PFLOP/s; a bf16 cache takes 1540 to 1670, a large
+// heads of 128: pipe 57 % busy, no LDS bank conflicts, 1625 to 1705 us, 1.21 to 1.27 PFLOP/s; a bf16 cache takes 1540 to 1670, a large
 // library product runs at 1.30 to 1.44).  512 behind 32000 take 237 (216), five prompts of 129 to 3001 tokens at 28/4 heads 93 (85 to 96: 1440
 // tiles of 20 pages or so, each with a start and an end).
 //
