@@ -39,7 +39,7 @@ struct PagedPrefillArgs {
   int table_pages, n_pages;
   const int32_t* kv_len;
   const uint8_t* mode;
-  int max_kv_len;
+  int max_q_len, max_kv_len;
   int hq, hkv, group, batch;
   Reciprocal by_group;
   int sink_lim, win_blocks, blk_shift;   // SA geometry (see sa_geom)
@@ -58,11 +58,11 @@ struct PagedPrefillArgs {
 constexpr int kPagedNoSplit = 0x3FFFFFFF;
 
 struct PagedSeq {
-  int q_begin, n_q, len, tiles, pages;   // pages: of its longest tile (an upper bound for SA)
+  int q_begin, n_q, len, rows, tiles, pages;   // rows: those within the bound on the queries; pages: of its longest tile (an upper bound for SA)
   bool sa, bad;
 };
 __device__ __forceinline__ PagedSeq paged_seq(const PagedPrefillArgs& a, int b, int bm) {
-  PagedSeq s = {0, 0, 0, 0, 0, false, false};
+  PagedSeq s = {0, 0, 0, 0, 0, 0, false, false};
   if (b >= a.batch) return s;
   s.q_begin = a.cu_q[b];
   s.n_q = a.cu_q[b + 1] - s.q_begin;
@@ -72,7 +72,8 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedPrefillArgs& a, int b, 
   s.bad = s.n_q < 0 || s.len < 0 || s.len > cap || s.n_q > s.len || s.q_begin < 0 || s.len > a.max_kv_len;
   s.len = s.len < 0 ? 0 : min(s.len, cap);
   s.n_q = s.n_q < 0 || s.q_begin < 0 ? 0 : min(s.n_q, s.len);
-  s.tiles = (int)min(((int64_t)s.n_q * a.group + bm - 1) / bm, (int64_t)a.n_qtiles);
+  s.rows = min(s.n_q, a.max_q_len) * a.group;                // (max_q_len * group <= 2^30)
+  s.tiles = (s.rows + bm - 1) / bm;
   s.pages = (s.len + 63) >> 6;
   if (s.sa) {
     const int64_t win = min((int64_t)a.win_blocks << a.blk_shift, (int64_t)s.len);
@@ -155,6 +156,7 @@ __device__ __forceinline__ PagedSeq seq_from_lane(const PagedSeq& s, int i) {
   r.q_begin = __builtin_amdgcn_readlane(s.q_begin, i);
   r.n_q = __builtin_amdgcn_readlane(s.n_q, i);
   r.len = __builtin_amdgcn_readlane(s.len, i);
+  r.rows = __builtin_amdgcn_readlane(s.rows, i);
   r.tiles = __builtin_amdgcn_readlane(s.tiles, i);
   r.pages = __builtin_amdgcn_readlane(s.pages, i);
   r.sa = __builtin_amdgcn_readlane((int)s.sa, i) != 0;
@@ -258,8 +260,7 @@ __global__ __launch_bounds__(256, paged_per_cu(D, 64 * QB)) void paged_prompt_ke
   if (u.b < 0) return;                                       // uniform for the workgroup
 
   // ---- rows and pages of the tile
-  const int rows = (int)min((int64_t)u.s.n_q * a.group - (int64_t)u.tile * BM, (int64_t)BM);
-  const int r0 = u.tile * BM;                                // (n_q * group may pass 2^31 only with tiles that the bound cuts)
+  const int r0 = u.tile * BM, rows = min(u.s.rows - r0, BM);
   const int pos0 = u.s.len - u.s.n_q;                        // position of the sequence's first query
   auto token_of = [&](int r) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(quotient(r, a.by_group)); };   // (r: uniform)
   const int i_min = pos0 + token_of(r0), i_max = pos0 + token_of(r0 + rows - 1);
@@ -622,7 +623,7 @@ struct PagedMergeArgs {
   const int32_t *cu_q, *kv_len;
   const float *part_o, *part_ml;
   const i32x4* tile_info;
-  int batch, hq, hkv, group, n_qtiles, bm, capacity, out_fp32;
+  int batch, hq, hkv, group, n_qtiles, bm, max_q_len, capacity, out_fp32;
   Reciprocal by_group;
   void* out;
 };
@@ -639,7 +640,7 @@ __global__ __launch_bounds__(256) void paged_prompt_merge(PagedMergeArgs a) {
     int n_q = a.cu_q[b + 1] - q_begin, len = a.kv_len[b];
     len = len < 0 ? 0 : min(len, a.capacity);
     n_q = n_q < 0 || q_begin < 0 ? 0 : min(n_q, len);
-    const int64_t rows = min((int64_t)n_q * a.group - (int64_t)tile * a.bm, (int64_t)a.bm);
+    const int rows = min(min(n_q, a.max_q_len) * a.group - tile * a.bm, a.bm);   // (max_q_len * group <= 2^30)
     const int x = rg * RPW + threadIdx.x / TPR, d = 4 * (threadIdx.x % TPR);
     if (rg * RPW >= rows) continue;                          // (no such tile: what its entry holds is not read)
     const i32x4 info = a.tile_info[1 + t];
@@ -698,6 +699,7 @@ hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const vo
   a.n_pages = kv.n_pages;
   a.kv_len = pt.kv_len;
   a.mode = mode;
+  a.max_q_len = max_q_len;
   a.max_kv_len = max_kv_len;
   a.hq = cfg.n_q_heads;
   a.hkv = cfg.n_kv_heads;
@@ -741,6 +743,7 @@ hipError_t launch_prefill_paged(const Ctx& c, const flux_attn_cfg& cfg, const vo
   m.by_group = a.by_group;
   m.n_qtiles = plan.tiles;
   m.bm = plan.bm;
+  m.max_q_len = max_q_len;
   m.capacity = pt.table_pages * kPageTokens;
   m.out_fp32 = a.out_fp32;
   m.out = out;
