@@ -72,6 +72,7 @@ __device__ __forceinline__ Seq load_counted(const PagedSplit& s, int b, bool& ba
 // Runs of a few queries per sequence (batches of up to 64): every lane holds the number of its sequence's.
 struct RunSplit : PagedSplit {
   int n_q;
+  int max_kv_len;         // a longer sequence is reported, also where the bound holds all pages of its list
 };
 __device__ __forceinline__ Seq load_counted(const RunSplit& s, int b, bool& bad) {
   const int got = s.kv_len[b];
@@ -80,7 +81,7 @@ __device__ __forceinline__ Seq load_counted(const RunSplit& s, int b, bool& bad)
   q.md = s.mode[b] != 0 ? 1 : 0;
   const int n = s.n_q < 0 ? 0 : min(s.n_q, q.len);
   q.nb = n > 0 ? page_list(s, q.len, q.md, q.len - n).pages : 0;
-  bad |= got != q.len || n != s.n_q || q.nb > s.max_pages;
+  bad |= got != q.len || n != s.n_q || q.len > s.max_kv_len;   // (or the list may have more pages than the bound)
   q.nb = min(q.nb, s.max_pages);
   return q;
 }
@@ -95,7 +96,7 @@ struct PagedDecodeArgs {
   PagedSplit sp;
   int hq, hkv, group, qblocks, rpu;      // see DecodeArgs in decode.hip; runs: one pair per KV head, rpu = max_q * group
   const int32_t* cu_q;    // runs only
-  int max_q;              // queries of a run that are computed
+  int max_q, max_kv_len;  // ... queries of a run that are computed, and the host's bound on the lengths
   Reciprocal by_group;
   float scale_log2;
   float* part_o;
@@ -149,6 +150,7 @@ __global__ __launch_bounds__(64 * W, runs_per_cu(D, QB)) void paged_decode_kerne
   static_cast<PagedSplit&>(split) = a.sp;
   int q_begin_mine = 0;
   if constexpr (RUN) {
+    split.max_kv_len = a.max_kv_len;
     split.n_q = 0;
     if (l < a.sp.batch) {
       q_begin_mine = a.cu_q[l];
@@ -600,6 +602,7 @@ PagedDecodeArgs decode_args(const Ctx& c, const flux_attn_cfg& cfg, const void* 
   a.rpu = plan.rpu;
   a.cu_q = nullptr;
   a.max_q = 1;
+  a.max_kv_len = max_kv_len;
   a.scale_log2 = (cfg.softmax_scale != 0.f ? cfg.softmax_scale : 1.0f / sqrtf((float)cfg.head_dim)) * kLog2e;
   a.part_o = part_rows;
   a.part_ml = a.part_o + (size_t)2 * plan.wgs * plan.rpu * cfg.head_dim;
