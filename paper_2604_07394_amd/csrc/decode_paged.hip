@@ -10,7 +10,7 @@
 // of 4224 20.0 (28 to 30), of which 3.0 are the launch and the cut, 1 page numbers, 10.3 the streaming, 1.5 the last page, 1 the merge of the
 // waves and 2.4 that of the parts; 32 ragged lists of 513 to 8400 at 28/4 heads 25.2 (38); one of 2001 at 8/2 heads of 64 7.3 (6.8:
 // page numbers are a latency more).  16 runs of 5 queries behind 300 to 16000 keys
-// 53 us, 240 MB: the loop over the pages takes 32 of them, the cut, two-block merges of waves and of parts the rest (the kernel for
+// 54.6 us, 240 MB: the loop over the pages takes more than half, the cut, two-block merges of waves and of parts the rest (the kernel for
 // prompts took 63, a bf16 cache 95).
 //
 // Per wave, a page at a time:
@@ -397,8 +397,10 @@ __global__ __launch_bounds__(64 * W, runs_per_cu(D, QB)) void paged_decode_kerne
       // maximum is taken (over the 4 lane groups of a query), the references move there and the weights are taken again.
       // TERMS bf16 values make a weight: two leave 2^-16 of it (see decode.hip), three 2^-24, which is what an fp32 output holds
       // (8/2 heads of 64, 2001 keys: 2-norm of the error 3.7e-6 of the result's with two).
-      // Runs take a term less: a weight of one is rounded to bf16, and the denominator sums the rounded ones.
-      constexpr int TERMS = (FP32 ? 3 : 2) - (RUN ? 1 : 0);
+      // Runs take as many, so that a drafted token is scored as the decode step that it stands for would score it.  (With a term less 16
+      // runs of 5 behind 300 to 16000 keys took 53.1 us for 54.6, 64 of them 158 for 166; 2-norm of the error 2.02e-3 and
+      // now 1.65e-3, which is the rounding of a bf16 output.)
+      constexpr int TERMS = FP32 ? 3 : 2;
       uint32_t pk[NB][TERMS][8];
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
@@ -426,7 +428,6 @@ __global__ __launch_bounds__(64 * W, runs_per_cu(D, QB)) void paged_decode_kerne
           for (int db = 0; db < DB; ++db) o[db][b] *= alpha;
           weights();
         }
-        if constexpr (TERMS == 1) psum = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           float x = e[2 * j], y = e[2 * j + 1];
@@ -437,7 +438,6 @@ __global__ __launch_bounds__(64 * W, runs_per_cu(D, QB)) void paged_decode_kerne
             y -= bf16_hi(pk[b][t][j]);
           }
           pk[b][TERMS - 1][j] = pack_bf16(x, y);
-          if constexpr (TERMS == 1) psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[b][0][j]), bf16x2{(__bf16)1.0f, (__bf16)1.0f}, psum, false);
         }
         l_run[b] = __builtin_fmaf(psum, inv_rest, l_run[b]);
       }
