@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 
 import torch
 
@@ -215,8 +215,15 @@ def _cache_arg(cache):
     return _pack_cache(k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], cache.kv_len.data_ptr(), b, cap)
 
 
+class _Handle:
+    """A handle is made from its tensors whenever it is copied or loaded: `packed` holds addresses, which no other tensors have."""
+
+    def __reduce__(self):
+        return type(self), tuple(getattr(self, f.name) for f in fields(self))
+
+
 @dataclass(frozen=True)
-class PageTable:
+class PageTable(_Handle):
     """Which pages the sequences of a batch have, for all layers: table int32 [B, table_pages], kv_len int32 [B], and the free
     pages, free_pages int32 [n_pages] (entries 0 .. n_free - 1) and n_free int32 [1].  A handle: its tensors are checked and their
     addresses taken when it is made (which costs as much as the launch of a small call)."""
@@ -244,7 +251,7 @@ class PageTable:
 
 
 @dataclass(frozen=True)
-class PagedKV:
+class PagedKV(_Handle):
     """One layer's pool of pages: k, v [n_pages, Hkv, 64, D] e4m3 codes (torch.float8_e4m3fn or uint8; any strides of multiples of
     16 with D contiguous), k_scale, v_scale fp32 [n_pages, Hkv].  Plain device memory; all reads and writes happen in the library.
     A handle, as PageTable."""
