@@ -263,7 +263,8 @@ class PagedKV(_Handle):
     def __post_init__(self):
         k, v = self.k, self.v
         strides, (n, h, tokens, _) = k.stride(), k.shape
-        assert tokens == PAGE_TOKENS and strides == v.stride() and strides[3] == 1 and k.element_size() == v.element_size() == 1 and v.shape == k.shape
+        assert tokens == PAGE_TOKENS and strides == v.stride() and strides[3] == 1 and v.shape == k.shape
+        assert all(x.dtype in (torch.float8_e4m3fn, torch.uint8) for x in (k, v))   # (other types of one byte have other codes)
         for s in (self.k_scale, self.v_scale):
             assert s.shape == (n, h) and s.is_contiguous() and s.dtype == torch.float32
         object.__setattr__(self, "packed", _pack_paged_kv(k.data_ptr(), v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),

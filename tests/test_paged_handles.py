@@ -37,3 +37,14 @@ def test_a_copy_holds_the_addresses_of_its_own_tensors(F, how, which):
     assert type(c) is type(h) and c.packed == made_anew(F, c).packed
     first = dataclasses.fields(h)[0].name
     assert (getattr(c, first).data_ptr() == getattr(h, first).data_ptr()) == (how is copy.copy) == (c.packed == h.packed)
+
+
+@pytest.mark.parametrize("dtype", [d for d in ("float8_e4m3fnuz", "float8_e5m2", "float8_e5m2fnuz", "int8", "bool") if hasattr(torch, d)])
+def test_codes_of_another_type_are_refused(F, dtype):
+    """Types of one byte whose codes stand for other values: read as e4m3 they would give wrong results without a word."""
+    good = F.PagedKV.empty(3, 2, 64, device="cpu")
+    k = torch.zeros(3, 2, 64, 64, dtype=torch.uint8).view(getattr(torch, dtype))
+    for pair in ((k, k.clone()), (good.k, k), (k, good.v)):
+        with pytest.raises(AssertionError):
+            F.PagedKV(*pair, good.k_scale, good.v_scale)
+    F.PagedKV(good.k, good.v.view(torch.uint8), good.k_scale, good.v_scale)
