@@ -30,6 +30,8 @@ def saved(h):
 @pytest.mark.parametrize("which", ["pages", "pool", "strided pool"])
 def test_a_copy_holds_the_addresses_of_its_own_tensors(F, how, which):
     h = F.PageTable.empty(2, 3, 5, device="cpu") if which == "pages" else F.PagedKV.empty(3, 2, 64, device="cpu")
+    if how is not copy.copy and which == "pool":             # (torch pickles tensors of uint8, but none of float8)
+        h = F.PagedKV(h.k.view(torch.uint8), h.v.view(torch.uint8), h.k_scale, h.v_scale)
     if which == "strided pool":
         wide = torch.zeros(3, 2, 64, 112, dtype=torch.uint8)
         h = F.PagedKV(wide[..., 16:80], wide.clone()[..., 16:80], h.k_scale, h.v_scale)
