@@ -136,8 +136,8 @@ int flux_kv_append(flux_ctx* ctx, const flux_kv_cache* cache, int n_kv_heads, in
  * longer prompt and a whole prompt are the same call).  mode dev uint8 [batch].
  * out dev [T, n_q_heads, head_dim] in cfg->out_dtype.  max_q_len, max_kv_len: host upper bounds
  * on n_q(b) and kv_len[b] (they size the launch; larger than needed is valid, smaller truncates
- * nothing: rows beyond max_q_len are not computed; a bound far above the real lengths costs empty
- * workgroups, and max_q_len from 32768 on (or from 16384 on with max_kv_len from 32768 on) selects
+ * nothing: of rows beyond max_q_len only such are computed as share a tile of 64 or 128 with rows within it; a bound far above the
+ * real lengths costs empty workgroups, and max_q_len from 32768 on (or from 16384 on with max_kv_len from 32768 on) selects
  * the launch shape tuned for long prompts).  All launch shapes give the same results bit for bit, with one exception:
  * where max_kv_len > max_q_len (queries behind a cached context), the batch has at most 64 sequences, the launch is not of
  * the long shape, and the queries alone would not fill the chip, the keys of a tile of query rows may be shared out over
@@ -145,7 +145,8 @@ int flux_kv_append(flux_ctx* ctx, const flux_kv_cache* cache, int n_kv_heads, in
  * for partial results in the workspace (lists of up to 1024 keys never are); the sums are then taken in another order
  * than in one walk.  SA tiles that the mask hides are skipped,
  * not masked: their K/V rows are never read.  A 64-key tile that is partly visible is read whole
- * (up to kv_len[b]), so the cached rows below kv_len[b] must hold finite values.  If the device finds n_q(b) > kv_len[b]
+ * (up to kv_len[b]), so the cached rows below kv_len[b] must hold finite values; those of V up to 2^64 in magnitude (rows are summed
+ * with weights of up to 2^32 before they are divided by the weights' sum).  If the device finds n_q(b) > kv_len[b]
  * (the caller did not append first), only the first
  * kv_len[b] query rows of that sequence are computed and FLUX_DEV_BAD_LENGTH is raised. */
 int flux_attn_prefill(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q,
@@ -343,8 +344,9 @@ int flux_kv_append_paged(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads,
                          const int32_t* slots, int total_new, void* stream);
 
 /* flux_attn_decode over a paged 8-bit cache: one query per sequence at position kv_len[b] - 1, mode bytes, SA rule, outputs and
- * determinism as there; keys and values are code * scale (any finite scale >= 0;
- * one of V below 2^-126 counts as that).  max_kv_len: host upper bound on kv_len[b],
+ * determinism as there; keys and values are code * scale (any finite scale >= 0; one of V below 2^-126 counts as that; values of V up to
+ * 2^64 in magnitude: rows are summed with weights of up to 2^32 before they are divided by the weights' sum, and a longer list of larger
+ * values may pass the range of fp32).  Weights are held to 2^-16, for fp32 outputs to 2^-24.  max_kv_len: host upper bound on kv_len[b],
  * at most 64 * table_pages (which is always valid); pages of a longer list are left out, the oldest kept, and FLUX_DEV_BAD_LENGTH
  * is raised.  Where all sequences are SA, 64 * (ceil(n_sink / 64) + ceil(window / 64) + 1) is enough (n_sink and window rounded
  * up to multiples of sa_block).  The workspace that flux_workspace_needed names for these arguments is enough.
@@ -357,14 +359,17 @@ int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* 
                            const flux_page_table* pt, const uint8_t* mode, void* out, void* stream);
 
 /* flux_attn_prefill over a paged 8-bit cache: q, cu_q, max_q_len, max_kv_len, mode, out as there (the queries of sequence b are the
- * last n_q(b) positions of its pages: flux_page_plan and flux_kv_append_paged first); keys and values are code * scale (any
- * finite scale >= 0; one of V below 2^-126 counts as that; scores as in flux_attn_decode_paged).  A tile of query rows holds all heads
- * of a group, token by token, and walks only pages of which a row sees something; pages of a tile may be shared out over several
- * workgroups where max_kv_len >= 1024, as far as the workspace has room for their results (any context will do), in a way that
- * depends on the bounds, lengths and modes of the whole batch.  Where max_q_len * group <= 32 the rows of a sequence are worked on
- * like a decode call's.  kv_len[b] above max_kv_len raises FLUX_DEV_BAD_LENGTH (the oldest pages may be all that such a sequence is
- * computed from).  max_q_len * group <= 2^30, and
- * batch * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^22 is always enough (FLUX_EINVAL).
+ * last n_q(b) positions of its pages: flux_page_plan and flux_kv_append_paged first); keys and values are code * scale (scales,
+ * values and scores as in flux_attn_decode_paged).  Query rows beyond max_q_len are left as they were.
+ * A tile of query rows holds all heads of a group, token by token, and walks only pages of which a row sees something.  Weights are
+ * rounded to bf16 (by 2^-8 of one at most; the denominator sums the rounded ones), whatever out_dtype is, as in flux_attn_prefill.
+ * Pages of a tile may be shared out over several workgroups where the batch has at most 64 sequences and max_kv_len is 961 (16
+ * pages) or more, or 8129 (128 pages) or more where the tiles of max_q_len queries are many, as far as the workspace has room for their
+ * results (any context will do), in a way that depends on the bounds, lengths and modes of the whole batch.
+ * Where max_q_len * group <= 32, the batch has at most 64 sequences, max_kv_len is 449 (eight pages) or more and the workspace has
+ * room (one of 18 MB always has), the rows of a sequence are worked on like a decode call's, and their weights are held as there.
+ * kv_len[b] above max_kv_len raises FLUX_DEV_BAD_LENGTH (the oldest pages may be all that such a sequence is computed from).
+ * max_q_len * group <= 2^30, and batch * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^22 is always enough (FLUX_EINVAL).
  * What lies behind kv_len[b] in a page is never used; the codes of a page of which a row of a tile sees something must not be NaN
  * below that, or rows of the tile that do not see them may become NaN as well.  A table entry outside the pool counts as a page that is
  * not there, and raises FLUX_DEV_BAD_PAGE; rows without any key are zero. */
