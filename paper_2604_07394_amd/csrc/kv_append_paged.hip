@@ -7,7 +7,8 @@
 //
 // One wave per block, K or V: up to 64 rows stay in its registers between the maximum and the rounding, so every row is read once,
 // with up to 16 KB on their way per wave, and nothing passes between waves.
-// What bounds it: the memory for long prompts, latencies (slots, scale, row) for a decode step.
+// What bounds it: the memory for long prompts, latencies (slots, scale, row) for a decode step, and where pages take a larger scale
+// the latencies of their old codes, RPS rows at a time: 64 sequences with a row each, 8 heads of 128, traced with every page so 10.8 us for 4.8.
 #include "paged.h"
 
 namespace flux {
