@@ -18,6 +18,8 @@ CASES = [
     ([2, 2], [900, 3000], 16, 1, 128),
     ([2, 0, 1], [900, 3, 3000], 14, 2, 128),                 # group 7
     ([1] * 5, [500, 64, 63, 2000, 130], 8, 2, 64),           # one query each
+    ([1, 0, 1], [3000, 5, 600], 40, 2, 128),                 # groups of 20 and 32: the heads of one query take two blocks
+    ([1], [900], 32, 1, 64),
 ]
 
 
