@@ -290,7 +290,8 @@ int flux_attn_decode_ring(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q
 
 /* Which pages the sequences have, and which are free.  Page `table[b * table_pages + i]` holds positions 64 i .. 64 i + 63 of
  * sequence b; a sequence has ceil(kv_len[b] / 64) pages, and table entries behind them are not read.  A page may stand in the
- * tables of several sequences (a shared prefix) as long as nobody appends to it or releases it. */
+ * tables of several sequences (a shared prefix) as long as nobody appends to it or releases it: flux_page_fork counts who has a
+ * page, and keeps that so. */
 typedef struct {
   int32_t* table;           /* dev int32 [batch, table_pages] */
   int32_t* kv_len;          /* dev int32 [batch]: valid positions per sequence */
@@ -376,6 +377,101 @@ int flux_attn_decode_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* 
 int flux_attn_prefill_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q, int max_q_len,
                             int max_kv_len, const flux_paged_kv* kv, const flux_page_table* pt, const uint8_t* mode,
                             void* out, void* stream);
+
+/* ---- Heads on their way from the projection to the attention: norms and position rotation of queries and keys.
+ *
+ * For a head row x of head_dim values (D):
+ *   y = x / sqrt(mean(x^2) + eps) * w     (w: q_norm or k_norm, one weight per dimension, the same for all heads; NULL: y = x)
+ *   of the first rotary_dim dimensions (R) of y, pair i < R/2 with t = position * inv_freq[i] (radians, in real numbers):
+ *     (a, b) -> (a cos t - b sin t, b cos t + a sin t),  a, b = dimensions i and i + R/2, or 2i and 2i + 1 where interleaved is 1.
+ * Everything between is held in fp32 (angles in 64 bits until whole turns are taken off; keys that go into pages of 8-bit codes wholly in 64 bits), and rounded once, to
+ * nearest even.  Positions are any int32 numbers. */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128 */
+  int32_t rotary_dim;       /* a multiple of 16, at most head_dim; 0: no rotation */
+  int32_t interleaved;      /* 0 or 1 */
+  float eps;                /* 1e-30 or more where there is a norm */
+  const void* q_norm;       /* dev bf16 [head_dim], 16-byte aligned, or NULL */
+  const void* k_norm;       /* the same */
+  const float* inv_freq;    /* dev fp32 [rotary_dim / 2], 16-byte aligned (rotary_dim 0: not used) */
+} flux_head_cfg;
+
+/* Rows of the projection: head h of token row t of q is q[t*stride_q + h*head_dim ..], the same for k and v (one buffer that holds
+ * all three side by side is three pointers into it).  dev bf16, 16-byte aligned; strides in elements, multiples of 8, at
+ * least a row of heads. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t stride_q, stride_k, stride_v;
+} flux_qkv_rows;
+
+/* Queries and keys of `total` token rows: q_out dev bf16 [total, n_q_heads, head_dim], k_out dev bf16 [total, n_kv_heads, head_dim],
+ * either NULL together with its input (v is not used).  positions: dev int32 [total] (rotary_dim 0: not used).  An output may be its
+ * input where that has no gaps (stride = heads * head_dim); otherwise they must not overlap.  total <= 2^30. */
+int flux_qk_norm_rope(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_qkv_rows* in, const int32_t* positions, int total,
+                      void* q_out, void* k_out, void* stream);
+
+/* flux_qk_norm_rope and flux_kv_append in one pass: queries go to q_out (NULL together with in->q: keys and values alone), finished
+ * keys and the values as they are to the tail of each sequence's cache; cu_new, total_new, max_new, lengths, FLUX_ECAPACITY and
+ * FLUX_DEV_KV_OVERFLOW as in flux_kv_append.  positions: dev int32 [total_new], or NULL: row r of sequence b is at kv_len[b] + r, the
+ * place that it goes to.  Rows of no sequence (before cu_new[0], from cu_new[batch] on) are left out, and q_out there is left as it was. */
+int flux_qkv_append(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_kv_cache* cache, const flux_qkv_rows* in,
+                    const int32_t* cu_new, int total_new, int max_new, const int32_t* positions, void* q_out, void* stream);
+
+/* flux_qk_norm_rope and flux_kv_append_paged in one pass: queries go to q_out (or both NULL), keys and values are quantised into their
+ * slots; slots, scales, limits and FLUX_DEV_BAD_PAGE as in flux_kv_append_paged.  A key's code is rounded once, from the value that the
+ * formula names.  positions: dev int32 [total_new] (rotary_dim 0: not used).  Every row of q_out is written, whatever its slot is. */
+int flux_qkv_append_paged(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_paged_kv* kv, const flux_qkv_rows* in,
+                          const int32_t* slots, const int32_t* positions, int total_new, void* q_out, void* stream);
+
+/* ---- Pages that change hands.  `shares` (dev int32 [n_pages], the same for all layers) holds for every page how many rows of the table have it,
+ * less one; 0 for a free page.  It begins as zeros; flux_page_plan and flux_page_release need not know it, as the pages that they give
+ * and take have one holder.  A sequence that may hold shared pages gives them back through flux_page_fork. */
+
+/* Sequence b goes on with the first n(b) = min(keep_len[b], kv_len[parent[b]]) positions of what sequence parent[b] holds now (dev int32 [batch]
+ * each; parent NULL: b itself; parent[b] = -1: nothing, the request is done; keep_len NULL: all of them; below 0 counts as 0): beams that are
+ * replaced, samples that begin as copies, prompts that requests share, finished requests and rejected tokens.  Row b of the table becomes the
+ * first ceil(n(b) / 64) entries of row parent[b] as it was, places that it had behind them become -1, kv_len[b] = n(b), and shares is brought up to date.
+ *   Pages that no row has any longer go back: they are listed behind the free pages, the one with the highest number first, so that the lowest is taken first.
+ *   A last page that is partly filled (n(b) % 64 != 0) is appended to next, so nobody else may have it: of the sequences that have a page partly
+ *   filled the first one keeps it if none has all of it filled; the others get a page each, in the order of the sequences, the j-th of them
+ *   free_pages[n_free - 1 - j] (after those that went back were listed), and copies[j] = {page, its copy, n(b) % 64} (dev int32 [batch, 3]); *n_copies
+ *   (dev int32) is their number, and entries behind them are left as they were.  flux_page_copy then copies them in each layer, before
+ *   anything is appended.  Where the free pages do not suffice, such a sequence is cut to whole pages and FLUX_DEV_KV_OVERFLOW is raised.
+ * Limits as in flux_page_release.  The partials of the workspace hold 4 bytes per page (FLUX_EWORKSPACE).  Parents outside the batch count as -1 and lengths
+ * outside the table are cut (FLUX_DEV_BAD_LENGTH); table entries outside the pool are not counted, are given on as -1 and raise FLUX_DEV_BAD_PAGE,
+ * as does a page that more rows lost than had it by `shares` (it goes back all the same). */
+int flux_page_fork(flux_ctx* ctx, const flux_page_table* pt, int32_t* shares, const int32_t* parent, const int32_t* keep_len,
+                   int32_t* copies, int32_t* n_copies, void* stream);
+
+/* Close the holes of the pool: as long as the lowest free page lies below the highest page in use (one that is not listed as free), the latter moves to
+ * the former, at most max_moves times.  moves[j] = {from, to, 64} (dev int32 [max_moves, 3]), *n_moves (dev int32) their number, entries behind
+ * them left as they were.  Tables and shares (NULL: nobody shares pages) follow; the free pages are listed again, the highest number first, so that
+ * the lowest is taken first.  flux_page_copy then moves the codes in each layer (no page is both moved from and to), before the next attention or append call.  After a call with
+ * enough moves the pages in use are 0 .. n_pages - n_free - 1.  n_pages <= 2^20, batch <= FLUX_MAX_PAGED_BATCH; the partials of the workspace hold 4 bytes per page
+ * (FLUX_EWORKSPACE).  Numbers in the list outside the pool, or listed twice, are dropped from it and raise FLUX_DEV_BAD_PAGE, as do table entries outside the
+ * pool (left as they were). */
+int flux_page_compact(flux_ctx* ctx, const flux_page_table* pt, int32_t* shares, int32_t* moves, int max_moves, int32_t* n_moves,
+                      void* stream);
+
+/* Copy pages within one layer's pool: for each entry {from, to, rows} of `copies` (dev int32 [max_copies, 3]) before *n_copies (dev int32; NULL:
+ * all of them) the codes of the first `rows` positions (0 .. 64, cut to that) and the scales of all heads.  Entries {-1, -1, ..} are left out; other numbers
+ * outside the pool raise FLUX_DEV_BAD_PAGE.  A page that is copied to must stand in no other entry. */
+int flux_page_copy(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int head_dim, const int32_t* copies,
+                   const int32_t* n_copies, int max_copies, void* stream);
+
+/* ---- Cross attention: every query row of sequence b sees all kv_len[b] keys of its cache (the states of an encoder, written by flux_kv_append or
+ * flux_qkv_append), whatever the number of queries.  q dev bf16 [T, n_q_heads, head_dim], rows of sequence b are cu_q[b] .. cu_q[b+1]-1
+ * (dev int32 [batch+1]); cu_q NULL: max_q_len rows each, one sequence behind the other.  out dev [T, n_q_heads, head_dim] in cfg->out_dtype; cfg->n_sink, window and
+ * sa_block are not used.  max_q_len, max_kv_len: host upper bounds (rows and keys beyond them are left out and raise FLUX_DEV_BAD_LENGTH; looser ones cost idle
+ * workgroups).  Rows without any key are zero; rows of no sequence are left as they were.  With cu_q NULL and max_q_len 1 (a decode step) the
+ * call is worked on like flux_attn_decode and needs the workspace that flux_workspace_needed names; any other call takes what there is.
+ * Weights are rounded to bf16 as in flux_attn_prefill (a decode step: as in flux_attn_decode), cached rows below kv_len[b] must be finite, those of V up to 2^64.
+ * Keys of a tile of rows may be shared out over workgroups, in a way that depends on the bounds and lengths of up to 64 sequences side by side.
+ * batch * max_q_len < 2^31 where cu_q is NULL; 64 * n_kv_heads * ceil(max_q_len * group / 64) <= 2^28 (FLUX_EINVAL). */
+int flux_attn_cross(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
+                    const flux_kv_cache* cache, void* out, void* stream);
 
 #ifdef __cplusplus
 }

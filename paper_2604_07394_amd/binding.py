@@ -30,7 +30,8 @@ EXPORTS = ["flux_create", "flux_destroy", "flux_strerror", "flux_workspace_neede
            "flux_kv_append_ring", "flux_kv_compact_ring", "flux_attn_decode_ring", "flux_attn_decode_static",
            "flux_attn_prefill_blocksparse", "flux_xa_select", "flux_attn_decode_append",
            "flux_page_plan", "flux_page_release", "flux_kv_append_paged", "flux_attn_decode_paged",
-           "flux_attn_prefill_paged"]
+           "flux_attn_prefill_paged", "flux_qk_norm_rope", "flux_qkv_append", "flux_qkv_append_paged",
+           "flux_page_fork", "flux_page_compact", "flux_page_copy", "flux_attn_cross"]
 PAGE_TOKENS, MAX_PAGED_BATCH = 64, 4096
 STATIC_SCRATCH_BYTES = 16 * 1024 * 1024 + 256
 
@@ -57,6 +58,17 @@ class FluxPagedKV(C.Structure):
                 ("stride_p", C.c_int64), ("stride_h", C.c_int64), ("stride_t", C.c_int64), ("n_pages", C.c_int32)]
 
 
+class FluxHeadCfg(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("eps", C.c_float), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("inv_freq", C.c_void_p)]
+
+
+class FluxQKVRows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("stride_q", C.c_int64), ("stride_k", C.c_int64), ("stride_v", C.c_int64)]
+
+
+_pack_rows = struct.Struct("@PPPqqq").pack                   # the bytes of a FluxQKVRows
 _pack_cache = struct.Struct("@PPqqqPii").pack                # the bytes of a FluxKVCache
 assert struct.calcsize("@PPqqqPii") == C.sizeof(FluxKVCache)
 _pack_pages, _pack_paged_kv = struct.Struct("@PPPPiii0P").pack, struct.Struct("@PPPPqqqi0q").pack
@@ -120,6 +132,21 @@ _lib.flux_attn_decode_paged.restype = C.c_int
 _lib.flux_attn_prefill_paged.argtypes = [C.c_void_p, C.POINTER(FluxAttnCfg), C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
 _lib.flux_attn_prefill_paged.restype = C.c_int
+
+_lib.flux_qk_norm_rope.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.flux_qk_norm_rope.restype = C.c_int
+_lib.flux_qkv_append.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.flux_qkv_append.restype = C.c_int
+_lib.flux_qkv_append_paged.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
+_lib.flux_qkv_append_paged.restype = C.c_int
+_lib.flux_page_fork.argtypes = [C.c_void_p] * 8
+_lib.flux_page_fork.restype = C.c_int
+_lib.flux_page_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
+_lib.flux_page_compact.restype = C.c_int
+_lib.flux_page_copy.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p]
+_lib.flux_page_copy.restype = C.c_int
+_lib.flux_attn_cross.argtypes = [C.c_void_p, C.POINTER(FluxAttnCfg), C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.flux_attn_cross.restype = C.c_int
 
 
 class FluxError(RuntimeError):
@@ -361,3 +388,86 @@ def flux_attn_decode_paged(ctx, cfg, q, max_kv_len, kv, pt, mode, out, stream=No
 def flux_attn_prefill_paged(ctx, cfg, q, cu_q, max_q_len, max_kv_len, kv, pt, mode, out, stream=None) -> None:
     _check(_lib.flux_attn_prefill_paged(ctx, C.byref(cfg), _ptr(q), _ptr(cu_q), max_q_len, max_kv_len, _handle_arg(kv), _handle_arg(pt),
                                         _ptr(mode), _ptr(out), _stream(stream)))
+
+
+@dataclass(frozen=True)
+class HeadCfg(_Handle):
+    """How the query and key heads of a layer are normed and turned (flux_head_cfg): q_norm, k_norm bf16 [head_dim] or None, inv_freq fp32
+    [rotary_dim / 2] or None.  A handle, as PageTable."""
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    q_norm: torch.Tensor | None
+    k_norm: torch.Tensor | None
+    eps: float
+    inv_freq: torch.Tensor | None
+    rotary_dim: int
+    interleaved: int
+
+    def __post_init__(self):
+        for w in (self.q_norm, self.k_norm):
+            assert w is None or (w.dtype == torch.bfloat16 and w.shape == (self.head_dim,) and w.is_contiguous())
+        f = self.inv_freq
+        assert f is None or (f.dtype == torch.float32 and f.shape == (self.rotary_dim // 2,) and f.is_contiguous())
+        object.__setattr__(self, "packed", bytes(FluxHeadCfg(self.n_q_heads, self.n_kv_heads, self.head_dim, self.rotary_dim, self.interleaved, self.eps,
+                                                             _ptr(self.q_norm), _ptr(self.k_norm), _ptr(f))))
+
+
+def head_cfg(n_q_heads, n_kv_heads, head_dim, q_norm=None, k_norm=None, eps=1e-6, inv_freq=None, rotary_dim=None, interleaved=0) -> HeadCfg:
+    """rotary_dim None: what inv_freq says (no inv_freq: no rotation)."""
+    if rotary_dim is None:
+        rotary_dim = 0 if inv_freq is None else 2 * inv_freq.numel()
+    return HeadCfg(n_q_heads, n_kv_heads, head_dim, q_norm, k_norm, eps, inv_freq, rotary_dim, interleaved)
+
+
+def _head_arg(hc):
+    return hc.packed if type(hc) is HeadCfg else C.byref(hc)
+
+
+def _rows_arg(q, k, v):
+    """The bytes of a FluxQKVRows: tensors [T, heads, head_dim] whose heads lie next to each other, any stride between tokens."""
+    at, strides = [], []
+    for x in (q, k, v):
+        if x is None:
+            at.append(0)
+            strides.append(0)
+            continue
+        s = x.stride()
+        assert x.dtype == torch.bfloat16 and s[2] == 1 and (s[1] == x.shape[2] or x.shape[1] == 1)
+        at.append(x.data_ptr())
+        strides.append(s[0] if x.shape[0] > 1 else x.shape[1] * x.shape[2])              # (of a single row torch may say anything)
+    return _pack_rows(*at, *strides)
+
+
+def flux_qk_norm_rope(ctx, hc, q, k, positions, total, q_out, k_out, stream=None) -> None:
+    _check(_lib.flux_qk_norm_rope(ctx, _head_arg(hc), _rows_arg(q, k, None), _ptr(positions), total, _ptr(q_out), _ptr(k_out), _stream(stream)))
+
+
+def flux_qkv_append(ctx, hc, cache, q, k, v, cu_new, total_new, max_new, positions, q_out, stream=None) -> None:
+    _check(_lib.flux_qkv_append(ctx, _head_arg(hc), _cache_arg(cache), _rows_arg(q, k, v), _ptr(cu_new), total_new, max_new, _ptr(positions),
+                                _ptr(q_out), _stream(stream)))
+
+
+def flux_qkv_append_paged(ctx, hc, kv, q, k, v, slots, positions, total_new, q_out, stream=None) -> None:
+    _check(_lib.flux_qkv_append_paged(ctx, _head_arg(hc), _handle_arg(kv), _rows_arg(q, k, v), _ptr(slots), _ptr(positions), total_new, _ptr(q_out),
+                                      _stream(stream)))
+
+
+def flux_page_fork(ctx, pt, shares, parent, keep_len, copies, n_copies, stream=None) -> None:
+    _check(_lib.flux_page_fork(ctx, _handle_arg(pt), _ptr(shares), _ptr(parent), _ptr(keep_len), _ptr(copies), _ptr(n_copies), _stream(stream)))
+
+
+def flux_page_compact(ctx, pt, shares, moves, n_moves, max_moves=None, stream=None) -> None:
+    """max_moves None: as many as `moves` [n, 3] has room for."""
+    _check(_lib.flux_page_compact(ctx, _handle_arg(pt), _ptr(shares), _ptr(moves), moves.shape[0] if max_moves is None else max_moves, _ptr(n_moves),
+                                  _stream(stream)))
+
+
+def flux_page_copy(ctx, kv, n_kv_heads, head_dim, copies, n_copies, max_copies=None, stream=None) -> None:
+    """max_copies None: as many as `copies` [n, 3] has."""
+    _check(_lib.flux_page_copy(ctx, _handle_arg(kv), n_kv_heads, head_dim, _ptr(copies), _ptr(n_copies),
+                               copies.shape[0] if max_copies is None else max_copies, _stream(stream)))
+
+
+def flux_attn_cross(ctx, cfg, q, cu_q, max_q_len, max_kv_len, cache, out, stream=None) -> None:
+    _check(_lib.flux_attn_cross(ctx, C.byref(cfg), _ptr(q), _ptr(cu_q), max_q_len, max_kv_len, _cache_arg(cache), _ptr(out), _stream(stream)))

@@ -16,10 +16,10 @@ COMMON = ["hipcc", "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 
 FLUX_SOURCES = ["flux_api.hip", "kv_append.hip", "decode.hip", "prefill.hip", "router.hip", "xa_select.hip", "pages.hip", "kv_append_paged.hip",
-                "decode_paged.hip", "prefill_paged.hip"]
+                "decode_paged.hip", "prefill_paged.hip", "heads.hip", "page_moves.hip", "cross.hip"]
 # Regions whose branches are the same for all lanes are left as they are written: the compiler structurises them by default, and
 # the loops of the prefill kernels then take up to seven branches per block and hold 20 registers more.
-SOURCE_FLAGS = {"prefill_paged.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"], "prefill.hip": ["-mllvm", "-structurizecfg-skip-uniform-regions=true"]}
+SOURCE_FLAGS = {name: ["-mllvm", "-structurizecfg-skip-uniform-regions=true"] for name in ("prefill_paged.hip", "prefill.hip", "cross.hip")}
 
 
 def _run(cmd):

@@ -8,7 +8,9 @@
 #include <mutex>
 #include <new>
 
-#include "paged.h"
+#include "cross.h"
+#include "heads.h"
+#include "page_moves.h"
 
 using namespace flux;
 
@@ -108,6 +110,29 @@ int check_paged_attention(const flux_attn_cfg* cfg, const void* q, int max_kv_le
   if (pt->n_pages > kv->n_pages || max_kv_len < 0) return FLUX_EINVAL;
   if (max_kv_len > pt->table_pages * kPageTokens) return FLUX_ECAPACITY;
   return aligned16(q) && aligned16(out) ? FLUX_OK : FLUX_EINVAL;
+}
+
+bool bad_row_stride(int64_t stride, int heads, int head_dim) { return stride < (int64_t)heads * head_dim || (stride & 7); }
+
+// What the calls that norm and turn heads share: `positions` and the rows of queries (with q_out) and keys, as far as they are given.
+int check_heads(const flux_head_cfg* cfg, const flux_qkv_rows* in, const void* q_out, const void* positions, int total) {
+  if (!cfg || !in || total < 0 || total > (1 << 30)) return FLUX_EINVAL;
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) return FLUX_EINVAL;
+  if (cfg->n_q_heads <= 0 || cfg->n_kv_heads <= 0 || cfg->n_q_heads > (1 << 20) || cfg->n_kv_heads > (1 << 20)) return FLUX_EINVAL;
+  if (cfg->rotary_dim < 0 || cfg->rotary_dim > cfg->head_dim || (cfg->rotary_dim & 15)) return FLUX_EINVAL;
+  if (cfg->interleaved != 0 && cfg->interleaved != 1) return FLUX_EINVAL;
+  if ((cfg->q_norm || cfg->k_norm) && (!(cfg->eps >= 1e-30f) || isinf(cfg->eps))) return FLUX_EINVAL;
+  if (!aligned16(cfg->q_norm) || !aligned16(cfg->k_norm)) return FLUX_EINVAL;
+  if (cfg->rotary_dim > 0 && (!cfg->inv_freq || !aligned16(cfg->inv_freq) || !positions)) return FLUX_EINVAL;
+  if (!in->q != !q_out) return FLUX_EINVAL;
+  if (in->q && (!aligned16(in->q) || !aligned16(q_out) || bad_row_stride(in->stride_q, cfg->n_q_heads, cfg->head_dim))) return FLUX_EINVAL;
+  if (in->q == q_out && in->q && in->stride_q != (int64_t)cfg->n_q_heads * cfg->head_dim) return FLUX_EINVAL;
+  if (in->k && (!aligned16(in->k) || bad_row_stride(in->stride_k, cfg->n_kv_heads, cfg->head_dim))) return FLUX_EINVAL;
+  return FLUX_OK;
+}
+int check_values(const flux_head_cfg* cfg, const flux_qkv_rows* in) {
+  if (!in->k || !in->v || !aligned16(in->v) || bad_row_stride(in->stride_v, cfg->n_kv_heads, cfg->head_dim)) return FLUX_EINVAL;
+  return FLUX_OK;
 }
 
 }  // namespace
@@ -489,6 +514,127 @@ int flux_attn_prefill_paged(flux_ctx* ctx, const flux_attn_cfg* cfg, const void*
   if (p.wgs > kAppendMost) return FLUX_EINVAL;
   if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
   const hipError_t e = launch_prefill_paged(ctx->c, *cfg, q, cu_q, max_q_len, max_kv_len, *kv, *pt, mode, out, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+// ---- heads of new tokens
+
+int flux_qk_norm_rope(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_qkv_rows* in, const int32_t* positions, int total, void* q_out,
+                      void* k_out, void* stream) {
+  if (!ctx) return FLUX_EINVAL;
+  const int rc = check_heads(cfg, in, q_out, positions, total);
+  if (rc != FLUX_OK) return rc;
+  if (!in->k != !k_out || (!in->q && !in->k)) return FLUX_EINVAL;
+  if (!aligned16(k_out)) return FLUX_EINVAL;
+  if (in->k && in->k == k_out && in->stride_k != (int64_t)cfg->n_kv_heads * cfg->head_dim) return FLUX_EINVAL;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  if (total == 0) return FLUX_OK;
+  const HeadRows r = {*cfg, *in, positions, total, q_out};
+  const hipError_t e = launch_head_rows(r, k_out, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+int flux_qkv_append(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_kv_cache* cache, const flux_qkv_rows* in, const int32_t* cu_new,
+                    int total_new, int max_new, const int32_t* positions, void* q_out, void* stream) {
+  if (!ctx || !cu_new) return FLUX_EINVAL;
+  int rc = check_heads(cfg, in, q_out, cu_new, total_new);   // (positions may be NULL: they follow from the lengths)
+  if (rc != FLUX_OK) return rc;
+  rc = check_values(cfg, in);
+  if (rc != FLUX_OK) return rc;
+  if (max_new < 0 || max_new > total_new) return FLUX_EINVAL;
+  rc = check_cache(cache, cfg->head_dim);
+  if (rc != FLUX_OK) return rc;
+  if (max_new > cache->capacity) return FLUX_ECAPACITY;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  if (total_new == 0) return FLUX_OK;
+  const HeadRows r = {*cfg, *in, positions, total_new, q_out};
+  const hipError_t e = launch_qkv_append(ctx->c, r, *cache, cu_new, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+int flux_qkv_append_paged(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_paged_kv* kv, const flux_qkv_rows* in, const int32_t* slots,
+                          const int32_t* positions, int total_new, void* q_out, void* stream) {
+  if (!ctx || !slots) return FLUX_EINVAL;
+  int rc = check_heads(cfg, in, q_out, positions, total_new);
+  if (rc != FLUX_OK) return rc;
+  rc = check_values(cfg, in);
+  if (rc != FLUX_OK) return rc;
+  if ((total_new / 64 + 1ll) * cfg->n_kv_heads > (1 << 30)) return FLUX_EINVAL;   // (tile of rows, head) pairs are counted in 32 bits
+  rc = check_paged_kv(kv, cfg->head_dim);
+  if (rc != FLUX_OK) return rc;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  if (total_new == 0) return FLUX_OK;
+  const HeadRows r = {*cfg, *in, positions, total_new, q_out};
+  const hipError_t e = launch_qkv_append_paged(ctx->c, r, *kv, slots, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+// ---- pages that change hands
+
+int flux_page_fork(flux_ctx* ctx, const flux_page_table* pt, int32_t* shares, const int32_t* parent, const int32_t* keep_len, int32_t* copies,
+                   int32_t* n_copies, void* stream) {
+  if (!ctx || !shares || !copies || !n_copies) return FLUX_EINVAL;
+  const int rc = check_page_table(pt, true);
+  if (rc != FLUX_OK) return rc;
+  if (ctx->c.device >= 0 && fork_bytes(pt->n_pages) > ctx->c.partials_bytes) return FLUX_EWORKSPACE;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  const hipError_t e = launch_page_fork(ctx->c, *pt, shares, parent, keep_len, copies, n_copies, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+int flux_page_compact(flux_ctx* ctx, const flux_page_table* pt, int32_t* shares, int32_t* moves, int max_moves, int32_t* n_moves, void* stream) {
+  if (!ctx || !moves || !n_moves || max_moves < 1 || max_moves > (1 << 24)) return FLUX_EINVAL;
+  const int rc = check_page_table(pt, true);
+  if (rc != FLUX_OK) return rc;
+  if (pt->n_pages > kCompactPages) return FLUX_EINVAL;
+  if (ctx->c.device >= 0 && compact_bytes(pt->n_pages) > ctx->c.partials_bytes) return FLUX_EWORKSPACE;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  const hipError_t e = launch_page_compact(ctx->c, *pt, shares, moves, max_moves, n_moves, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+int flux_page_copy(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int head_dim, const int32_t* copies, const int32_t* n_copies, int max_copies,
+                   void* stream) {
+  if (!ctx || !copies || max_copies < 0 || max_copies > (1 << 24)) return FLUX_EINVAL;
+  if (head_dim != 64 && head_dim != 128) return FLUX_EINVAL;
+  if (n_kv_heads <= 0) return FLUX_EINVAL;
+  const int rc = check_paged_kv(kv, head_dim);
+  if (rc != FLUX_OK) return rc;
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  if (max_copies == 0) return FLUX_OK;
+  const hipError_t e = launch_page_copy(ctx->c, *kv, n_kv_heads, head_dim, copies, n_copies, max_copies, (hipStream_t)stream);
+  return e == hipSuccess ? FLUX_OK : hip_fail(e);
+}
+
+// ---- cross attention
+
+int flux_attn_cross(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
+                    const flux_kv_cache* cache, void* out, void* stream) {
+  if (!ctx || !q || !out) return FLUX_EINVAL;
+  int rc = check_cfg(cfg);
+  if (rc != FLUX_OK) return rc;
+  rc = check_cache(cache, cfg->head_dim);
+  if (rc != FLUX_OK) return rc;
+  if (max_q_len < 0 || max_kv_len < 0) return FLUX_EINVAL;
+  if (max_kv_len > cache->capacity) return FLUX_ECAPACITY;
+  if (!aligned16(q) || !aligned16(out)) return FLUX_EINVAL;
+  // rows and workgroups are counted in 32 bits
+  const long long rows = (long long)max_q_len * (cfg->n_q_heads / cfg->n_kv_heads);
+  if ((rows + 63) / 64 > (1 << 22) / cfg->n_kv_heads) return FLUX_EINVAL;
+  if (!cu_q && (long long)cache->batch * max_q_len > 0x7FFFFFFFll) return FLUX_EINVAL;
+  if (!cu_q && max_q_len == 1) {
+    // a decode step: a ring of all rows of the cache, which sees all that it holds
+    flux_attn_cfg ring = *cfg;
+    ring.n_sink = ring.sa_block = 0;
+    ring.window = cache->capacity;
+    const DecodePlan p = plan_decode(ring, cache->batch, max_kv_len);
+    if (ctx->c.device >= 0 && decode_partials_bytes(ring, p) > ctx->c.partials_bytes) return FLUX_EWORKSPACE;
+    if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+    const hipError_t e = launch_decode(ctx->c, ring, q, max_kv_len, *cache, nullptr, 1, nullptr, nullptr, out, (hipStream_t)stream);
+    return e == hipSuccess ? FLUX_OK : hip_fail(e);
+  }
+  if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
+  const hipError_t e = launch_cross(ctx->c, *cfg, q, cu_q, max_q_len, max_kv_len, *cache, out, (hipStream_t)stream);
   return e == hipSuccess ? FLUX_OK : hip_fail(e);
 }
 

@@ -1,0 +1,28 @@
+// Launchers of the calls that norm and turn the heads of new tokens (each validates nothing: flux_api.hip has done it).
+#pragma once
+
+#include "paged.h"
+
+namespace flux {
+
+// What a call takes from the projection and how its heads are worked on.
+struct HeadRows {
+  flux_head_cfg cfg;
+  flux_qkv_rows in;
+  const int32_t* positions;   // null: nothing is turned, or (contiguous cache) the places of the rows
+  int total;
+  void* q_out;                // null: no queries
+};
+
+hipError_t launch_head_rows(const HeadRows& r, void* k_out, hipStream_t s);
+hipError_t launch_qkv_append(const Ctx& c, const HeadRows& r, const flux_kv_cache& cache, const int32_t* cu_new, hipStream_t s);
+hipError_t launch_qkv_append_paged(const Ctx& c, const HeadRows& r, const flux_paged_kv& kv, const int32_t* slots, hipStream_t s);
+
+constexpr int kHeadWaves = 8192;            // waves that a launch takes where a token's heads can be shared out over so many
+// Waves that the heads of a token are shared out over, `passes` of 64 lanes in all.
+inline int head_waves(int total, int passes) {
+  const int most = total > 0 ? kHeadWaves / total : 1;
+  return most < 1 ? 1 : (most < passes ? most : passes);
+}
+
+}  // namespace flux

@@ -2,7 +2,9 @@
 // reports that there is no device.  (The real ones live next to their kernels.)  The two calls of the runtime with which the
 // static scratch is looked up are answered here, so that flux_attn_decode_static gets as far as its launcher, which notes
 // what it was given.
-#include "paged.h"
+#include "cross.h"
+#include "heads.h"
+#include "page_moves.h"
 
 extern "C" {
 hipError_t hipGetDevice(int* device) { *device = 0; return hipSuccess; }
@@ -89,5 +91,13 @@ hipError_t launch_decode_paged(const Ctx&, const flux_attn_cfg&, const void*, in
                                const uint8_t*, void*, hipStream_t) { return hipErrorNoDevice; }
 hipError_t launch_prefill_paged(const Ctx&, const flux_attn_cfg&, const void*, const int32_t*, int, int, const flux_paged_kv&,
                                 const flux_page_table&, const uint8_t*, void*, hipStream_t) { return hipErrorNoDevice; }
+
+hipError_t launch_head_rows(const HeadRows&, void*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_qkv_append(const Ctx&, const HeadRows&, const flux_kv_cache&, const int32_t*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_qkv_append_paged(const Ctx&, const HeadRows&, const flux_paged_kv&, const int32_t*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_page_fork(const Ctx&, const flux_page_table&, int32_t*, const int32_t*, const int32_t*, int32_t*, int32_t*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_page_compact(const Ctx&, const flux_page_table&, int32_t*, int32_t*, int, int32_t*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_page_copy(const Ctx&, const flux_paged_kv&, int, int, const int32_t*, const int32_t*, int, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_cross(const Ctx&, const flux_attn_cfg&, const void*, const int32_t*, int, int, const flux_kv_cache&, void*, hipStream_t) { return hipErrorNoDevice; }
 
 }  // namespace flux

@@ -1,0 +1,26 @@
+// Launchers of the calls that hand pages around, move and copy them (each validates nothing: flux_api.hip has done it).
+#pragma once
+
+#include "paged.h"
+
+namespace flux {
+
+constexpr int kForkPages = 4096;            // pages that a workgroup of the fork's second launch looks through
+constexpr int kForkEntries = 16384;         // entries of the table that a workgroup of its first launch holds in LDS
+constexpr int kCompactPages = 1 << 20;      // pages of a pool that one workgroup holds a bit of each of in LDS (128 KB)
+constexpr int kCopyWgs = 8192;              // workgroups that copy at most
+static_assert(kForkEntries >= FLUX_MAX_PAGED_BATCH, "a column of the table fits");
+
+// Bytes of the partials that the calls take: what every workgroup found and how much, or where every page went.
+inline size_t fork_bytes(int n_pages) {
+  const size_t groups = ((size_t)n_pages + kForkPages - 1) / kForkPages;
+  return groups * (kForkPages + 1) * sizeof(int32_t);
+}
+inline size_t compact_bytes(int n_pages) { return ((size_t)n_pages + 1) * sizeof(int32_t); }
+
+hipError_t launch_page_fork(const Ctx& c, const flux_page_table& pt, int32_t* shares, const int32_t* parent, const int32_t* keep, int32_t* copies,
+                            int32_t* n_copies, hipStream_t s);
+hipError_t launch_page_compact(const Ctx& c, const flux_page_table& pt, int32_t* shares, int32_t* moves, int max_moves, int32_t* n_moves, hipStream_t s);
+hipError_t launch_page_copy(const Ctx& c, const flux_paged_kv& kv, int hkv, int d, const int32_t* copies, const int32_t* n_copies, int max_copies, hipStream_t s);
+
+}  // namespace flux
