@@ -6,11 +6,12 @@
 namespace flux {
 
 constexpr int kCrossBatch = 64;             // sequences of a launch: a lane looks after each; longer batches take several launches
-constexpr int kCrossMaxUnits = 2048;        // units that a launch may have beyond one per tile
+constexpr int kCrossMaxUnits = 1024;        // units of a launch whose tiles may be shared out (or one per tile, where those are more)
+constexpr int kCrossRunWgs = 512;           // workgroups of short runs that the chip holds at once
 constexpr int cross_resident(int head_dim) { return 256 * (head_dim == 128 ? 2 : 3); }   // workgroups that the chip holds at once
 
 struct CrossPlan {
-  int bm;                 // rows of a tile
+  int bm;                 // rows of a tile; 16 or 32: short runs, of a tile each
   int tiles;              // of a sequence and KV head, at most
   long long wgs;          // workgroups of a launch
   int part_units;         // units whose rows the workspace holds; 0: tiles are not shared out
@@ -20,16 +21,17 @@ inline CrossPlan plan_cross(const flux_attn_cfg& cfg, int batch, int max_q_len, 
   CrossPlan p;
   const int n = batch < kCrossBatch ? batch : kCrossBatch;
   const long long rows = (long long)max_q_len * (cfg.n_q_heads / cfg.n_kv_heads);
-  p.bm = rows <= 64 ? 64 : 128;
+  p.bm = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   p.tiles = (int)((rows + p.bm - 1) / p.bm);
   const long long tiles = (long long)n * cfg.n_kv_heads * p.tiles;
   p.wgs = tiles + 8 * n;                                     // (the units of a sequence are padded to whole rounds of the XCDs)
   p.part_units = 0;
-  p.info_bytes = ((size_t)tiles * 16 + 255) / 256 * 256;
-  if (max_kv_len > 128 && (long long)cfg.n_kv_heads * p.tiles < 2 * cross_resident(cfg.head_dim) && p.info_bytes <= partials_bytes / 4) {
+  p.info_bytes = (((size_t)tiles + 1) * 16 + 255) / 256 * 256;
+  // (tiles are shared out where all of them run side by side; the longest sequence alone says whether they may)
+  if (max_kv_len > 128 && (long long)cfg.n_kv_heads * p.tiles < cross_resident(cfg.head_dim) && p.info_bytes <= partials_bytes / 4) {
     const size_t fit = (partials_bytes - p.info_bytes) / ((size_t)p.bm * (cfg.head_dim + 2) * sizeof(float));
     p.part_units = (int)(fit < (size_t)kCrossMaxUnits ? fit : (size_t)kCrossMaxUnits);
-    p.wgs += kCrossMaxUnits;
+    if (p.wgs < p.part_units) p.wgs = p.part_units;
   }
   return p;
 }

@@ -31,7 +31,7 @@ struct CrossArgs {
   int out_fp32;
   void* out;
   float *part_o, *part_ml;        // unnormalised rows of a unit [unit][BM][D]; reference and sum of weights [unit][BM][2]
-  i32x4* info;                    // of a tile [batch][hkv][n_tiles]: first unit, step between its units, how many
+  i32x4* info;                    // of a tile [batch][hkv][n_tiles]: first unit, step between its units, how many; before them, whether any has more than one
   uint32_t* status;
 };
 
@@ -43,15 +43,27 @@ struct CrossUnit {
   int q_begin, n_q, len;
 };
 
-// Keys of the tiles of a sequence in parts of at most `chunk` blocks of 64.  Every lane works out one size by a model in units of a
-// block (1.6 us a round of workgroups): the longest part where all run side by side, else their mean and half of the longest for
-// unevenness; starting and ending a workgroup is worth kEnds blocks, and the second launch kJoin.
-constexpr float kEnds = 2.5f, kJoin = 3.0f;
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_inclusive_sum(x), 63); }
+// Largest of the lanes' numbers, none below 0: the moves of wave_inclusive_sum.
+__device__ __forceinline__ int wave_most(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 
+// Keys of the tiles of a sequence in parts of at most so many blocks of 64.  A few sizes are tried on a model in units of a
+// block (of tiles 1.6 us; of short runs 0.6 at head dimension 64 and 1.2 at 128, in which a CU takes its bytes in): the longest part where all run
+// side by side, else their mean and half of the longest for unevenness; starting and ending a workgroup and the second launch are worth
+// some blocks.
 template <int D, int BM>
 __device__ __forceinline__ CrossUnit cross_plan(const CrossArgs& a, int wg, int l) {
-  constexpr int resident = cross_resident(D);
-  CrossUnit u;
+  constexpr int resident = BM <= 32 ? kCrossRunWgs : cross_resident(D);
+  constexpr float kEnds = BM <= 32 ? (D == 64 ? 5.0f : 2.5f) : 2.5f, kJoin = BM <= 32 ? (D == 64 ? 6.0f : 3.0f) : 3.0f;
+  CrossUnit u = {};
   int q_begin = 0, n_q = 0, len = 0, tiles = 0, nb = 0;
   bool bad = false;
   if (l < a.batch) {
@@ -67,34 +79,31 @@ __device__ __forceinline__ CrossUnit cross_plan(const CrossArgs& a, int wg, int 
   if (wg == 0 && threadIdx.x < 64 && bad) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_LENGTH);
   int nc = tiles > 0 ? 1 : 0;
   if (a.part_units > 0) {
-    const int t_all = __builtin_amdgcn_readlane(wave_inclusive_sum(tiles), 63) * a.hkv;
+    const int t_all = wave_total(tiles) * a.hkv;
     if (t_all < resident) {
-      const float work = (float)__builtin_amdgcn_readlane(wave_inclusive_sum(tiles * nb), 63) * (float)a.hkv;
-      const float share = work / (float)resident;
-      const int cand = l == 63 ? 0x3FFFFFFF : max(2, (int)(share * (float)(l + 8) * (1.0f / 16.0f)) + 1);
-      int units = 0, parts = 0;
-      float longest = 0.f;
-      const float inv = 1.0f / (float)cand;
-      for (int j = 0; j < a.batch; ++j) {
-        const int tj = __builtin_amdgcn_readlane(tiles, j) * a.hkv, nbj = __builtin_amdgcn_readlane(nb, j);
-        if (tj == 0) continue;
-        int n = (int)((float)(nbj - 1) * inv);
-        n += (n + 1) * cand <= nbj - 1 ? 1 : (n * cand > nbj - 1 ? -1 : 0);
-        ++n;                                                 // ceil(nbj / cand)
-        units += tj * n;
-        parts += n > 1 ? tj * n : 0;
-        longest = fmaxf(longest, (float)((nbj + n - 1) / n));
-      }
-      float cost = units <= resident ? longest + kEnds : (work + kEnds * (float)units) / (float)resident + 0.5f * longest;
-      if (parts > 0) cost += kJoin + 0.004f * (float)parts;
-      if (units + 8 * a.batch > a.n_wgs || units + 8 * a.batch > a.part_units) cost = parts > 0 ? 1e30f : cost;
-      int best = (__builtin_bit_cast(int, cost) & ~63) | l;  // (positive floats order like their bits)
+      const float work = (float)wave_total(tiles * nb) * (float)a.hkv, share = work / (float)resident;
+      float best = 1e30f;
 #pragma unroll
-      for (int off = 32; off > 0; off >>= 1) best = min(best, __shfl_xor(best, off));
-      const int chunk = __builtin_amdgcn_readlane(cand, __builtin_amdgcn_readfirstlane(best) & 63);
-      nc = tiles > 0 ? (int)(((int64_t)nb + chunk - 1) / chunk) : 0;
+      for (int i = 0; i < 9; ++i) {
+        const float factor[9] = {0.0f, 0.55f, 0.7f, 0.85f, 1.02f, 1.25f, 1.6f, 2.1f, 3.0f};      // (0: nothing is shared out)
+        const int cand = i == 0 ? 0x3FFFFFFF : max(2, (int)(share * factor[i]) + 1);
+        int n = i == 0 ? 0 : (int)((float)(nb - 1) / (float)cand);
+        n += (int64_t)(n + 1) * cand <= nb - 1 ? 1 : (n * cand > nb - 1 && n > 0 ? -1 : 0);
+        ++n;                                                 // ceil(nb / cand)
+        const int units = wave_total(tiles * n) * a.hkv;
+        const float longest = (float)wave_most(tiles > 0 ? (int)((float)nb / (float)n + 0.999f) : 0);
+        float cost = units <= resident ? longest + kEnds : (work + kEnds * (float)units) / (float)resident + 0.5f * longest;
+        if (i > 0) cost += kJoin + 0.004f * (float)units;
+        if (i > 0 && (units + 8 * a.batch > a.n_wgs || units + 8 * a.batch > a.part_units)) cost = 1e30f;
+        if (cost < best) {                                   // (uniform)
+          best = cost;
+          nc = tiles > 0 ? n : 0;
+        }
+      }
     }
   }
+  const bool shared_out = __builtin_amdgcn_ballot_w64(nc > 1) != 0;
+  if (a.part_units > 0 && wg == 0 && threadIdx.x == 0) a.info[-1] = i32x4{shared_out ? 1 : 0, 0, 0, 0};
   // Units of a sequence: one per (KV head, part, tile).  Workgroups go to the 8 XCDs by id mod 8, and the units of one (KV head,
   // part) walk the same rows of K and V: they get ids of one residue, or of 8 / groups residues.
   const int groups = a.hkv * nc;
@@ -103,8 +112,9 @@ __device__ __forceinline__ CrossUnit cross_plan(const CrossArgs& a, int wg, int 
   int units_s = units, idx_s = l, incl = wave_inclusive_sum(units);
   u.b = -1;
   if (wg >= __builtin_amdgcn_readlane(incl, 63)) return u;
-  if (a.batch > 1) {                                         // longest first
-    const int size = nc > 0 ? (nb + nc - 1) / nc : 0, key = (size << 6) | (63 - l);
+  const int size = nc > 0 ? (int)((float)nb / (float)nc) : 0;
+  if (__builtin_amdgcn_ballot_w64(l < a.batch && size != __builtin_amdgcn_readlane(size, 0)) != 0) {   // not all alike: longest first
+    const int key = (size << 6) | (63 - l);
     int rank = 0;
     for (int j = 0; j < a.batch; ++j) rank += __builtin_amdgcn_readlane(key, j) > key ? 1 : 0;
     rank = l < a.batch ? rank : l;
@@ -144,6 +154,22 @@ __device__ __forceinline__ CrossUnit cross_plan(const CrossArgs& a, int wg, int 
   return u;
 }
 
+// The first wave makes the plan for its workgroup: made by all four it takes the SIMDs four times as long (16 sequences, 600
+// workgroups, us of the launch and the plan: 7.4 for 4.7).
+template <int D, int BM>
+__device__ __forceinline__ CrossUnit cross_unit(const CrossArgs& a, int w, int l, CrossUnit* shared) {
+  if (w == 0) {
+    const CrossUnit u = cross_plan<D, BM>(a, blockIdx.x, l);
+    if (l == 0) *shared = u;
+  }
+  __syncthreads();
+  CrossUnit u = *shared;
+  int* words = (int*)&u;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(CrossUnit) / 4); ++i) words[i] = __builtin_amdgcn_readfirstlane(words[i]);
+  return u;
+}
+
 #define FLUX_DMA_ONE(v, p, o) "s_add_u32 m0, %[lds], %[" o "]\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %[" v "], %[" p "]\n\t"
 // The transfers of one wave for a tile of 64 keys, N of K and N of V, 1 KB each, every fourth KB of the stage at byte OFF.
 template <int OFF, int KT, int N>
@@ -174,7 +200,8 @@ __global__ __launch_bounds__(256, 2) void cross_tile_kernel(CrossArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
 
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, g = l >> 4, n = l & 15;
-  const CrossUnit u = cross_plan<D, BM>(a, blockIdx.x, l);
+  __shared__ CrossUnit s_unit;
+  const CrossUnit u = cross_unit<D, BM>(a, w, l, &s_unit);
   if (u.b < 0) return;                                       // (uniform)
   const int64_t n_rows = (int64_t)u.n_q * a.group, row0 = (int64_t)u.tile * BM;
   const int rows = (int)min((int64_t)BM, n_rows - row0);
@@ -432,11 +459,188 @@ __global__ __launch_bounds__(256, 2) void cross_tile_kernel(CrossArgs a) {
   }
 }
 
+// Short runs: the rows of a KV head fit one or two blocks of 16 columns (a decode step of several beams, say), and a call is bound by the
+// bytes of K and V.  The four waves of a workgroup take blocks of 32 keys in turn, K from memory into the MFMA's operand, V through
+// LDS of their own, each block asked for while the one before is worked on, and join their rows in the end.
+template <int D, int QB>
+__global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
+  constexpr int BM = 16 * QB, KC = D / 32, DB = D / 16, CPR = D / 8, ROWB = 2 * D, VL = 32 * CPR / 64;
+  __shared__ __attribute__((aligned(1024))) char smem[4 * 32 * ROWB];              // a block of V per wave; the rows of O in the end
+  __shared__ float s_m[4][BM], s_l[4][BM];
+  static_assert(4 * 32 * ROWB >= 4 * 16 * D * 4, "one block of columns at a time is joined");
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, g = l >> 4, n = l & 15;
+  __shared__ CrossUnit s_unit;
+  const CrossUnit u = cross_unit<D, BM>(a, w, l, &s_unit);
+  if (u.b < 0) return;                                       // (uniform)
+  const int rows = u.n_q * a.group, len = u.len;             // (at most BM)
+  if (a.part_units > 0 && tid == 0 && u.ci == 0) a.info[(int64_t)u.b * a.hkv + u.kvh] = i32x4{u.slot, u.slot_step, u.parts, 0};
+  const int64_t tile_off = ((int64_t)u.q_begin * a.hq + u.kvh * a.group) * D;
+  auto row_off = [&](int x) {
+    const int t = (int)((uint32_t)x / (uint32_t)a.group);
+    return tile_off + ((int64_t)t * a.hq + (x - t * a.group)) * D;
+  };
+  const int blocks = (len + 63) / 64;
+  int k0 = 0, k1 = len;                                      // this unit's keys
+  if (u.parts > 1) {
+    k0 = 64 * (int)((int64_t)u.ci * blocks / u.parts);
+    k1 = min(len, 64 * (int)((int64_t)(u.ci + 1) * blocks / u.parts));
+  }
+  k0 = __builtin_amdgcn_readfirstlane(k0);
+  k1 = __builtin_amdgcn_readfirstlane(k1);
+  const char* kbase = (const char*)(a.k + (int64_t)u.b * a.stride_b + (int64_t)u.kvh * a.stride_h);
+  const char* vbase = (const char*)(a.v + (int64_t)u.b * a.stride_b + (int64_t)u.kvh * a.stride_h);
+  const int pitch = (int)a.stride_t * 2;
+  u32x4 kreg[2][KC], vreg[VL];
+  auto load_block = [&](int j0) __attribute__((always_inline)) {                   // (rows past the last key: that one again)
+    const char *kt = kbase + (int64_t)j0 * pitch, *vt = vbase + (int64_t)j0 * pitch;
+    const int last = k1 - 1 - j0;
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) kreg[sb][kc] = *(const u32x4*)(kt + min(16 * sb + n, last) * pitch + 64 * kc + 16 * g);
+#pragma unroll
+    for (int i = 0; i < VL; ++i) vreg[i] = *(const u32x4*)(vt + min((i * 64 + l) / CPR, last) * pitch + (l % CPR) * 16);
+  };
+  int j0 = k0 + 32 * w;
+  if (j0 < k1) load_block(j0);
+  bf16x8 qf[QB][KC];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const __bf16* qrow = a.q + row_off(min(16 * qb + n, rows - 1));
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc) qf[qb][kc] = *(const bf16x8*)(qrow + 32 * kc + 8 * g);
+  }
+  FLUX_LDS char* const vs = (FLUX_LDS char*)smem + w * 32 * ROWB;
+  // V: units of 32 bytes XOR-swizzled by the row, as in the tiles
+  int v_wr[VL];
+#pragma unroll
+  for (int i = 0; i < VL; ++i) {
+    const int r = (i * 64 + l) / CPR;
+    v_wr[i] = r * ROWB + (((l % CPR) ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) * 16);
+  }
+  const int v_row = 4 * g + (n >> 2), v_xr = D == 128 ? (v_row & 7) : ((v_row >> 1) & 3);
+  int v_rd[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) v_rd[db] = v_row * ROWB + ((db ^ v_xr) * 32) + (n & 3) * 8;
+  float m[QB], sum[QB];
+  f32x4 o[DB][QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    m[qb] = -INFINITY;
+    sum[qb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  while (j0 < k1) {
+#pragma unroll
+    for (int i = 0; i < VL; ++i) *(FLUX_LDS u32x4*)(vs + v_wr[i]) = vreg[i];
+    f32x4 s[2][QB];
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        s[sb][qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kc = 0; kc < KC; ++kc) s[sb][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kreg[sb][kc]), qf[qb][kc], s[sb][qb], 0, 0, 0);
+      }
+    const int left = k1 - j0;
+    j0 += 128;
+    __builtin_amdgcn_sched_barrier(0);
+    if (j0 < k1) load_block(j0);                             // (its registers have been read by now)
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 pf[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      if (left < 32) {
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[sb][qb][i] = 16 * sb + 4 * g + i < left ? s[sb][qb][i] : -INFINITY;
+      }
+      float top = m[qb];
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[sb][qb][i]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      // (a row whose scores are all -inf so far refers to 0)
+      const float ref = top == -INFINITY ? 0.f : top, al = fast_exp2((m[qb] - ref) * a.scale_log2), mneg = -ref * a.scale_log2;
+      m[qb] = top;
+      const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+      uint32_t pk[4];
+      float add = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        pk[t] = pack_bf16(fast_exp2(__builtin_fmaf(s[t >> 1][qb][2 * (t & 1)], a.scale_log2, mneg)), fast_exp2(__builtin_fmaf(s[t >> 1][qb][2 * (t & 1) + 1], a.scale_log2, mneg)));
+        add = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[t]), ones, add, false);
+      }
+      sum[qb] = __builtin_fmaf(sum[qb], al, add);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db][qb] *= al;
+      pf[qb] = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)(vs + v_rd[db]));
+      const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)(vs + v_rd[db] + 16 * ROWB));
+      const bf16x8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qb], o[db][qb], 0, 0, 0);
+    }
+  }
+  // the waves' rows: references and sums first
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    sum[qb] += __shfl_xor(sum[qb], 16);
+    sum[qb] += __shfl_xor(sum[qb], 32);
+    if (g == 0) {
+      s_m[w][16 * qb + n] = m[qb];
+      s_l[w][16 * qb + n] = sum[qb];
+    }
+  }
+  FLUX_LDS float* const so = (FLUX_LDS float*)(FLUX_LDS char*)smem;                // [wave][d / 4][column][4]
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    __syncthreads();                                         // (V, or the columns before, have been read)
+    const float top = fmaxf(fmaxf(s_m[0][16 * qb + n], s_m[1][16 * qb + n]), fmaxf(s_m[2][16 * qb + n], s_m[3][16 * qb + n]));
+    const float mine = m[qb] == -INFINITY ? 0.f : fast_exp2((m[qb] - top) * a.scale_log2);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *(FLUX_LDS f32x4*)(so + ((w * D / 4 + 4 * db + g) * 16 + n) * 4) = o[db][qb] * mine;
+    __syncthreads();
+    for (int e = tid; e < 16 * (D / 4); e += 256) {
+      const int c = e / (D / 4), d4 = e - c * (D / 4), x = 16 * qb + c;
+      if (x >= rows) continue;
+      f32x4 num = {0.f, 0.f, 0.f, 0.f};
+      float den = 0.f;
+      const float ref = fmaxf(fmaxf(s_m[0][x], s_m[1][x]), fmaxf(s_m[2][x], s_m[3][x]));
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        num += *(FLUX_LDS f32x4*)(so + ((v * D / 4 + d4) * 16 + c) * 4);
+        den += s_m[v][x] == -INFINITY ? 0.f : s_l[v][x] * fast_exp2((s_m[v][x] - ref) * a.scale_log2);
+      }
+      if (u.parts > 1) {
+        const int64_t row = (int64_t)(u.slot + u.ci * u.slot_step) * BM + x;
+        if (d4 == 0) {
+          a.part_ml[2 * row] = ref;
+          a.part_ml[2 * row + 1] = den;
+        }
+        *(f32x4*)(a.part_o + row * D + 4 * d4) = num;
+      } else {
+        const float inv = len > 0 ? 1.0f / den : 0.f;        // (rows without keys are zero)
+        if (a.out_fp32) *(f32x4*)((float*)a.out + row_off(x) + 4 * d4) = num * inv;
+        else *(u32x2*)((__bf16*)a.out + row_off(x) + 4 * d4) = u32x2{pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv)};
+      }
+    }
+  }
+}
+
 // Tiles whose keys were shared out: out = sum_c w_c O_c / sum_c w_c l_c with w_c = 2^(scale (m_c - max m)), parts in order.  D / 4 threads
 // per row, eight or sixteen rows of a tile per workgroup.
 template <int D, int BM>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   constexpr int RPW = 1024 / D;
+  if (a.info[-1][0] == 0) return;                            // no tile was
   const int b = blockIdx.z, d = 4 * (threadIdx.x % (D / 4));
   const int q_begin = a.cu ? a.cu[b] : (a.first + b) * a.q_len, n_q = a.cu ? min(a.cu[b + 1] - q_begin, a.q_len) : a.q_len;
   const int64_t n_rows = (int64_t)n_q * a.group;
@@ -479,15 +683,25 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
 }
 
 namespace {
-template <int D, int QB>
-hipError_t launch_tiles(const CrossArgs& a, hipStream_t s) {
-  constexpr int BM = 64 * QB;
-  hipLaunchKernelGGL((cross_tile_kernel<D, QB>), dim3(a.n_wgs), dim3(256), 0, s, a);
+template <int D, int BM>
+hipError_t launch_one(const CrossArgs& a, hipStream_t s) {
+  if constexpr (BM <= 32) hipLaunchKernelGGL((cross_run_kernel<D, BM / 16>), dim3(a.n_wgs), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((cross_tile_kernel<D, BM / 64>), dim3(a.n_wgs), dim3(256), 0, s, a);
   if (a.part_units == 0) return hipGetLastError();
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((cross_join_kernel<D, BM>), dim3(BM * D / 1024, a.hkv * a.n_tiles, a.batch), dim3(256), 0, s, a);
+  constexpr int RPW = 1024 / D, rows = BM < RPW ? RPW : BM;
+  hipLaunchKernelGGL((cross_join_kernel<D, BM>), dim3(rows / RPW, a.hkv * a.n_tiles, a.batch), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+template <int D>
+hipError_t launch_rows(const CrossArgs& a, int bm, hipStream_t s) {
+  switch (bm) {
+    case 16: return launch_one<D, 16>(a, s);
+    case 32: return launch_one<D, 32>(a, s);
+    case 64: return launch_one<D, 64>(a, s);
+    default: return launch_one<D, 128>(a, s);
+  }
 }
 }  // namespace
 
@@ -512,7 +726,7 @@ hipError_t launch_cross(const Ctx& c, const flux_attn_cfg& cfg, const void* q, c
   a.out_fp32 = cfg.out_dtype;
   a.out = out;
   a.status = c.status;
-  a.info = (i32x4*)c.partials;
+  a.info = (i32x4*)c.partials + 1;
   a.part_o = (float*)((char*)c.partials + p.info_bytes);
   a.part_ml = a.part_o + (long long)p.part_units * p.bm * cfg.head_dim;
   for (a.first = 0; a.first < cache.batch; a.first += kCrossBatch) {
@@ -521,9 +735,7 @@ hipError_t launch_cross(const Ctx& c, const flux_attn_cfg& cfg, const void* q, c
     a.k = (const __bf16*)cache.k + a.first * cache.stride_b;
     a.v = (const __bf16*)cache.v + a.first * cache.stride_b;
     a.kv_len = cache.kv_len + a.first;
-    hipError_t e;
-    if (cfg.head_dim == 128) e = p.bm == 64 ? launch_tiles<128, 1>(a, s) : launch_tiles<128, 2>(a, s);
-    else e = p.bm == 64 ? launch_tiles<64, 1>(a, s) : launch_tiles<64, 2>(a, s);
+    const hipError_t e = cfg.head_dim == 128 ? launch_rows<128>(a, p.bm, s) : launch_rows<64>(a, p.bm, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

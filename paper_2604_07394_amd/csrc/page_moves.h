@@ -5,14 +5,16 @@
 
 namespace flux {
 
-constexpr int kForkPages = 4096;            // pages that a workgroup of the fork's second launch looks through
-constexpr int kForkEntries = 16384;         // entries of the table that a workgroup of its first launch holds in LDS
+constexpr int kForkAlone = 16384;           // pages of a pool up to which one workgroup of a fork looks through all of them
+constexpr int kForkPages = 4096;            // pages that each of several looks through in a second launch
+constexpr int kForkEntries = 16384;         // entries of the table that a workgroup holds in LDS
 constexpr int kCompactPages = 1 << 20;      // pages of a pool that one workgroup holds a bit of each of in LDS (128 KB)
 constexpr int kCopyWgs = 8192;              // workgroups that copy at most
-static_assert(kForkEntries >= FLUX_MAX_PAGED_BATCH, "a column of the table fits");
+static_assert(kForkEntries >= 4 * FLUX_MAX_PAGED_BATCH, "four columns of the table fit");
 
 // Bytes of the partials that the calls take: what every workgroup found and how much, or where every page went.
 inline size_t fork_bytes(int n_pages) {
+  if (n_pages <= kForkAlone) return 0;
   const size_t groups = ((size_t)n_pages + kForkPages - 1) / kForkPages;
   return groups * (kForkPages + 1) * sizeof(int32_t);
 }

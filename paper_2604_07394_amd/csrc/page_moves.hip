@@ -17,7 +17,7 @@ struct MoveArgs {
   const int32_t *parent, *keep;
   int32_t *list, *n_list;         // pages to copy: [.][3] from, to, rows; how many
   int batch, table_pages, n_pages, most;
-  int cols;                       // columns that a workgroup of the fork's first launch takes
+  int cols_shift;                 // log2 of the columns that a workgroup of a fork takes
   int slots_shift;                // 32 less log2 of the places of the table of last pages
   int32_t* scratch;               // fork: counts and pages that went back; compact: where a page went, and from which page on they went
   uint32_t *counter, *status;
@@ -64,59 +64,221 @@ __device__ __forceinline__ int goes_on(const MoveArgs& a, int b, int& p, uint32_
   return a.keep ? clampi(a.keep[b], 0, len) : len;
 }
 
-__global__ __launch_bounds__(256) void page_fork_kernel(MoveArgs a) {
-  __shared__ int s_old[kMaxBatch], s_new[kMaxBatch], s_parent[kMaxBatch], s_entry[kForkEntries], s_most;
+// What the last workgroup of a fork finds out about the last pages that are partly filled: a table in LDS by page (open addressing) of how
+// many sequences have it so, and which is the first.
+struct LastPages {
+  int *page, *holders, *first;
+  int shift;                      // 32 less log2 of the places
+  __device__ __forceinline__ int places() const { return 1 << (32 - shift); }
+  __device__ __forceinline__ void clear() const {
+    for (int i = threadIdx.x; i < places(); i += 1024) {
+      page[i] = -1;
+      holders[i] = 0;
+      first[i] = 0x7FFFFFFF;
+    }
+  }
+  __device__ __forceinline__ int add(int p, int b) const {
+    int at = (int)(((uint32_t)p * 2654435769u) >> shift);    // (2^32 over the golden ratio: neighbours lie far apart)
+    for (;;) {
+      const int was = atomicCAS(&page[at], -1, p);
+      if (was == -1 || was == p) break;
+      at = (at + 1) & (places() - 1);                        // (twice as many places as sequences)
+    }
+    atomicAdd(&holders[at], 1);
+    atomicMin(&first[at], b);
+    return at;
+  }
+};
+constexpr int kMine = kMaxBatch / 1024;     // sequences that a thread looks after: tid, tid + 1024, ..
+
+// The lengths, and copies of last pages that may not be shared, in the order of the sequences.  len(b), last page and its holders less
+// one (shares) as the first part left them; nth_free(j): the j-th free page, of `listed` in all.
+template <typename F>
+__device__ __forceinline__ void fork_copies(const MoveArgs& a, const int* s_len, const LastPages& t, const int (&page)[kMine], const int (&shares)[kMine],
+                                            const int (&place)[kMine], int listed, int* s_sums, F nth_free, uint32_t& bad) {
+  const int tid = threadIdx.x;
+  int copies = 0, nth[kMine];
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    bool copy = false;
+    if (page[i] >= 0) copy = shares[i] > 0 && !(shares[i] + 1 == t.holders[place[i]] && t.first[place[i]] == tid + 1024 * i);
+    int total = 0;
+    nth[i] = -1;
+    if (1024 * i < a.batch) {                                // (uniform)
+      __syncthreads();
+      const int j = copies + sum_before<16>(copy ? 1 : 0, s_sums, total);
+      if (copy) nth[i] = j;
+    }
+    copies += total;
+  }
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int b = tid + 1024 * i;
+    if (b >= a.batch) continue;
+    int len = s_len[b];
+    if (nth[i] >= 0) {
+      const bool given = nth[i] < listed;
+      int to = given ? nth_free(nth[i]) : -1;
+      if (given && (uint32_t)to >= (uint32_t)a.n_pages) {
+        bad |= FLUX_DEV_BAD_PAGE;
+        to = -1;
+      }
+      if (!given) bad |= FLUX_DEV_KV_OVERFLOW;
+      a.table[(int64_t)b * a.table_pages + (len >> 6)] = to;
+      atomicSub(a.shares + page[i], 1);
+      if (given) {
+        a.list[3 * nth[i]] = to >= 0 ? page[i] : -1;
+        a.list[3 * nth[i] + 1] = to;
+        a.list[3 * nth[i] + 2] = len & 63;
+      } else {
+        len &= ~63;
+      }
+    }
+    a.kv_len[b] = len;
+  }
+  if (tid == 0) {
+    *a.n_free = listed - min(copies, listed);
+    *a.n_list = min(copies, listed);
+  }
+}
+
+// The first part, in columns; where the pool is small (ALL) the last workgroup to arrive does the rest, else a second launch does, whose
+// workgroups look through the pool side by side.  What workgroups hand on is written past the caches, and waited for before they arrive.  us of the
+// launch with 64 sequences and 680 pages / 256 and 8200: 26 / 58 in two launches of 64 columns per workgroup; now 10 / 12.
+template <bool ALL>
+__global__ __launch_bounds__(1024) void page_fork_kernel(MoveArgs a) {
+  __shared__ int s_old[kMaxBatch], s_len[kMaxBatch], s_parent[kMaxBatch], s_work[3 * kSlots], s_sums[16], s_most, s_last;
+  static_assert(3 * kSlots >= kForkEntries, "the entries of the first part, then the table of last pages");
   const int tid = threadIdx.x;
   if (tid == 0) s_most = 0;
   __syncthreads();
   uint32_t bad = 0, bad_page = 0;
   int most = 0;
-  for (int b = tid; b < a.batch; b += 256) {
+  for (int b = tid; b < a.batch; b += 1024) {
     int p;
-    const int n = goes_on(a, b, p, bad);
-    s_old[b] = (clampi(a.kv_len[b], 0, a.table_pages << 6) + 63) >> 6;
-    s_new[b] = (n + 63) >> 6;
+    const int n = goes_on(a, b, p, bad), had = (clampi(a.kv_len[b], 0, a.table_pages << 6) + 63) >> 6;
+    s_old[b] = had;
+    s_len[b] = n;
     s_parent[b] = p;
-    most = max(most, max(s_old[b], s_new[b]));
+    most = max(most, max(had, (n + 63) >> 6));
   }
-  atomicMax(&s_most, most);
+  if (most > 0) atomicMax(&s_most, most);
   __syncthreads();
   most = s_most;
-  const int entries = a.batch * a.cols;                      // (at most kForkEntries)
-  for (int64_t c0 = (int64_t)blockIdx.x * a.cols; c0 < most; c0 += (int64_t)gridDim.x * a.cols) {
+  const int shift = a.cols_shift, cols = 1 << shift, entries = a.batch << shift;   // (at most kForkEntries)
+  for (int64_t c0 = (int64_t)blockIdx.x * cols; c0 < most; c0 += (int64_t)gridDim.x * cols) {
     // entries of these columns, -1 where a row has none
-    for (int i = tid; i < entries; i += 256) {
-      const int b = i / a.cols, c = (int)c0 + (i - b * a.cols);
-      int page = -1;
-      if (c < s_old[b]) {
-        page = a.table[(int64_t)b * a.table_pages + c];
-        if ((uint32_t)page >= (uint32_t)a.n_pages) {
-          bad_page = FLUX_DEV_BAD_PAGE;
-          page = -1;
-        }
+    for (int i0 = tid; i0 < entries; i0 += 4096) {
+      int page[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + 1024 * u, b = i >> shift, c = (int)c0 + (i & (cols - 1));
+        page[u] = i < entries && c < s_old[b] ? a.table[(int64_t)b * a.table_pages + c] : -1;
       }
-      s_entry[i] = page;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + 1024 * u;
+        if (i >= entries) continue;
+        if ((uint32_t)page[u] >= (uint32_t)a.n_pages) {
+          if ((int)c0 + (i & (cols - 1)) < s_old[i >> shift]) bad_page = FLUX_DEV_BAD_PAGE;
+          page[u] = -1;
+        }
+        s_work[i] = page[u];
+      }
     }
     __syncthreads();
-    for (int i = tid; i < entries; i += 256) {
-      const int b = i / a.cols, x = i - b * a.cols, c = (int)c0 + x;
-      const int before = s_entry[i], now = c < s_new[b] ? s_entry[s_parent[b] * a.cols + x] : -1;
+    for (int i = tid; i < entries; i += 1024) {
+      const int b = i >> shift, x = i & (cols - 1), c = (int)c0 + x, p = s_parent[b];
+      const int has = (s_len[b] + 63) >> 6, before = s_work[i], now = c < has ? s_work[(p << shift) + x] : -1;
       if (now != before) {
         if (before >= 0) atomicSub(a.shares + before, 1);
         if (now >= 0) atomicAdd(a.shares + now, 1);
       }
-      if (c < max(s_old[b], s_new[b]) && (s_parent[b] != b || c >= s_new[b])) a.table[(int64_t)b * a.table_pages + c] = now;
+      if (c < max(s_old[b], has) && (p != b || c >= has)) put(a.table + (int64_t)b * a.table_pages + c, now);
     }
     __syncthreads();
   }
   if (blockIdx.x != 0) bad = 0;                              // (once per launch)
-  if (bad | bad_page) atomicOr(a.status, bad | bad_page);
+  bad |= bad_page;
+  if (!ALL) {
+    if (bad) atomicOr(a.status, bad);
+    return;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) s_last = atomicAdd(a.counter, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (!s_last) {
+    if (bad) atomicOr(a.status, bad);
+    return;
+  }
+  if (tid == 0) *a.counter = 0;                              // ready for the next launch on this stream
+
+  // the whole pool, from the highest page down, four pages per thread and turn; last pages; all asked for together
+  constexpr int TURNS = kForkAlone / 4096;
+  int have[TURNS][4], page[kMine], shares[kMine], place[kMine];
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = a.n_pages - 1 - 4096 * t - 4 * tid - i;
+      have[t][i] = p >= 0 ? get(a.shares + p) : 0;
+    }
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int b = tid + 1024 * i;
+    page[i] = b < a.batch && (s_len[b] & 63) != 0 ? get(a.table + (int64_t)b * a.table_pages + (s_len[b] >> 6)) : -1;
+  }
+  const int n_free = *a.n_free, avail = clampi(n_free, 0, a.n_pages);
+  if (n_free != avail) bad |= FLUX_DEV_BAD_LENGTH;
+  const LastPages last = {s_work, s_work + kSlots, s_work + 2 * kSlots, a.slots_shift};
+  last.clear();
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) shares[i] = page[i] >= 0 ? get(a.shares + page[i]) : 0;
+  int* const s_low = s_old;                                  // of the pages that go back the lowest, from the lowest up (as many as there may be copies)
+  int listed = avail, back_all = 0, n = 0;
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += have[t][i] < 0 ? 1 : 0;
+  // (how many in all, so that the lowest are known by their place)
+  sum_before<16>(n, s_sums, back_all);
+  int done = 0;
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t) {
+    if (4096 * t >= a.n_pages) continue;                     // (uniform)
+    int m = 0, total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m += have[t][i] < 0 ? 1 : 0;
+    __syncthreads();
+    int at = done + sum_before<16>(m, s_sums, total);
+    done += total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (have[t][i] >= 0) continue;
+      const int p = a.n_pages - 1 - 4096 * t - 4 * tid - i;
+      if (listed + at < a.n_pages) a.free_pages[listed + at] = p;
+      else bad |= FLUX_DEV_BAD_PAGE;
+      const int nth = back_all - 1 - at;
+      if (nth < kMaxBatch) s_low[nth] = p;
+      a.shares[p] = 0;
+      if (have[t][i] < -1) bad |= FLUX_DEV_BAD_PAGE;         // more rows lost it than held it
+      ++at;
+    }
+  }
+  const bool fits = listed + back_all <= a.n_pages;          // (else the list would grow past the pool)
+  listed = min(listed + back_all, a.n_pages);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) place[i] = page[i] >= 0 ? last.add(page[i], tid + 1024 * i) : 0;
+  __syncthreads();
+  fork_copies(a, s_len, last, page, shares, place, listed, s_sums,
+              [&](int j) { return fits && j < back_all ? s_low[j] : a.free_pages[listed - 1 - j]; }, bad);
+  if (bad) atomicOr(a.status, bad);
 }
 
 __global__ __launch_bounds__(1024) void page_fork_end_kernel(MoveArgs a) {
-  __shared__ int s_sums[16], s_begin[1024], s_count[1024], s_last;
-  // last pages that are partly filled, by page: how many sequences have it so, and which is the first (open addressing)
-  __shared__ int s_len[kMaxBatch], s_page[kSlots], s_holders[kSlots], s_first[kSlots];
+  __shared__ int s_sums[16], s_begin[1024], s_count[1024], s_last, s_len[kMaxBatch], s_work[3 * kSlots];
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
   const int groups = (a.n_pages + kForkPages - 1) / kForkPages;
   int32_t* const counts = a.scratch;                         // of every workgroup's pages that go back
@@ -142,7 +304,7 @@ __global__ __launch_bounds__(1024) void page_fork_end_kernel(MoveArgs a) {
     if (tid == 0) put(counts + blockIdx.x, total);
   }
   // the last workgroup to arrive does the rest; what the others found is in memory by then
-  __threadfence();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   if (tid == 0) s_last = atomicAdd(a.counter, 1u) == gridDim.x - 1;
   __syncthreads();
@@ -150,15 +312,9 @@ __global__ __launch_bounds__(1024) void page_fork_end_kernel(MoveArgs a) {
     if (bad) atomicOr(a.status, bad);
     return;
   }
-  __threadfence();
   if (tid == 0) *a.counter = 0;                              // ready for the next launch on this stream
-
-  const int slots = 1 << (32 - a.slots_shift);
-  for (int i = tid; i < slots; i += 1024) {
-    s_page[i] = -1;
-    s_holders[i] = 0;
-    s_first[i] = 0x7FFFFFFF;
-  }
+  const LastPages last = {s_work, s_work + kSlots, s_work + 2 * kSlots, a.slots_shift};
+  last.clear();
   uint32_t known = 0;                                        // (what the first launch has reported)
   for (int b = tid; b < a.batch; b += 1024) {
     int p;
@@ -167,28 +323,16 @@ __global__ __launch_bounds__(1024) void page_fork_end_kernel(MoveArgs a) {
   const int n_free = *a.n_free, avail = clampi(n_free, 0, a.n_pages);
   if (n_free != avail) bad |= FLUX_DEV_BAD_LENGTH;
   __syncthreads();
-  // (a thread looks after the same sequences throughout: up to four)
-  constexpr int MINE = kMaxBatch / 1024;
-  int page[MINE], place[MINE];
+  int page[kMine], shares[kMine], place[kMine];
 #pragma unroll
-  for (int i = 0; i < MINE; ++i) {
+  for (int i = 0; i < kMine; ++i) {
     const int b = tid + 1024 * i;
     page[i] = b < a.batch && (s_len[b] & 63) != 0 ? a.table[(int64_t)b * a.table_pages + (s_len[b] >> 6)] : -1;
   }
 #pragma unroll
-  for (int i = 0; i < MINE; ++i) {
-    place[i] = 0;
-    if (page[i] < 0) continue;
-    int at = (int)(((uint32_t)page[i] * 2654435769u) >> a.slots_shift);          // (2^32 over the golden ratio: neighbours lie far apart)
-    for (;;) {
-      const int was = atomicCAS(&s_page[at], -1, page[i]);
-      if (was == -1 || was == page[i]) break;
-      at = (at + 1) & (slots - 1);                           // (twice as many places as sequences)
-    }
-    atomicAdd(&s_holders[at], 1);
-    atomicMin(&s_first[at], tid + 1024 * i);
-    place[i] = at;
-  }
+  for (int i = 0; i < kMine; ++i) shares[i] = page[i] >= 0 ? get(a.shares + page[i]) : 0;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) place[i] = page[i] >= 0 ? last.add(page[i], tid + 1024 * i) : 0;
   // the list of free pages takes what goes back, the highest first
   int listed = avail;
   for (int g0 = groups - 1; g0 >= 0; g0 -= 1024) {
@@ -210,53 +354,7 @@ __global__ __launch_bounds__(1024) void page_fork_end_kernel(MoveArgs a) {
   }
   __threadfence_block();
   __syncthreads();
-  // copies, in the order of the sequences
-  int copies = 0, nth[MINE];
-#pragma unroll
-  for (int i = 0; i < MINE; ++i) {
-    bool copy = false;
-    if (page[i] >= 0) {
-      const int holders = get(a.shares + page[i]) + 1;
-      copy = holders > 1 && !(holders == s_holders[place[i]] && s_first[place[i]] == tid + 1024 * i);
-    }
-    int total = 0;
-    nth[i] = -1;
-    if (1024 * i < a.batch) {                                // (uniform)
-      const int j = copies + sum_before<16>(copy ? 1 : 0, s_sums, total);
-      if (copy) nth[i] = j;
-      __syncthreads();
-    }
-    copies += total;
-  }
-#pragma unroll
-  for (int i = 0; i < MINE; ++i) {
-    const int b = tid + 1024 * i;
-    if (b >= a.batch) continue;
-    int len = s_len[b];
-    if (nth[i] >= 0) {
-      const bool given = nth[i] < listed;
-      int to = given ? a.free_pages[listed - 1 - nth[i]] : -1;
-      if (given && (uint32_t)to >= (uint32_t)a.n_pages) {
-        bad |= FLUX_DEV_BAD_PAGE;
-        to = -1;
-      }
-      if (!given) bad |= FLUX_DEV_KV_OVERFLOW;
-      a.table[(int64_t)b * a.table_pages + (len >> 6)] = to;
-      atomicSub(a.shares + page[i], 1);
-      if (given) {
-        a.list[3 * nth[i]] = to >= 0 ? page[i] : -1;
-        a.list[3 * nth[i] + 1] = to;
-        a.list[3 * nth[i] + 2] = len & 63;
-      } else {
-        len &= ~63;
-      }
-    }
-    a.kv_len[b] = len;
-  }
-  if (tid == 0) {
-    *a.n_free = listed - min(copies, listed);
-    *a.n_list = min(copies, listed);
-  }
+  fork_copies(a, s_len, last, page, shares, place, listed, s_sums, [&](int j) { return a.free_pages[listed - 1 - j]; }, bad);
   if (bad) atomicOr(a.status, bad);
 }
 
@@ -272,7 +370,7 @@ __global__ __launch_bounds__(1024) void page_compact_kernel(MoveArgs a) {
   const int n_free = *a.n_free, avail = clampi(n_free, 0, a.n_pages);
   if (n_free != avail) bad |= FLUX_DEV_BAD_LENGTH;
   __syncthreads();
-  constexpr int U = 8;
+  constexpr int U = 16;
   for (int i0 = tid; i0 < avail; i0 += 1024 * U) {
     int page[U];
 #pragma unroll
@@ -308,36 +406,50 @@ __global__ __launch_bounds__(1024) void page_compact_kernel(MoveArgs a) {
   int moves = 0;
   for (int i = 0; i < 16; ++i) moves += s_sums[1][i];
   moves = min(moves, a.most);
-  // which pages move, and which are free afterwards
-  int rank = before;                                         // of the chunk's first free page
+  // which pages move, and which are free afterwards.  A lane has one of 64 chunks and their ranks, and hands them to the wave
+  int rank = before;                                         // of the next chunk's first free page
   mine = 0;
-  for (int k = k0; k < k1; ++k) {
-    const uint64_t bits = s_free[k];
-    const int page = 64 * k + l;
-    const bool is_free = (bits >> l) & 1, there = page < a.n_pages;
-    const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
-    const int nth = is_free ? rank + below : used - 1 - (page - rank - below);   // from the lowest; from the highest
-    const bool moved = there && nth < moves;
-    if (moved) {
-      a.list[3 * nth + (is_free ? 1 : 0)] = page;
-      if (!is_free) a.list[3 * nth + 2] = kPageTokens;
+  for (int k = k0; k < k1; k += 64) {
+    const uint64_t own = k + l < k1 ? s_free[k + l] : 0;
+    const int count = __builtin_popcountll(own), incl = wave_inclusive_sum(count), first = rank + incl - count;
+    // (free pages of a chunk move while they are among the lowest, pages in use while they are among the highest)
+    const bool any = k + l < k1 && (first < moves || used - 64 * (k + l + 1) + first + count < moves);
+    uint64_t after = own;
+    for (uint64_t todo = __builtin_amdgcn_ballot_w64(any); todo != 0; todo &= todo - 1) {
+      const int j = __builtin_ctzll(todo);
+      const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)own, j), hi = __builtin_amdgcn_readlane((int)(uint32_t)(own >> 32), j);
+      const int page = 64 * (k + j) + l, r = __builtin_amdgcn_readlane(first, j) + __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+      const bool is_free = ((l < 32 ? lo : hi) >> (l & 31)) & 1;
+      const int nth = is_free ? r : used - 1 - (page - r);   // from the lowest; from the highest
+      const bool moved = page < a.n_pages && nth < moves;
+      if (moved) {
+        a.list[3 * nth + (is_free ? 1 : 0)] = page;
+        if (!is_free) a.list[3 * nth + 2] = kPageTokens;
+      }
+      const uint64_t change = __builtin_amdgcn_ballot_w64(moved);
+      if (l == j) after = own ^ change;
     }
-    const uint64_t after = bits ^ __builtin_amdgcn_ballot_w64(moved);
-    rank += __builtin_popcountll(bits);
+    if (k + l < k1) s_free[k + l] = after;
+    rank += __builtin_amdgcn_readlane(incl, 63);
     mine += __builtin_popcountll(after);
-    if (l == 0) s_free[k] = after;
   }
+  mine = __builtin_amdgcn_readlane(wave_inclusive_sum(mine), 63);
   if (l == 0) s_sums[2][w] = mine;
   __threadfence_block();
   __syncthreads();
   before = 0;
   for (int i = 0; i < w; ++i) before += s_sums[2][i];
-  int at = free_all - 1 - before;                            // the lowest page last
-  for (int k = k0; k < k1; ++k) {
-    const uint64_t bits = s_free[k];
-    const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
-    if ((bits >> l) & 1) a.free_pages[at - below] = 64 * k + l;
-    at -= __builtin_popcountll(bits);
+  rank = before;
+  for (int k = k0; k < k1; k += 64) {
+    const uint64_t own = k + l < k1 ? s_free[k + l] : 0;
+    const int count = __builtin_popcountll(own), incl = wave_inclusive_sum(count), first = rank + incl - count;
+    for (uint64_t todo = __builtin_amdgcn_ballot_w64(own != 0); todo != 0; todo &= todo - 1) {
+      const int j = __builtin_ctzll(todo);
+      const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)own, j), hi = __builtin_amdgcn_readlane((int)(uint32_t)(own >> 32), j);
+      const int r = __builtin_amdgcn_readlane(first, j) + __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+      if (((l < 32 ? lo : hi) >> (l & 31)) & 1) a.free_pages[free_all - 1 - r] = 64 * (k + j) + l;   // the lowest page last
+    }
+    rank += __builtin_amdgcn_readlane(incl, 63);
   }
   // holders go along; where a page went, for the tables
   for (int j = tid; j < moves; j += 1024) {
@@ -358,11 +470,13 @@ __global__ __launch_bounds__(1024) void page_compact_kernel(MoveArgs a) {
 
 // All pages in use from scratch[0] on have moved.
 __global__ __launch_bounds__(256) void page_renumber_kernel(MoveArgs a) {
-  const int from = a.scratch[0];
+  int from = a.scratch[0], len = a.kv_len[blockIdx.y];       // (asked for together; there are no more rows of workgroups than sequences)
+  asm volatile("" : "+s"(from), "+s"(len));
   if (from >= a.n_pages) return;
   uint32_t bad = 0;
   for (int b = blockIdx.y; b < a.batch; b += gridDim.y) {
-    const int pages = (clampi(a.kv_len[b], 0, a.table_pages << 6) + 63) >> 6;
+    if (b != (int)blockIdx.y) len = a.kv_len[b];
+    const int pages = (clampi(len, 0, a.table_pages << 6) + 63) >> 6;
     int32_t* const row = a.table + (int64_t)b * a.table_pages;
     for (int i = blockIdx.x * 256 + threadIdx.x; i < pages; i += gridDim.x * 256) {
       const int page = row[i];
@@ -392,12 +506,12 @@ template <int D>
 __global__ __launch_bounds__(256) void page_copy_kernel(CopyArgs a) {
   constexpr int LPR = D / 16, RPS = 64 / LPR, STEPS = 64 / RPS;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = a.n_list ? min(*a.n_list, a.most) : a.most;
   const int per = 2 * a.hkv;
-  for (int64_t u = (int64_t)blockIdx.x * 4 + w; u < (int64_t)n * per; u += (int64_t)gridDim.x * 4) {
+  int n = a.n_list ? *a.n_list : a.most;
+  for (int64_t u = (int64_t)blockIdx.x * 4 + w; u < (int64_t)min(n, a.most) * per; u += (int64_t)gridDim.x * 4) {
     const int64_t j = u / per;
     const int part = (int)(u - j * per), h = part >> 1;
-    const int from = a.list[3 * j], to = a.list[3 * j + 1], rows = clampi(a.list[3 * j + 2], 0, kPageTokens);
+    int from = a.list[3 * j], to = a.list[3 * j + 1], rows = clampi(a.list[3 * j + 2], 0, kPageTokens);
     if (from == to && from == -1) continue;                  // (an entry that is left out)
     if ((uint32_t)from >= (uint32_t)a.n_pages || (uint32_t)to >= (uint32_t)a.n_pages) {
       if (l == 0 && part == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_BAD_PAGE);
@@ -445,15 +559,21 @@ hipError_t launch_page_fork(const Ctx& c, const flux_page_table& pt, int32_t* sh
   MoveArgs a = move_args(c, pt, shares, copies, n_copies, pt.batch);
   a.parent = parent;
   a.keep = keep;
-  a.cols = 64;
-  while (a.cols > 1 && (long long)a.cols * pt.batch > kForkEntries) a.cols >>= 1;
+  // (16 columns are a line of memory of each row)
+  a.cols_shift = 4;
+  while (a.cols_shift > 2 && (pt.batch << a.cols_shift) > 4096) --a.cols_shift;
   a.slots_shift = 26;                                        // 64 places
   while ((1 << (32 - a.slots_shift)) < 2 * pt.batch) --a.slots_shift;
-  const int wgs = (pt.table_pages + a.cols - 1) / a.cols;
-  hipLaunchKernelGGL(page_fork_kernel, dim3(wgs < 1024 ? wgs : 1024), dim3(256), 0, s, a);
+  const int wgs = (pt.table_pages + (1 << a.cols_shift) - 1) >> a.cols_shift;
+  const dim3 grid(wgs < 1024 ? wgs : 1024), block(1024);
+  if (pt.n_pages <= kForkAlone) {
+    hipLaunchKernelGGL((page_fork_kernel<true>), grid, block, 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((page_fork_kernel<false>), grid, block, 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(page_fork_end_kernel, dim3((pt.n_pages + kForkPages - 1) / kForkPages), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(page_fork_end_kernel, dim3((pt.n_pages + kForkPages - 1) / kForkPages), block, 0, s, a);
   return hipGetLastError();
 }
 
