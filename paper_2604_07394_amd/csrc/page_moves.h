@@ -12,13 +12,13 @@ constexpr int kCompactPages = 1 << 20;      // pages of a pool that one workgrou
 constexpr int kCopyWgs = 8192;              // workgroups that copy at most
 static_assert(kForkEntries >= 4 * FLUX_MAX_PAGED_BATCH, "four columns of the table fit");
 
-// Bytes of the partials that the calls take: what every workgroup found and how much, or where every page went.
+// Bytes of the partials that the calls take: what every workgroup found and how much, or a bit per page and a count per 256.
 inline size_t fork_bytes(int n_pages) {
   if (n_pages <= kForkAlone) return 0;
   const size_t groups = ((size_t)n_pages + kForkPages - 1) / kForkPages;
   return groups * (kForkPages + 1) * sizeof(int32_t);
 }
-inline size_t compact_bytes(int n_pages) { return ((size_t)n_pages + 1) * sizeof(int32_t); }
+inline size_t compact_bytes(int n_pages) { return 16 + ((size_t)n_pages + 255) / 256 * (4 * sizeof(uint64_t) + sizeof(int32_t)); }
 
 hipError_t launch_page_fork(const Ctx& c, const flux_page_table& pt, int32_t* shares, const int32_t* parent, const int32_t* keep, int32_t* copies,
                             int32_t* n_copies, hipStream_t s);
