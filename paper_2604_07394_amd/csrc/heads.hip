@@ -118,14 +118,15 @@ __device__ __forceinline__ void lane_angles(const float* freq, int i, int pos, T
   for (int j = 0; j < 8; ++j) sincos_turn(turn_of(pos, j < 4 ? lo[j] : hi[j & 3]), s[j], c[j]);
 }
 
-// Rows of a token that a wave asks for at once.
-constexpr int kPassesInFlight = 4;
+// Passes that a wave asks for at once.  us of the kernels with 4 / 3 / 2, 32/8 heads of 128, 32768 tokens 135 / 132 / 131; appended, 28/4 heads, 129 to
+// 3001 tokens of five sequences 29.4 / 26.2 / 25.0 (of fewer registers more waves are at work).
+constexpr int kPassesInFlight = 2;
 
 // All rows of one token that this wave has: passes p0, p0 + step, ...  A pass is 64 / (D / 16) rows: the query heads first, then the
-// key heads, then (V) the value heads, which are copied.
-// q_at(h), k_at(h), v_at(h): where a finished row goes, null: nowhere.
-template <int D, bool NEAR, bool V, typename KP, typename VP>
-__device__ __forceinline__ void token_rows(const HeadArgs& a, int64_t t, int pos, int p0, int l, KP k_at, VP v_at) {
+// key heads, then (V) the value heads, which are copied.  position(): of the token, asked when its first rows are on their way; k_at(h), v_at(h):
+// where a finished row goes, null: nowhere.
+template <int D, bool NEAR, bool V, typename PP, typename KP, typename VP>
+__device__ __forceinline__ void token_rows(const HeadArgs& a, int64_t t, PP position, int p0, int l, KP k_at, VP v_at) {
   constexpr int LPH = D / 16, RPP = 64 / LPH;
   const int i = l % LPH;
   int c0, c1;
@@ -159,6 +160,8 @@ __device__ __forceinline__ void token_rows(const HeadArgs& a, int64_t t, int pos
     }
     if (!angles) {                                           // (behind the rows, which take longer to come)
       angles = true;
+      __builtin_amdgcn_sched_barrier(0);
+      const int pos = position();
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] = 0.f, c[j] = 1.f;
       if (turns) lane_angles(a.freq, i, pos, s, c);
@@ -225,8 +228,7 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
   const int64_t units = (int64_t)a.total * a.waves;
   for (int64_t u = (int64_t)blockIdx.x * 4 + w; u < units; u += (int64_t)gridDim.x * 4) {
     const int64_t t = u / a.waves;
-    const int pos = a.rot ? a.pos[t] : 0;
-    token_rows<D, NEAR, false>(a, t, pos, (int)(u - t * a.waves), l, [&](int h) { return a.k_out + (t * a.hkv + h) * D * 2; }, [&](int) { return (char*)nullptr; });
+    token_rows<D, NEAR, false>(a, t, [&]() { return a.rot ? a.pos[t] : 0; }, (int)(u - t * a.waves), l, [&](int h) { return a.k_out + (t * a.hkv + h) * D * 2; }, [&](int) { return (char*)nullptr; });
   }
 }
 
@@ -251,24 +253,31 @@ template <int D, bool NEAR>
 __global__ __launch_bounds__(256) void qkv_rows_kernel(HeadArgs a) {
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t units = (int64_t)a.total * a.waves;
+  // what the last workgroup needs of up to 256 sequences, one per thread
+  const int own = min((int)threadIdx.x, a.batch - 1);
+  const int my_cu = a.cu[own], my_end = a.cu[own + 1], my_len = a.kv_len[own];
   const int end = a.cu[a.batch], begin = a.cu[0];
   bool overflow = false;
   for (int64_t u = (int64_t)blockIdx.x * 4 + w; u < units; u += (int64_t)gridDim.x * 4) {
     const int64_t t = u / a.waves;
     if (t < begin || t >= end) continue;                     // rows of no sequence
-    const int b = sequence_of(a.cu, a.batch, (int)t, l);
-    const int64_t at = (int64_t)a.kv_len[b] + (t - a.cu[b]);
-    const bool kept = at >= 0 && at < a.capacity;
-    overflow |= !kept;
-    const int64_t row = (int64_t)b * a.stride_b + at * a.stride_t;
-    const int pos = a.pos ? a.pos[t] : (int)at;
-    token_rows<D, NEAR, true>(a, t, pos, (int)(u - t * a.waves), l, [&](int h) { return kept ? a.kc + row + h * a.stride_h : nullptr; },
+    bool kept = false;
+    int64_t row = 0;
+    auto place = [&]() {
+      const int b = sequence_of(a.cu, a.batch, (int)t, l);
+      const int64_t at = (int64_t)a.kv_len[b] + (t - a.cu[b]);
+      kept = at >= 0 && at < a.capacity;
+      overflow |= !kept;
+      row = (int64_t)b * a.stride_b + at * a.stride_t;
+      return a.pos ? a.pos[t] : (int)at;
+    };
+    token_rows<D, NEAR, true>(a, t, place, (int)(u - t * a.waves), l, [&](int h) { return kept ? a.kc + row + h * a.stride_h : nullptr; },
                               [&](int h) { return kept ? a.vc + row + h * a.stride_h : nullptr; });
   }
   if (overflow && l == 0) atomicOr(a.status, (uint32_t)FLUX_DEV_KV_OVERFLOW);
   // (a wave holds the length that it read before it passes the barrier, as its rows' places come from it; the stores are not waited for)
   __shared__ int is_last;
-  asm volatile("" ::: "memory");
+  asm volatile("" : : "v"(my_len), "v"(my_cu), "v"(my_end) : "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
     const uint32_t n = gridDim.x, x = blockIdx.x & (kAppendGather - 1);
@@ -284,8 +293,8 @@ __global__ __launch_bounds__(256) void qkv_rows_kernel(HeadArgs a) {
   __syncthreads();
   if (!is_last) return;
   for (int b = threadIdx.x; b < a.batch; b += 256) {
-    const int n = a.cu[b + 1] - a.cu[b];
-    int len = a.kv_len[b];
+    const int n = b < 256 ? my_end - my_cu : a.cu[b + 1] - a.cu[b];
+    int len = b < 256 ? my_len : a.kv_len[b];
     if (n > 0) len = (int)min((int64_t)len + n, (int64_t)a.capacity);
     a.kv_len[b] = min(len, a.capacity);
   }
@@ -304,8 +313,7 @@ struct QuantArgs {
   int64_t stride_p, stride_h, stride_t;
   const int32_t* slots;
   int n_pages;
-  uint32_t units;                 // (tile of 64 token rows, K or V, 2^share), of one head or of all
-  int share;
+  int share;                      // 2^share workgroups look after a tile of 64 token rows, of K or V
   unsigned kv_wgs;                // workgroups that look after K and V; the others have the queries
 };
 
@@ -401,354 +409,159 @@ __device__ __forceinline__ void put_codes(char* at, int c0, int c1, u32x4 codes)
   *(u32x2*)(at + c1) = u32x2{codes[2], codes[3]};
 }
 
-// Where blocks begin among the 64 token rows from t0 on: a row whose slot does not follow that of the row before in the same page; of
-// those one in 2^share.
-__device__ __forceinline__ uint64_t block_begins(const QuantArgs& a, int t0, int turn, int l) {
+// The blocks of a tile of 64 token rows.  A row goes on a block if its slot follows that of the row before in the same page, and begins one
+// otherwise; a block that the tile's last row has goes on in the next tile.
+struct Tile {
+  int slot;                       // of this lane's row, -1: none
+  uint64_t begins, on, on_next;   // rows that begin a block, that go on one, and those of the next tile
+};
+__device__ __forceinline__ Tile load_tile(const QuantArgs& a, int t0, int l) {
+  Tile x;
   const int t = t0 + l;
-  const int s = t < a.h.total ? a.slots[t] : -1, p = t > 0 && t < a.h.total ? a.slots[t - 1] : -1;
-  const uint64_t begins = __builtin_amdgcn_ballot_w64(s >= 0 && !(p == s - 1 && (s & 63) != 0));
-  const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(begins >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)begins, 0));
-  return begins & __builtin_amdgcn_ballot_w64((before & ((1 << a.share) - 1)) == turn);
+  x.slot = t < a.h.total ? a.slots[t] : -1;
+  const int next = t + 64 < a.h.total ? a.slots[t + 64] : -1, first = t0 > 0 ? a.slots[t0 - 1] : -1;
+  const int last = __builtin_amdgcn_readlane(x.slot, 63);
+  const int up = __shfl_up(x.slot, 1), up_next = __shfl_up(next, 1);              // (by all lanes)
+  const int p = l > 0 ? up : first, p_next = l > 0 ? up_next : last;
+  const bool follows = x.slot >= 0 && p == x.slot - 1 && (x.slot & 63) != 0;
+  x.begins = __builtin_amdgcn_ballot_w64(x.slot >= 0 && !follows);
+  x.on = __builtin_amdgcn_ballot_w64(follows);
+  x.on_next = __builtin_amdgcn_ballot_w64(next >= 0 && p_next == next - 1 && (next & 63) != 0);
+  return x;
 }
-// Slot and rows of the block that begins at t; false: its page is not in the pool.
-__device__ __forceinline__ bool block_at(const QuantArgs& a, int t, int l, int& slot, int& rows) {
-  const int mine = t + l < a.h.total ? a.slots[t + l] : -1;
-  slot = __builtin_amdgcn_readfirstlane(mine);
-  const uint64_t others = ~__builtin_amdgcn_ballot_w64((slot & 63) + l < 64 && mine == slot + l);
-  rows = others == 0 ? 64 : __builtin_ctzll(others);
-  if ((slot >> 6) < a.n_pages) return true;
-  if (l == 0) atomicOr(a.h.status, (uint32_t)FLUX_DEV_BAD_PAGE);
-  return false;
+// Rows of the block that begins at this lane's row.
+__device__ __forceinline__ int block_rows(const Tile& x, int l) {
+  const uint64_t stop = l < 63 ? ~x.on >> (l + 1) : 0;       // (shifted-in zeros: the next tile)
+  if (stop != 0) return 1 + __builtin_ctzll(stop);
+  return 64 - l + (~x.on_next == 0 ? 64 : __builtin_ctzll(~x.on_next));
+}
+// Place of the n-th set bit of x (which has so many).
+__device__ __forceinline__ int nth_set(uint64_t x, int n) {
+  int at = 0;
+#pragma unroll
+  for (int step = 32; step > 0; step >>= 1) {
+    const int below = __builtin_popcountll(x & ((1ull << step) - 1));
+    if (n >= below) {
+      n -= below;
+      at += step;
+      x >>= step;
+    }
+  }
+  return at;
 }
 
-// Short calls: a workgroup per block, head and K or V, 16 rows per wave (most blocks of a decode step have one), and the queries beside them.
+// What a workgroup has of its tile's (block, head) pairs, which 2^share workgroups look after: pairs of up to 16 rows go to single waves, the
+// others to all four waves of a workgroup.  one(at, slot, rows, head, alone)
 constexpr int kWaveRows = 16;
+template <typename F>
+__device__ __forceinline__ void for_blocks(const QuantArgs& a, int tile, int turn, int l, int w, F one) {
+  const Tile x = load_tile(a, tile * 64, l);
+  const int mine = block_rows(x, l), hkv = a.h.hkv;
+  const bool begins = (x.begins >> l) & 1, in_pool = (x.slot >> 6) < a.n_pages;
+  if (turn == 0 && w == 0 && __builtin_amdgcn_ballot_w64(begins && !in_pool) != 0 && l == 0) atomicOr(a.h.status, (uint32_t)FLUX_DEV_BAD_PAGE);
+  const uint64_t short_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine <= kWaveRows);
+  const uint64_t long_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine > kWaveRows);
+#pragma unroll 1
+  for (int phase = 0; phase < 2; ++phase) {
+    const bool alone = phase == 0;
+    const uint64_t set = alone ? short_ones : long_ones;
+    const int sharers = (alone ? 4 : 1) << a.share, me = alone ? 4 * turn + w : turn;
+    const int64_t pairs = (int64_t)__builtin_popcountll(set) * hkv;
+#pragma unroll 1
+    for (int64_t pair = me; pair < pairs; pair += sharers) {
+      const int block = (int)((uint32_t)pair / (uint32_t)hkv), at = __builtin_amdgcn_readfirstlane(nth_set(set, block));
+      one(at, __builtin_amdgcn_readlane(x.slot, at), __builtin_amdgcn_readlane(mine, at), (int)pair - block * hkv, alone);
+    }
+  }
+}
+// Largest of what the lanes of a wave (alone), or of the workgroup, have.
+__device__ __forceinline__ uint32_t block_max(uint32_t y, bool alone, uint32_t* words, int l, int w) {
+  y = wave_max(y);
+  if (!alone) {
+    if (l == 0) words[w] = y;
+    __syncthreads();
+    y = max(max(words[0], words[1]), max(words[2], words[3]));
+  }
+  return (uint32_t)__builtin_amdgcn_readfirstlane(y);
+}
+
+// One launch: K and V, then the queries.  What bounds it: a decode step its latencies (slots, rows, the arithmetic of 64 bits), a long prompt the
+// memory and that arithmetic together.  us, 32/8 heads of 128: 64 sequences with a row each 6.3, 256 10.3, 1024 31, 1024 rows of one 17, 4096
+// 30, 16384 111 (3.3 TB/s; three waves per SIMD: with the registers of two 120).  Keys from 32 bits, worked out again in 64 where 32 do not settle a
+// code, in launches of their own for queries, keys and values: 108 for the 16384 rows, 38 for the 4096.
 template <int D, bool NEAR>
-__global__ __launch_bounds__(256) void qkv_quant_kernel(QuantArgs a) {
+__global__ __launch_bounds__(256, 3) void qkv_quant_kernel(QuantArgs a) {
   constexpr int LPR = D / 16, RPS = 64 / LPR, STEPS = kWaveRows / RPS;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (blockIdx.x >= a.kv_wgs) {
     const int64_t units = (int64_t)a.h.total * a.h.waves, step = (int64_t)(gridDim.x - a.kv_wgs) * 4;
     for (int64_t u = (int64_t)(blockIdx.x - a.kv_wgs) * 4 + w; u < units; u += step) {
       const int64_t t = u / a.h.waves;
-      const int pos = a.h.rot ? a.h.pos[t] : 0;
       HeadArgs q = a.h;
       q.hkv = 0;
-      token_rows<D, NEAR, false>(q, t, pos, (int)(u - t * a.h.waves), l, [&](int) { return (char*)nullptr; }, [&](int) { return (char*)nullptr; });
+      token_rows<D, NEAR, false>(q, t, [&]() { return a.h.rot ? a.h.pos[t] : 0; }, (int)(u - t * a.h.waves), l, [&](int) { return (char*)nullptr; }, [&](int) { return (char*)nullptr; });
     }
     return;
   }
   __shared__ uint32_t tops[2][4];
-  int turns_of = 0;                                          // (blocks take turns with the words: a barrier each)
+  int turn_of = 0;                                           // (blocks take turns with the words: a barrier each)
   const int i = l % LPR;
-  const uint32_t per_tile = (2u * a.h.hkv) << a.share;
-  for (uint32_t u = blockIdx.x; u < a.units; u += a.kv_wgs) {                      // (units < 2^31, a launch below 2^25)
-    const int tile = (int)(u / per_tile), rest = (int)(u - tile * per_tile), h = rest >> (a.share + 1);
-    const bool is_v = (rest >> a.share) & 1;
-    const bool norm = !is_v && a.h.k_norm != nullptr;
-    int c0 = 16 * i, c1 = 16 * i + 8;
-    bool turns = false;
-    if (!is_v) lane_places<NEAR>(i, a.h.rot, c0, c1, turns);
-    const char* src = (is_v ? a.h.v : a.h.k) + (int64_t)h * D * 2;
-    const int64_t src_step = is_v ? a.h.stride_v : a.h.stride_k;
-    uint64_t begins = block_begins(a, tile * 64, rest & ((1 << a.share) - 1), l);
-    while (begins != 0) {                                    // (the same for all waves of the workgroup)
-      const int t0 = tile * 64 + __builtin_ctzll(begins);
-      begins &= begins - 1;
-      int slot, rows;
-      if (!block_at(a, t0, l, slot, rows)) continue;
-      const int page = slot >> 6, held = slot & 63;
-      float* const scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.h.hkv + h;
-      char* const dst = (is_v ? a.v : a.k) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h;
-      u32x4 x[STEPS][2], wp[2];
-      int pos[STEPS];
-#pragma unroll
-      for (int k = 0; k < STEPS; ++k) {
-        const int r = kWaveRows * w + k * RPS + l / LPR;
-        x[k][0] = x[k][1] = u32x4{0, 0, 0, 0};
-        pos[k] = 0;
-        if (r < rows) {
-          const char* at = src + (int64_t)(t0 + r) * src_step;
-          x[k][0] = *(const u32x4*)(at + 2 * c0);
-          x[k][1] = *(const u32x4*)(at + 2 * c1);
-          if (turns) pos[k] = a.h.pos[t0 + r];
-        }
-      }
-      const float old = held != 0 ? *scale_at : 0.f;
-      if (norm) {
-        wp[0] = *(const u32x4*)(a.h.k_norm + 2 * c0);
-        wp[1] = *(const u32x4*)(a.h.k_norm + 2 * c1);
-      }
-      uint32_t val[STEPS][16], top = 0;
-#pragma unroll
-      for (int k = 0; k < STEPS; ++k) {
-        if (kWaveRows * w + k * RPS >= rows) continue;       // (uniform)
-        if (is_v) {
-          given_values(x[k], val[k]);
-        } else {
-          double s[8], c[8];
-          key_angles<NEAR>(a.h, i, pos[k], turns, s, c);
-          key_values<LPR, NEAR>(x[k], wp, a.h.eps, norm, turns, s, c, val[k]);
-        }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) top = max(top, finite_or_zero(val[k][j]));
-      }
-      // (rows that the block does not have count as zeros)
-      top = wave_max(top);
-      turns_of ^= 1;
-      if (l == 0) tops[turns_of][w] = top;
-      __syncthreads();
-      top = max(max(tops[turns_of][0], tops[turns_of][1]), max(tops[turns_of][2], tops[turns_of][3]));
-      top = __builtin_amdgcn_readfirstlane(top);
-      const float scale = block_scale(top, old), inv = 1.0f / scale;      // (exact: a power of two)
-#pragma unroll
-      for (int k = 0; k < STEPS; ++k) {
-        const int r = kWaveRows * w + k * RPS + l / LPR;
-        if (r < rows) put_codes(dst + (int64_t)(held + r) * a.stride_t, c0, c1, codes16(val[k], (double)inv));
-      }
-      if (held != 0 && scale > old)                          // the rows that the page holds take the new scale too
-        for (int r = w * RPS + l / LPR; r < held; r += 4 * RPS) scale_down(dst + (int64_t)r * a.stride_t + 16 * i, old * inv);
-      if (threadIdx.x == 0 && (held == 0 || scale > old)) *scale_at = scale;
-    }
-  }
-}
-
-// Long calls: a workgroup per block, head and K or V, 16 rows per wave.  Keys are worked out in 32 bits.  Where the bounds of a value's error round to two different codes (one step of 8 or 16 rows in ten has such a
-// value) the step is worked out again in 64 bits, and so is the block's largest value where it lies next to the border of its scale.
-//
-// The error in 32 bits, in units of 2^-24: the mean of squares takes 4 + 2 + 3 sums and one product, 10 of it; its root's reciprocal
-// half of that and 2 for the instruction, 7; two products, 9 for each of a pair (a, b).  Sine and cosine are off by 4 at most, so a turned
-// value by (9 + 4 + 2) (|a| + |b|) and 1 for its own rounding: below 2^-20 (|a| + |b|), where |a| + |b| is at most sqrt(2) times the
-// sum of the turned magnitudes.
-constexpr float kTurnedError = 0x1.7p-20f;                   // of the sum of a turned pair's magnitudes
-constexpr uint32_t kBorder = 0x600000u, kBorderError = 64;   // 0.75 as a fraction; the error of a largest value in steps of it (2^-20 * 1.5 * 2 * 2^24, and more)
-
-// Sine and cosine of `quarters` quarter turns in 32 bits: the nearest whole number of them (adding 1.5 * 2^52 rounds to one, whose low bits
-// are then the low bits of the sum), and Taylor's series of what is left, at most pi / 4, whose remainders are 2^-29 and 2^-25.3; with the roundings
-// of the argument and of the sums below 2^-22.
-__device__ __forceinline__ void sincos_close(double quarters, float& s, float& c) {
-  constexpr double kRound = 6755399441055744.0;
-  const double m = quarters + kRound;
-  const uint32_t n = __builtin_bit_cast(u32x2, m)[0];
-  const float x = (float)(quarters - (m - kRound)) * 1.57079632679489661923f, z = x * x;
-  float a = 1.0f / 362880, b = 1.0f / 40320;
-  a = __builtin_fmaf(a, z, -1.0f / 5040);
-  b = __builtin_fmaf(b, z, -1.0f / 720);
-  a = __builtin_fmaf(a, z, 1.0f / 120);
-  b = __builtin_fmaf(b, z, 1.0f / 24);
-  a = __builtin_fmaf(a, z, -1.0f / 6);
-  b = __builtin_fmaf(b, z, -0.5f);
-  a = __builtin_fmaf(a * z, x, x);
-  b = __builtin_fmaf(b, z, 1.0f);
-  const float p = n & 1 ? b : a, r = n & 1 ? a : b;
-  s = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p) ^ ((n & 2) << 30));
-  c = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, r) ^ (((n + 1) & 2) << 30));
-}
-
-// The values of a lane in 64 bits, pair by pair.  (Nothing of it is to be worked out before it is needed, or kept from what 32 bits took:
-// with what both share held in registers the kernel has 200 of them in memory.)
-template <int LPR, bool NEAR>
-__device__ __forceinline__ void key_values_one_by_one(const u32x4* x_in, const u32x4* w_in, const f32x4* freq_in, float eps, bool norm, bool turns, int pos, uint32_t* hi) {
-  u32x4 x[2] = {x_in[0], x_in[1]}, w[2] = {w_in[0], w_in[1]};
-  f32x4 freq[2] = {freq_in[0], freq_in[1]};
-  asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(w[0]), "+v"(w[1]), "+v"(freq[0]), "+v"(freq[1]), "+v"(pos));
-  double inv = 1.0;
-  if (norm) {
-    double sum = 0.0;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) sum = __builtin_fma(value_of(x, j), value_of(x, j), sum);
-    inv = 1.0 / __builtin_sqrt(row_sum<LPR>(sum) * (1.0 / (16 * LPR)) + (double)eps);
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int u = NEAR ? 2 * j : j, v = NEAR ? 2 * j + 1 : 8 + j;
-    double p = value_of(x, u), q = value_of(x, v);
-    if (norm) {
-      p = p * inv * value_of(w, u);
-      q = q * inv * value_of(w, v);
-    }
-    if (turns) {
-      double s, c;
-      sincos_turn(turn_of(pos, freq[j >> 2][j & 3]), s, c);
-      const double p0 = p, q0 = q;
-      p = __builtin_fma(-q0, s, p0 * c);
-      q = __builtin_fma(p0, s, q0 * c);
-    }
-    hi[u] = to_odd(p);
-    hi[v] = to_odd(q);
-    asm volatile("" : "+v"(hi[u]), "+v"(hi[v]));
-    __builtin_amdgcn_sched_barrier(0);
-  }
-}
-
-// Rows `all` from token row t on, of head h of K (KEY) or V, into the page of `slot`: 16 of them per wave.
-template <int D, bool NEAR, bool KEY>
-__device__ __forceinline__ void quantise_block(const QuantArgs& a, int t, int slot, int all, int h, int l, int w, uint32_t* tops) {
-  constexpr int LPR = D / 16, RPS = 64 / LPR, STEPS = kWaveRows / RPS;
-  const int page = slot >> 6, held = slot & 63, i = l % LPR, r0 = kWaveRows * w + l / LPR;
+  const int tile = (int)(blockIdx.x >> (a.share + 1));
+  const bool is_v = (blockIdx.x >> a.share) & 1, norm = !is_v && a.h.k_norm != nullptr;
   int c0 = 16 * i, c1 = 16 * i + 8;
   bool turns = false;
-  if (KEY) lane_places<NEAR>(i, a.h.rot, c0, c1, turns);
-  const int64_t src_step = KEY ? a.h.stride_k : a.h.stride_v;
-  const char* src = (KEY ? a.h.k : a.h.v) + t * src_step + (int64_t)h * D * 2;
-  const bool norm = KEY && a.h.k_norm != nullptr;
-  float* const scale_at = (KEY ? a.k_scale : a.v_scale) + (int64_t)page * a.h.hkv + h;
-  char* const dst = (KEY ? a.k : a.v) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h;
-  u32x4 x[STEPS][2], wp[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-  int pos[STEPS];
+  if (!is_v) lane_places<NEAR>(i, a.h.rot, c0, c1, turns);
+  const int64_t src_step = is_v ? a.h.stride_v : a.h.stride_k;
+  for_blocks(a, tile, blockIdx.x & ((1 << a.share) - 1), l, w, [&](int at, int slot, int rows, int h, bool alone) __attribute__((always_inline)) {
+    const int t0 = tile * 64 + at, page = slot >> 6, held = slot & 63, part = alone ? 0 : w, parts = alone ? 1 : 4;
+    const char* src = (is_v ? a.h.v : a.h.k) + t0 * src_step + (int64_t)h * D * 2;
+    float* const scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.h.hkv + h;
+    char* const dst = (is_v ? a.v : a.k) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h;
+    u32x4 x[STEPS][2], wp[2];
+    int pos[STEPS];
 #pragma unroll
-  for (int k = 0; k < STEPS; ++k) {
-    x[k][0] = x[k][1] = u32x4{0, 0, 0, 0};
-    pos[k] = 0;
-    const int r = r0 + k * RPS;
-    if (r < all) {
-      x[k][0] = *(const u32x4*)(src + r * src_step + 2 * c0);
-      x[k][1] = *(const u32x4*)(src + r * src_step + 2 * c1);
-      if (KEY && turns) pos[k] = a.h.pos[t + r];
-    }
-  }
-  const float old = held != 0 ? *scale_at : 0.f;
-  f32x4 freq[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  if (norm) {
-    wp[0] = *(const u32x4*)(a.h.k_norm + 2 * c0);
-    wp[1] = *(const u32x4*)(a.h.k_norm + 2 * c1);
-  }
-  if (KEY && turns) {
-    freq[0] = *(const f32x4*)(a.h.freq + 8 * i);
-    freq[1] = *(const f32x4*)(a.h.freq + 8 * i + 4);
-  }
-  // step k in 64 bits; its rows are read again
-  auto in_full = [&](int k, uint32_t* hi) __attribute__((always_inline)) {
-    const int r = r0 + k * RPS;
-    u32x4 y[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    int p = 0;
-    if (r < all) {
-      y[0] = *(const u32x4*)(src + r * src_step + 2 * c0);
-      y[1] = *(const u32x4*)(src + r * src_step + 2 * c1);
-      if (KEY && turns) p = a.h.pos[t + r];
-    }
-    if (KEY) key_values_one_by_one<LPR, NEAR>(y, wp, freq, a.h.eps, norm, turns, p, hi);
-    else given_values(y, hi);
-  };
-  float val[STEPS][16];
-  uint32_t top = 0, odd = 0;                                 // largest magnitude; whether squares pass 32 bits
-#pragma unroll
-  for (int k = 0; k < STEPS; ++k) {
-    float* y = val[k];
-    unpack8(x[k][0], y);
-    unpack8(x[k][1], y + 8);
-    if (norm) {
-      float part[4] = {0.f, 0.f, 0.f, 0.f}, f[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) part[j & 3] = __builtin_fmaf(y[j], y[j], part[j & 3]);
-      const float sum = row_sum<LPR>((part[0] + part[1]) + (part[2] + part[3]));
-      const float inv = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.0f / D, a.h.eps));
-      odd |= sum < 0x1p100f ? 0u : 1u;
-      unpack8(wp[0], f);
-      unpack8(wp[1], f + 8);
-#pragma unroll
-      for (int j = 0; j < 16; ++j) y[j] = y[j] * inv * f[j];
-    }
-    if (KEY && a.h.rot != 0) {                               // (lanes that turn nothing turn by nothing)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float s, c;
-        sincos_close((double)pos[k] * ((double)freq[j >> 2][j & 3] * (4.0 * kTurnsPerRadian)), s, c);
-        float& u = NEAR ? y[2 * j] : y[j];
-        float& v = NEAR ? y[2 * j + 1] : y[8 + j];
-        const float u0 = u, v0 = v;
-        u = __builtin_fmaf(-v0, s, u0 * c);
-        v = __builtin_fmaf(u0, s, v0 * c);
-        if (j % 2 == 1) __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 16; ++j) top = max(top, __builtin_bit_cast(uint32_t, y[j]) & 0x7FFFFFFFu);
-  }
-  auto most_of_all = [&](uint32_t y, uint32_t* at) __attribute__((always_inline)) {
-    y = wave_max(y);                                         // (rows that the block does not have count as zeros)
-    if (l == 0) at[w] = y;
-    __syncthreads();
-    return (uint32_t)__builtin_amdgcn_readfirstlane(max(max(at[0], at[1]), max(at[2], at[3])));
-  };
-  if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) top = 0x7F800000u;
-  top = most_of_all(top, tops);
-  const bool some_odd = top >= 0x7F800000u;                  // some value of the block is not finite, or left to 64 bits
-  float scale;
-  if (__builtin_expect(some_odd || (KEY && (top & 0x7FFFFFu) + kBorderError - kBorder <= 2 * kBorderError), 0)) {   // (the same for all waves)
-    uint32_t most = 0;
-#pragma unroll 1
     for (int k = 0; k < STEPS; ++k) {
-      uint32_t hi[16];
-      in_full(k, hi);
-#pragma unroll
-      for (int j = 0; j < 16; ++j) most = max(most, finite_or_zero(hi[j]));
+      const int r = kWaveRows * part + k * RPS + l / LPR;
+      x[k][0] = x[k][1] = u32x4{0, 0, 0, 0};
+      pos[k] = 0;
+      if (r < rows) {
+        x[k][0] = *(const u32x4*)(src + r * src_step + 2 * c0);
+        x[k][1] = *(const u32x4*)(src + r * src_step + 2 * c1);
+        if (turns) pos[k] = a.h.pos[t0 + r];
+      }
     }
-    scale = block_scale(most_of_all(most, tops + 4), old);
-  } else {
-    const int e = max((int)(top >> 23) - 135 + ((top & 0x7FFFFFu) > kBorder ? 1 : 0), kMinScaleExp);
-    scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
-    scale = old > scale ? old : scale;
-  }
-  const float inv = 1.0f / scale;                            // exact: a power of two
-  uint32_t again = some_odd ? ~0u : 0u;                      // steps that 32 bits do not settle
+    const float old = held != 0 ? *scale_at : 0.f;
+    if (norm) {
+      wp[0] = *(const u32x4*)(a.h.k_norm + 2 * c0);
+      wp[1] = *(const u32x4*)(a.h.k_norm + 2 * c1);
+    }
+    uint32_t val[STEPS][16], top = 0;
 #pragma unroll
-  for (int k = 0; k < STEPS; ++k) {
-    u32x4 codes;
-    if (KEY) {
-      uint32_t apart = 0;
-      float below[16], above[16];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int u = NEAR ? 2 * j : j, v = NEAR ? 2 * j + 1 : 8 + j;
-        const float p = val[k][u] * inv, q = val[k][v] * inv, off = (__builtin_fabsf(p) + __builtin_fabsf(q)) * kTurnedError;
-        below[u] = p - off, above[u] = p + off;
-        below[v] = q - off, above[v] = q + off;
+    for (int k = 0; k < STEPS; ++k) {
+      if (kWaveRows * part + k * RPS >= rows) continue;      // (uniform)
+      if (is_v) {
+        given_values(x[k], val[k]);
+      } else {
+        double s[8], c[8];
+        key_angles<NEAR>(a.h, i, pos[k], turns, s, c);
+        key_values<LPR, NEAR>(x[k], wp, a.h.eps, norm, turns, s, c, val[k]);
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        codes[j] = codes4(below[4 * j], below[4 * j + 1], below[4 * j + 2], below[4 * j + 3]);
-        apart |= codes[j] ^ codes4(above[4 * j], above[4 * j + 1], above[4 * j + 2], above[4 * j + 3]);
-      }
-      if (__builtin_amdgcn_ballot_w64(apart != 0) != 0) again |= 1u << k;
-    } else {
+      for (int j = 0; j < 16; ++j) top = max(top, finite_or_zero(val[k][j]));
+    }
+    // (rows that the block does not have count as zeros)
+    turn_of ^= alone ? 0 : 1;
+    top = block_max(top, alone, tops[turn_of], l, w);
+    const float scale = block_scale(top, old), inv = 1.0f / scale;        // (exact: a power of two)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) codes[j] = codes4(val[k][4 * j] * inv, val[k][4 * j + 1] * inv, val[k][4 * j + 2] * inv, val[k][4 * j + 3] * inv);
+    for (int k = 0; k < STEPS; ++k) {
+      const int r = kWaveRows * part + k * RPS + l / LPR;
+      if (r < rows) put_codes(dst + (int64_t)(held + r) * a.stride_t, c0, c1, codes16(val[k], (double)inv));
     }
-    if (r0 + k * RPS < all) put_codes(dst + (int64_t)(held + r0 + k * RPS) * a.stride_t, c0, c1, codes);
-    __builtin_amdgcn_sched_barrier(0);
-  }
-#pragma unroll 1
-  for (int k = 0; k < STEPS; ++k) {
-    if (!((again >> k) & 1)) continue;
-    uint32_t hi[16];
-    in_full(k, hi);
-    if (r0 + k * RPS < all) put_codes(dst + (int64_t)(held + r0 + k * RPS) * a.stride_t, c0, c1, codes16(hi, (double)inv));
-  }
-  if (held != 0 && scale > old)                              // the rows that the page holds take the new scale too
-    for (int r = w * RPS + l / LPR; r < held; r += 4 * RPS) scale_down(dst + (int64_t)r * a.stride_t + 16 * i, old * inv);
-  if (threadIdx.x == 0 && (held == 0 || scale > old)) *scale_at = scale;
-}
-
-template <int D, bool NEAR>
-__global__ __launch_bounds__(256, 3) void quant_pages_kernel(QuantArgs a) {
-  __shared__ uint32_t tops[2][8];
-  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int turn = 0;                                              // (blocks take turns with the words: a barrier each)
-  const uint32_t per_tile = (2u * a.h.hkv) << a.share;
-  for (uint32_t u = blockIdx.x; u < a.units; u += gridDim.x) {                     // (units < 2^31, a launch below 2^25)
-    const int tile = (int)(u / per_tile), rest = (int)(u - tile * per_tile), h = rest >> (a.share + 1);
-    uint64_t begins = block_begins(a, tile * 64, rest & ((1 << a.share) - 1), l);
-    while (begins != 0) {                                    // (the same for all waves of the workgroup)
-      const int t0 = tile * 64 + __builtin_ctzll(begins);
-      begins &= begins - 1;
-      int slot, rows;
-      if (!block_at(a, t0, l, slot, rows)) continue;
-      turn ^= 1;
-      if ((rest >> a.share) & 1) quantise_block<D, NEAR, false>(a, t0, slot, rows, h, l, w, tops[turn]);
-      else quantise_block<D, NEAR, true>(a, t0, slot, rows, h, l, w, tops[turn]);
-    }
-  }
+    if (held != 0 && scale > old)                            // the rows that the page holds take the new scale too
+      for (int r = part * RPS + l / LPR; r < held; r += parts * RPS) scale_down(dst + (int64_t)r * a.stride_t + 16 * i, old * inv);
+    if (l == 0 && part == 0 && (held == 0 || scale > old)) *scale_at = scale;
+  });
 }
 
 namespace {
@@ -781,19 +594,19 @@ unsigned wgs_for(const HeadArgs& a) {
 }
 }  // namespace
 
-#define FLUX_HEADS(kernel, cfg, grid, threads, stream, args)                                                                       \
+#define FLUX_HEADS(kernel, cfg, grid, stream, args)                                                                       \
   do {                                                                                                                             \
-    if ((cfg).head_dim == 128 && (cfg).interleaved) hipLaunchKernelGGL((kernel<128, true>), dim3(grid), dim3(threads), 0, stream, args);   \
-    else if ((cfg).head_dim == 128) hipLaunchKernelGGL((kernel<128, false>), dim3(grid), dim3(threads), 0, stream, args);          \
-    else if ((cfg).interleaved) hipLaunchKernelGGL((kernel<64, true>), dim3(grid), dim3(threads), 0, stream, args);                \
-    else hipLaunchKernelGGL((kernel<64, false>), dim3(grid), dim3(threads), 0, stream, args);                                      \
+    if ((cfg).head_dim == 128 && (cfg).interleaved) hipLaunchKernelGGL((kernel<128, true>), dim3(grid), dim3(256), 0, stream, args);   \
+    else if ((cfg).head_dim == 128) hipLaunchKernelGGL((kernel<128, false>), dim3(grid), dim3(256), 0, stream, args);          \
+    else if ((cfg).interleaved) hipLaunchKernelGGL((kernel<64, true>), dim3(grid), dim3(256), 0, stream, args);                \
+    else hipLaunchKernelGGL((kernel<64, false>), dim3(grid), dim3(256), 0, stream, args);                                      \
   } while (0)
 
 hipError_t launch_head_rows(const HeadRows& r, void* k_out, hipStream_t s) {
   HeadArgs a = head_args(r, k_out != nullptr, false);
   a.k_out = (char*)k_out;
   if (!k_out) a.hkv = 0;
-  FLUX_HEADS(head_rows_kernel, r.cfg, wgs_for(a), 256, s, a);
+  FLUX_HEADS(head_rows_kernel, r.cfg, wgs_for(a), s, a);
   return hipGetLastError();
 }
 
@@ -811,7 +624,7 @@ hipError_t launch_qkv_append(const Ctx& c, const HeadRows& r, const flux_kv_cach
   a.counter = c.counters + 0;
   a.gather = c.append_counters;
   a.status = c.status;
-  FLUX_HEADS(qkv_rows_kernel, r.cfg, wgs_for(a), 256, s, a);
+  FLUX_HEADS(qkv_rows_kernel, r.cfg, wgs_for(a), s, a);
   return hipGetLastError();
 }
 
@@ -828,27 +641,14 @@ hipError_t launch_qkv_append_paged(const Ctx& c, const HeadRows& r, const flux_p
   a.stride_t = kv.stride_t;
   a.slots = slots;
   a.n_pages = kv.n_pages;
+  // Workgroups per tile: as many as there are heads, for blocks that fill the tile, and more where that makes few of them, for tiles of
+  // many short blocks
   const long long tiles = ((long long)r.total + 63) / 64;
-  if (r.total >= kQuantLong) {
-    a.share = 6;
-    while (a.share > 0 && (tiles * 2 * r.cfg.n_kv_heads << a.share) > kAppendPagedWaves) --a.share;
-    a.units = (uint32_t)(tiles * 2 * r.cfg.n_kv_heads << a.share);
-    if (a.h.passes > 0) {
-      HeadArgs q = a.h;
-      q.hkv = 0;
-      FLUX_HEADS(head_rows_kernel, r.cfg, wgs_for(q), 256, s, q);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-    FLUX_HEADS(quant_pages_kernel, r.cfg, a.units < (uint32_t)kAppendMost ? a.units : (uint32_t)kAppendMost, 256, s, a);
-    return hipGetLastError();
-  }
-  a.share = 6;
-  while (a.share > 0 && (tiles * 2 * r.cfg.n_kv_heads << a.share) > kAppendPagedWaves) --a.share;
-  a.units = (uint32_t)(tiles * 2 * r.cfg.n_kv_heads << a.share);
-  a.kv_wgs = a.units < (uint32_t)kAppendMost ? a.units : (uint32_t)kAppendMost;
+  a.share = 0;
+  while (a.share < 7 && ((1 << a.share) < r.cfg.n_kv_heads ? tiles << a.share < kQuantMost : tiles << a.share < kQuantWgs)) ++a.share;
+  a.kv_wgs = (unsigned)(tiles << (a.share + 1));             // (at most 2^25: total <= 2^30)
   const unsigned q_wgs = a.h.passes > 0 ? wgs_for(a.h) : 0;
-  FLUX_HEADS(qkv_quant_kernel, r.cfg, a.kv_wgs + q_wgs, 256, s, a);
+  FLUX_HEADS(qkv_quant_kernel, r.cfg, a.kv_wgs + q_wgs, s, a);
   return hipGetLastError();
 }
 
