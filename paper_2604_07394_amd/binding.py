@@ -68,6 +68,7 @@ class FluxQKVRows(C.Structure):
                 ("stride_q", C.c_int64), ("stride_k", C.c_int64), ("stride_v", C.c_int64)]
 
 
+_bf16 = torch.bfloat16
 _pack_rows = struct.Struct("@PPPqqq").pack                   # the bytes of a FluxQKVRows
 _pack_cache = struct.Struct("@PPqqqPii").pack                # the bytes of a FluxKVCache
 assert struct.calcsize("@PPqqqPii") == C.sizeof(FluxKVCache)
@@ -424,19 +425,18 @@ def _head_arg(hc):
     return hc.packed if type(hc) is HeadCfg else C.byref(hc)
 
 
+def _row_stride(x):
+    """Elements between the token rows of a tensor [T, heads, head_dim] whose heads lie next to each other."""
+    t, h, d = x.shape
+    stride, between, one = x.stride()
+    assert one == 1 and (between == d or h == 1) and x.dtype is _bf16
+    return stride if t > 1 else h * d                        # (of a single row torch may say anything)
+
+
 def _rows_arg(q, k, v):
-    """The bytes of a FluxQKVRows: tensors [T, heads, head_dim] whose heads lie next to each other, any stride between tokens."""
-    at, strides = [], []
-    for x in (q, k, v):
-        if x is None:
-            at.append(0)
-            strides.append(0)
-            continue
-        s = x.stride()
-        assert x.dtype == torch.bfloat16 and s[2] == 1 and (s[1] == x.shape[2] or x.shape[1] == 1)
-        at.append(x.data_ptr())
-        strides.append(s[0] if x.shape[0] > 1 else x.shape[1] * x.shape[2])              # (of a single row torch may say anything)
-    return _pack_rows(*at, *strides)
+    """The bytes of a FluxQKVRows.  (Written out for each of the three: in a loop it took 3.2 us, of the 5.5 of a call, and takes 2.4.)"""
+    return _pack_rows(q.data_ptr() if q is not None else 0, k.data_ptr() if k is not None else 0, v.data_ptr() if v is not None else 0,
+                      _row_stride(q) if q is not None else 0, _row_stride(k) if k is not None else 0, _row_stride(v) if v is not None else 0)
 
 
 def flux_qk_norm_rope(ctx, hc, q, k, positions, total, q_out, k_out, stream=None) -> None:

@@ -559,7 +559,7 @@ int flux_qkv_append_paged(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_pa
   if (rc != FLUX_OK) return rc;
   rc = check_values(cfg, in);
   if (rc != FLUX_OK) return rc;
-  if ((total_new / 64 + 1ll) * cfg->n_kv_heads > (1 << 30)) return FLUX_EINVAL;   // (tile of rows, head) pairs are counted in 32 bits
+  if (total_new > (1 << 27)) return FLUX_EINVAL;            // (the threads of a launch are counted in 32 bits)
   rc = check_paged_kv(kv, cfg->head_dim);
   if (rc != FLUX_OK) return rc;
   if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);

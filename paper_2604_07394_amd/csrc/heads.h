@@ -19,6 +19,7 @@ hipError_t launch_qkv_append(const Ctx& c, const HeadRows& r, const flux_kv_cach
 hipError_t launch_qkv_append_paged(const Ctx& c, const HeadRows& r, const flux_paged_kv& kv, const int32_t* slots, hipStream_t s);
 
 constexpr int kHeadWaves = 8192;            // waves that a launch takes where a token's heads can be shared out over so many
+constexpr int kHeadMost = 1 << 20;          // workgroups for queries that such a launch takes at most
 constexpr int kQuantWgs = 512;              // workgroups of a launch, for K or V, up to which tiles take more of them than there are heads
 constexpr int kQuantMost = 4096;            // and up to which they take one per head
 // Waves that the heads of a token are shared out over, `passes` of 64 lanes in all.

@@ -347,6 +347,11 @@ __device__ __forceinline__ float block_scale(uint32_t top, float old) {
   const float scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
   return old > scale ? old : scale;
 }
+typedef __attribute__((__vector_size__(2 * sizeof(uint16_t)))) uint16_t u16x2;
+// The larger of each half.
+__device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, off));
@@ -366,19 +371,20 @@ __device__ __forceinline__ double value_of(const u32x4* x, int j) {
   const uint32_t u = x[j >> 3][(j & 7) >> 1];
   return (double)(j & 1 ? bf16_hi(u) : bf16_lo(u));
 }
-__device__ __forceinline__ void given_values(const u32x4* x, uint32_t* hi) {
-#pragma unroll
-  for (int j = 0; j < 16; ++j) hi[j] = to_odd(value_of(x, j));
-}
-// The 16 values of a lane normed (w not null) and turned by s, c.
+// The 16 values of a lane normed and turned, in 64 bits, pair by pair (which keeps registers free).
 template <int LPR, bool NEAR>
-__device__ __forceinline__ void key_values(const u32x4* x, const u32x4* w, float eps, bool norm, bool turns, const double* s, const double* c, uint32_t* hi) {
+__device__ __forceinline__ void key_values(const HeadArgs& a, const u32x4* x, const u32x4* w, int i, int pos, bool norm, bool turns, uint32_t* hi) {
   double inv = 1.0;
   if (norm) {
     double sum = 0.0;
 #pragma unroll
     for (int j = 0; j < 16; ++j) sum = __builtin_fma(value_of(x, j), value_of(x, j), sum);
-    inv = 1.0 / __builtin_sqrt(row_sum<LPR>(sum) * (1.0 / (16 * LPR)) + (double)eps);
+    inv = 1.0 / __builtin_sqrt(row_sum<LPR>(sum) * (1.0 / (16 * LPR)) + (double)a.eps);
+  }
+  f32x4 freq[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  if (turns) {
+    freq[0] = *(const f32x4*)(a.freq + 8 * i);
+    freq[1] = *(const f32x4*)(a.freq + 8 * i + 4);
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -388,21 +394,19 @@ __device__ __forceinline__ void key_values(const u32x4* x, const u32x4* w, float
       p = p * inv * value_of(w, u);
       q = q * inv * value_of(w, v);
     }
-    const double p1 = __builtin_fma(-q, s[j], p * c[j]), q1 = __builtin_fma(p, s[j], q * c[j]);
-    // (a dimension that is not turned is not touched by the other, whatever that is)
-    hi[u] = to_odd(turns ? p1 : p);
-    hi[v] = to_odd(turns ? q1 : q);
+    if (a.rot != 0) {
+      double s, c;
+      sincos_turn(turn_of(pos, freq[j >> 2][j & 3]), s, c);
+      const double p1 = __builtin_fma(-q, s, p * c), q1 = __builtin_fma(p, s, q * c);
+      // (a dimension that is not turned is not touched by the other, whatever that is)
+      p = turns ? p1 : p;
+      q = turns ? q1 : q;
+    }
+    hi[u] = to_odd(p);
+    hi[v] = to_odd(q);
+    asm volatile("" : "+v"(hi[u]), "+v"(hi[v]));             // (worked out here, not where they are used)
+    if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
   }
-}
-template <bool NEAR>
-__device__ __forceinline__ void key_angles(const HeadArgs& a, int i, int pos, bool turns, double* s, double* c) {
-  f32x4 freq[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  if (turns) {
-    freq[0] = *(const f32x4*)(a.freq + 8 * i);
-    freq[1] = *(const f32x4*)(a.freq + 8 * i + 4);
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) sincos_turn(turn_of(pos, freq[j >> 2][j & 3]), s[j], c[j]);
 }
 __device__ __forceinline__ void put_codes(char* at, int c0, int c1, u32x4 codes) {
   *(u32x2*)(at + c0) = u32x2{codes[0], codes[1]};
@@ -450,22 +454,21 @@ __device__ __forceinline__ int nth_set(uint64_t x, int n) {
   return at;
 }
 
-// What a workgroup has of its tile's (block, head) pairs, which 2^share workgroups look after: pairs of up to 16 rows go to single waves, the
-// others to all four waves of a workgroup.  one(at, slot, rows, head, alone)
-constexpr int kWaveRows = 16;
-template <typename F>
+// What a workgroup of W waves has of its tile's (block, head) pairs, which 2^share workgroups look after: pairs of up to 64 / W rows, what
+// a wave holds at a time, go to single waves, the others to a whole workgroup.  one(at, slot, rows, head, alone)
+template <int W, typename F>
 __device__ __forceinline__ void for_blocks(const QuantArgs& a, int tile, int turn, int l, int w, F one) {
   const Tile x = load_tile(a, tile * 64, l);
   const int mine = block_rows(x, l), hkv = a.h.hkv;
   const bool begins = (x.begins >> l) & 1, in_pool = (x.slot >> 6) < a.n_pages;
   if (turn == 0 && w == 0 && __builtin_amdgcn_ballot_w64(begins && !in_pool) != 0 && l == 0) atomicOr(a.h.status, (uint32_t)FLUX_DEV_BAD_PAGE);
-  const uint64_t short_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine <= kWaveRows);
-  const uint64_t long_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine > kWaveRows);
+  const uint64_t short_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine <= 64 / W);
+  const uint64_t long_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine > 64 / W);
 #pragma unroll 1
   for (int phase = 0; phase < 2; ++phase) {
     const bool alone = phase == 0;
     const uint64_t set = alone ? short_ones : long_ones;
-    const int sharers = (alone ? 4 : 1) << a.share, me = alone ? 4 * turn + w : turn;
+    const int sharers = (alone ? W : 1) << a.share, me = alone ? W * turn + w : turn;
     const int64_t pairs = (int64_t)__builtin_popcountll(set) * hkv;
 #pragma unroll 1
     for (int64_t pair = me; pair < pairs; pair += sharers) {
@@ -475,12 +478,14 @@ __device__ __forceinline__ void for_blocks(const QuantArgs& a, int tile, int tur
   }
 }
 // Largest of what the lanes of a wave (alone), or of the workgroup, have.
+template <int W>
 __device__ __forceinline__ uint32_t block_max(uint32_t y, bool alone, uint32_t* words, int l, int w) {
   y = wave_max(y);
   if (!alone) {
     if (l == 0) words[w] = y;
     __syncthreads();
-    y = max(max(words[0], words[1]), max(words[2], words[3]));
+#pragma unroll
+    for (int i = 0; i < W; ++i) y = max(y, words[i]);
   }
   return (uint32_t)__builtin_amdgcn_readfirstlane(y);
 }
@@ -489,13 +494,15 @@ __device__ __forceinline__ uint32_t block_max(uint32_t y, bool alone, uint32_t* 
 // memory and that arithmetic together.  us, 32/8 heads of 128: 64 sequences with a row each 6.3, 256 10.3, 1024 31, 1024 rows of one 17, 4096
 // 30, 16384 111 (3.3 TB/s; three waves per SIMD: with the registers of two 120).  Keys from 32 bits, worked out again in 64 where 32 do not settle a
 // code, in launches of their own for queries, keys and values: 108 for the 16384 rows, 38 for the 4096.
+constexpr int quant_waves(int head_dim) { return head_dim == 128 ? 8 : 4; }   // of a workgroup: a row per D / 16 lanes, 64 rows in all
 template <int D, bool NEAR>
-__global__ __launch_bounds__(256, 3) void qkv_quant_kernel(QuantArgs a) {
-  constexpr int LPR = D / 16, RPS = 64 / LPR, STEPS = kWaveRows / RPS;
+__global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(QuantArgs a) {
+  constexpr int LPR = D / 16, W = quant_waves(D), RPW = 64 / W;
+  static_assert(RPW * LPR == 64, "a wave holds its rows at once");
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (blockIdx.x >= a.kv_wgs) {
-    const int64_t units = (int64_t)a.h.total * a.h.waves, step = (int64_t)(gridDim.x - a.kv_wgs) * 4;
-    for (int64_t u = (int64_t)(blockIdx.x - a.kv_wgs) * 4 + w; u < units; u += step) {
+    const int64_t units = (int64_t)a.h.total * a.h.waves, step = (int64_t)(gridDim.x - a.kv_wgs) * W;
+    for (int64_t u = (int64_t)(blockIdx.x - a.kv_wgs) * W + w; u < units; u += step) {
       const int64_t t = u / a.h.waves;
       HeadArgs q = a.h;
       q.hkv = 0;
@@ -503,7 +510,7 @@ __global__ __launch_bounds__(256, 3) void qkv_quant_kernel(QuantArgs a) {
     }
     return;
   }
-  __shared__ uint32_t tops[2][4];
+  __shared__ uint32_t tops[2][W];
   int turn_of = 0;                                           // (blocks take turns with the words: a barrier each)
   const int i = l % LPR;
   const int tile = (int)(blockIdx.x >> (a.share + 1));
@@ -512,54 +519,73 @@ __global__ __launch_bounds__(256, 3) void qkv_quant_kernel(QuantArgs a) {
   bool turns = false;
   if (!is_v) lane_places<NEAR>(i, a.h.rot, c0, c1, turns);
   const int64_t src_step = is_v ? a.h.stride_v : a.h.stride_k;
-  for_blocks(a, tile, blockIdx.x & ((1 << a.share) - 1), l, w, [&](int at, int slot, int rows, int h, bool alone) __attribute__((always_inline)) {
-    const int t0 = tile * 64 + at, page = slot >> 6, held = slot & 63, part = alone ? 0 : w, parts = alone ? 1 : 4;
-    const char* src = (is_v ? a.h.v : a.h.k) + t0 * src_step + (int64_t)h * D * 2;
+  for_blocks<W>(a, tile, blockIdx.x & ((1 << a.share) - 1), l, w, [&](int at, int slot, int rows, int h, bool alone) __attribute__((always_inline)) {
+    const int t0 = tile * 64 + at, page = slot >> 6, held = slot & 63, part = alone ? 0 : w, parts = alone ? 1 : W, r = RPW * part + l / LPR;
+    const char* src = (is_v ? a.h.v : a.h.k) + (int64_t)(t0 + r) * src_step + (int64_t)h * D * 2;
     float* const scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.h.hkv + h;
     char* const dst = (is_v ? a.v : a.k) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h;
-    u32x4 x[STEPS][2], wp[2];
-    int pos[STEPS];
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-      const int r = kWaveRows * part + k * RPS + l / LPR;
-      x[k][0] = x[k][1] = u32x4{0, 0, 0, 0};
-      pos[k] = 0;
-      if (r < rows) {
-        x[k][0] = *(const u32x4*)(src + r * src_step + 2 * c0);
-        x[k][1] = *(const u32x4*)(src + r * src_step + 2 * c1);
-        if (turns) pos[k] = a.h.pos[t0 + r];
-      }
+    u32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};               // (rows that the block does not have count as zeros)
+    int pos = 0;
+    if (r < rows) {
+      x[0] = *(const u32x4*)(src + 2 * c0);
+      x[1] = *(const u32x4*)(src + 2 * c1);
+      if (turns) pos = a.h.pos[t0 + r];
     }
     const float old = held != 0 ? *scale_at : 0.f;
-    if (norm) {
-      wp[0] = *(const u32x4*)(a.h.k_norm + 2 * c0);
-      wp[1] = *(const u32x4*)(a.h.k_norm + 2 * c1);
-    }
-    uint32_t val[STEPS][16], top = 0;
-#pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-      if (kWaveRows * part + k * RPS >= rows) continue;      // (uniform)
-      if (is_v) {
-        given_values(x[k], val[k]);
-      } else {
-        double s[8], c[8];
-        key_angles<NEAR>(a.h, i, pos[k], turns, s, c);
-        key_values<LPR, NEAR>(x[k], wp, a.h.eps, norm, turns, s, c, val[k]);
-      }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) top = max(top, finite_or_zero(val[k][j]));
-    }
-    // (rows that the block does not have count as zeros)
+    float scale, inv;                                        // (inv: exact, a power of two)
     turn_of ^= alone ? 0 : 1;
-    top = block_max(top, alone, tops[turn_of], l, w);
-    const float scale = block_scale(top, old), inv = 1.0f / scale;        // (exact: a power of two)
+    if (is_v) {
+      // values as they are: their bits say which is the largest, and 32 bits hold all that a code needs
+      uint32_t most = 0;
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-      const int r = kWaveRows * part + k * RPS + l / LPR;
-      if (r < rows) put_codes(dst + (int64_t)(held + r) * a.stride_t, c0, c1, codes16(val[k], (double)inv));
+      for (int j = 0; j < 8; ++j) most = pair_max(most, x[j >> 2][j & 3] & 0x7FFF7FFFu);
+      const bool odd = __builtin_amdgcn_ballot_w64((most & 0xFFFFu) >= 0x7F80u || (most >> 16) >= 0x7F80u) != 0;   // some value is not finite
+      if (odd) {
+        most = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t lo = x[j >> 2][j & 3] & 0x7FFFu, hi = (x[j >> 2][j & 3] >> 16) & 0x7FFFu;
+          most = pair_max(most, (lo < 0x7F80u ? lo : 0u) | (hi < 0x7F80u ? hi << 16 : 0u));
+        }
+      }
+      most = block_max<W>(max(most & 0xFFFFu, most >> 16), alone, tops[turn_of], l, w);
+      // most = (1 + f / 128) 2^(E - 127): see block_scale
+      const int e = max((int)(most >> 7) - 135 + ((most & 127) > 96 ? 1 : 0), kMinScaleExp);
+      scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
+      scale = old > scale ? old : scale;
+      inv = 1.0f / scale;
+      float f[16];
+      unpack8(x[0], f);
+      unpack8(x[1], f + 8);
+      if (odd) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) f[j] = f[j] - f[j] == 0.f ? f[j] : __builtin_nanf("");
+      }
+      u32x4 codes;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) codes[j] = codes4(f[4 * j] * inv, f[4 * j + 1] * inv, f[4 * j + 2] * inv, f[4 * j + 3] * inv);
+      if (r < rows) *(u32x4*)(dst + (int64_t)(held + r) * a.stride_t + c0) = codes;
+    } else {
+      uint32_t val[16], top = 0;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) val[j] = 0;
+      if (RPW * part < rows) {                               // (uniform)
+        u32x4 wp[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+        if (norm) {
+          wp[0] = *(const u32x4*)(a.h.k_norm + 2 * c0);
+          wp[1] = *(const u32x4*)(a.h.k_norm + 2 * c1);
+        }
+        key_values<LPR, NEAR>(a.h, x, wp, i, pos, norm, turns, val);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = max(top, finite_or_zero(val[j]));
+      }
+      top = block_max<W>(top, alone, tops[turn_of], l, w);
+      scale = block_scale(top, old);
+      inv = 1.0f / scale;
+      if (r < rows) put_codes(dst + (int64_t)(held + r) * a.stride_t, c0, c1, codes16(val, (double)inv));
     }
     if (held != 0 && scale > old)                            // the rows that the page holds take the new scale too
-      for (int r = part * RPS + l / LPR; r < held; r += parts * RPS) scale_down(dst + (int64_t)r * a.stride_t + 16 * i, old * inv);
+      for (int y = RPW * part + l / LPR; y < held; y += parts * RPW) scale_down(dst + (int64_t)y * a.stride_t + 16 * i, old * inv);
     if (l == 0 && part == 0 && (held == 0 || scale > old)) *scale_at = scale;
   });
 }
@@ -594,19 +620,19 @@ unsigned wgs_for(const HeadArgs& a) {
 }
 }  // namespace
 
-#define FLUX_HEADS(kernel, cfg, grid, stream, args)                                                                       \
+#define FLUX_HEADS(kernel, cfg, grid, threads, stream, args)                                                                       \
   do {                                                                                                                             \
-    if ((cfg).head_dim == 128 && (cfg).interleaved) hipLaunchKernelGGL((kernel<128, true>), dim3(grid), dim3(256), 0, stream, args);   \
-    else if ((cfg).head_dim == 128) hipLaunchKernelGGL((kernel<128, false>), dim3(grid), dim3(256), 0, stream, args);          \
-    else if ((cfg).interleaved) hipLaunchKernelGGL((kernel<64, true>), dim3(grid), dim3(256), 0, stream, args);                \
-    else hipLaunchKernelGGL((kernel<64, false>), dim3(grid), dim3(256), 0, stream, args);                                      \
+    if ((cfg).head_dim == 128 && (cfg).interleaved) hipLaunchKernelGGL((kernel<128, true>), dim3(grid), dim3(threads), 0, stream, args);   \
+    else if ((cfg).head_dim == 128) hipLaunchKernelGGL((kernel<128, false>), dim3(grid), dim3(threads), 0, stream, args);          \
+    else if ((cfg).interleaved) hipLaunchKernelGGL((kernel<64, true>), dim3(grid), dim3(threads), 0, stream, args);                \
+    else hipLaunchKernelGGL((kernel<64, false>), dim3(grid), dim3(threads), 0, stream, args);                                      \
   } while (0)
 
 hipError_t launch_head_rows(const HeadRows& r, void* k_out, hipStream_t s) {
   HeadArgs a = head_args(r, k_out != nullptr, false);
   a.k_out = (char*)k_out;
   if (!k_out) a.hkv = 0;
-  FLUX_HEADS(head_rows_kernel, r.cfg, wgs_for(a), s, a);
+  FLUX_HEADS(head_rows_kernel, r.cfg, wgs_for(a), 256, s, a);
   return hipGetLastError();
 }
 
@@ -624,7 +650,7 @@ hipError_t launch_qkv_append(const Ctx& c, const HeadRows& r, const flux_kv_cach
   a.counter = c.counters + 0;
   a.gather = c.append_counters;
   a.status = c.status;
-  FLUX_HEADS(qkv_rows_kernel, r.cfg, wgs_for(a), s, a);
+  FLUX_HEADS(qkv_rows_kernel, r.cfg, wgs_for(a), 256, s, a);
   return hipGetLastError();
 }
 
@@ -646,9 +672,11 @@ hipError_t launch_qkv_append_paged(const Ctx& c, const HeadRows& r, const flux_p
   const long long tiles = ((long long)r.total + 63) / 64;
   a.share = 0;
   while (a.share < 7 && ((1 << a.share) < r.cfg.n_kv_heads ? tiles << a.share < kQuantMost : tiles << a.share < kQuantWgs)) ++a.share;
-  a.kv_wgs = (unsigned)(tiles << (a.share + 1));             // (at most 2^25: total <= 2^30)
-  const unsigned q_wgs = a.h.passes > 0 ? wgs_for(a.h) : 0;
-  FLUX_HEADS(qkv_quant_kernel, r.cfg, a.kv_wgs + q_wgs, s, a);
+  a.kv_wgs = (unsigned)(tiles << (a.share + 1));
+  const int waves = quant_waves(r.cfg.head_dim);
+  const long long q_wgs = a.h.passes > 0 ? ((long long)r.total * a.h.waves + waves - 1) / waves : 0;
+  const unsigned grid = a.kv_wgs + (unsigned)(q_wgs < kHeadMost ? q_wgs : kHeadMost);
+  FLUX_HEADS(qkv_quant_kernel, r.cfg, grid, 64 * waves, s, a);
   return hipGetLastError();
 }
 

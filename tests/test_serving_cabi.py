@@ -58,7 +58,7 @@ def test_heads(F, nodev, kind):
         assert call(cu=None) == call(mx=-1) == call(mx=6) == call(kc=cache_struct(F, k=None)) == call(kc=cache_struct(F, stride_t=64)) == F.FLUX_EINVAL
         assert call(t=100, mx=65) == F.FLUX_ECAPACITY
     else:
-        assert call(slots=None) == call(head(F, n_kv_heads=1 << 20), rows(F, stride_k=1 << 27, stride_v=1 << 27), t=1 << 17) == F.FLUX_EINVAL
+        assert call(slots=None) == call(t=(1 << 27) + 1) == F.FLUX_EINVAL and call(t=1 << 27) == F.FLUX_EHIP
         for kw in BAD_POOLS:
             assert call(kv=pool(F, **kw)) == F.FLUX_EINVAL, kw
 
