@@ -367,13 +367,15 @@ __device__ __forceinline__ void scale_down(char* at, float down) {
   }
   *(u32x4*)at = c;
 }
+typedef __attribute__((__vector_size__(2 * sizeof(double)))) double f64x2;
 __device__ __forceinline__ double value_of(const u32x4* x, int j) {
   const uint32_t u = x[j >> 3][(j & 7) >> 1];
   return (double)(j & 1 ? bf16_hi(u) : bf16_lo(u));
 }
-// The 16 values of a lane normed and turned, in 64 bits, pair by pair (which keeps registers free).
-template <int LPR, bool NEAR>
-__device__ __forceinline__ void key_values(const HeadArgs& a, const u32x4* x, const u32x4* w, int i, int pos, bool norm, bool turns, uint32_t* hi) {
+// The 16 values of a lane normed and turned, in 64 bits, pair by pair (which keeps registers free).  `angles`: this thread's eight sines and cosines in
+// LDS, THREADS apart; they are worked out where `fresh`, else found there.
+template <int LPR, bool NEAR, int THREADS>
+__device__ __forceinline__ void key_values(const HeadArgs& a, const u32x4* x, const u32x4* w, int i, int pos, bool norm, bool turns, bool fresh, f64x2* angles, uint32_t* hi) {
   double inv = 1.0;
   if (norm) {
     double sum = 0.0;
@@ -381,10 +383,19 @@ __device__ __forceinline__ void key_values(const HeadArgs& a, const u32x4* x, co
     for (int j = 0; j < 16; ++j) sum = __builtin_fma(value_of(x, j), value_of(x, j), sum);
     inv = 1.0 / __builtin_sqrt(row_sum<LPR>(sum) * (1.0 / (16 * LPR)) + (double)a.eps);
   }
-  f32x4 freq[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  if (turns) {
-    freq[0] = *(const f32x4*)(a.freq + 8 * i);
-    freq[1] = *(const f32x4*)(a.freq + 8 * i + 4);
+  if (fresh && a.rot != 0) {
+    f32x4 freq[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    if (turns) {
+      freq[0] = *(const f32x4*)(a.freq + 8 * i);
+      freq[1] = *(const f32x4*)(a.freq + 8 * i + 4);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      double s, c;
+      sincos_turn(turn_of(pos, freq[j >> 2][j & 3]), s, c);
+      angles[j * THREADS] = f64x2{s, c};
+      if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -395,8 +406,8 @@ __device__ __forceinline__ void key_values(const HeadArgs& a, const u32x4* x, co
       q = q * inv * value_of(w, v);
     }
     if (a.rot != 0) {
-      double s, c;
-      sincos_turn(turn_of(pos, freq[j >> 2][j & 3]), s, c);
+      const f64x2 turn = angles[j * THREADS];
+      const double s = turn[0], c = turn[1];
       const double p1 = __builtin_fma(-q, s, p * c), q1 = __builtin_fma(p, s, q * c);
       // (a dimension that is not turned is not touched by the other, whatever that is)
       p = turns ? p1 : p;
@@ -491,9 +502,9 @@ __device__ __forceinline__ uint32_t block_max(uint32_t y, bool alone, uint32_t* 
 }
 
 // One launch: K and V, then the queries.  What bounds it: a decode step its latencies (slots, rows, the arithmetic of 64 bits), a long prompt the
-// memory and that arithmetic together.  us, 32/8 heads of 128: 64 sequences with a row each 6.3, 256 10.3, 1024 31, 1024 rows of one 17, 4096
-// 30, 16384 111 (3.3 TB/s; three waves per SIMD: with the registers of two 120).  Keys from 32 bits, worked out again in 64 where 32 do not settle a
-// code, in launches of their own for queries, keys and values: 108 for the 16384 rows, 38 for the 4096.
+// memory and that arithmetic together.  A workgroup with several heads of a block works their angles out once and keeps them in LDS.  us, 32/8 heads of 128:
+// 64 sequences with a row each 6.9, 256 10.5, 1024 rows of one 13, 4096 28, 16384 91 (4.1 TB/s; 118 with angles for every head).  Keys from 32 bits,
+// worked out again in 64 where 32 do not settle a code, took 108 for the 16384 rows in launches of their own for queries, keys and values.
 constexpr int quant_waves(int head_dim) { return head_dim == 128 ? 8 : 4; }   // of a workgroup: a row per D / 16 lanes, 64 rows in all
 template <int D, bool NEAR>
 __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(QuantArgs a) {
@@ -511,7 +522,9 @@ __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(Quant
     return;
   }
   __shared__ uint32_t tops[2][W];
+  __shared__ f64x2 s_angles[8 * 64 * W];
   int turn_of = 0;                                           // (blocks take turns with the words: a barrier each)
+  int angles_of = -1;                                        // the block whose angles this wave has in LDS
   const int i = l % LPR;
   const int tile = (int)(blockIdx.x >> (a.share + 1));
   const bool is_v = (blockIdx.x >> a.share) & 1, norm = !is_v && a.h.k_norm != nullptr;
@@ -575,7 +588,8 @@ __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(Quant
           wp[0] = *(const u32x4*)(a.h.k_norm + 2 * c0);
           wp[1] = *(const u32x4*)(a.h.k_norm + 2 * c1);
         }
-        key_values<LPR, NEAR>(a.h, x, wp, i, pos, norm, turns, val);
+        key_values<LPR, NEAR, 64 * W>(a.h, x, wp, i, pos, norm, turns, angles_of != at, s_angles + threadIdx.x, val);
+        angles_of = at;
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = max(top, finite_or_zero(val[j]));
       }
@@ -667,11 +681,8 @@ hipError_t launch_qkv_append_paged(const Ctx& c, const HeadRows& r, const flux_p
   a.stride_t = kv.stride_t;
   a.slots = slots;
   a.n_pages = kv.n_pages;
-  // Workgroups per tile: as many as there are heads, for blocks that fill the tile, and more where that makes few of them, for tiles of
-  // many short blocks
   const long long tiles = ((long long)r.total + 63) / 64;
-  a.share = 0;
-  while (a.share < 7 && ((1 << a.share) < r.cfg.n_kv_heads ? tiles << a.share < kQuantMost : tiles << a.share < kQuantWgs)) ++a.share;
+  a.share = quant_share(tiles, r.cfg.n_kv_heads);
   a.kv_wgs = (unsigned)(tiles << (a.share + 1));
   const int waves = quant_waves(r.cfg.head_dim);
   const long long q_wgs = a.h.passes > 0 ? ((long long)r.total * a.h.waves + waves - 1) / waves : 0;
