@@ -420,7 +420,7 @@ int flux_qkv_append(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_kv_cache
                     const int32_t* cu_new, int total_new, int max_new, const int32_t* positions, void* q_out, void* stream);
 
 /* flux_qk_norm_rope and flux_kv_append_paged in one pass: queries go to q_out (or both NULL), keys and values are quantised into their
- * slots; slots, scales, limits and FLUX_DEV_BAD_PAGE as in flux_kv_append_paged.  A key's code is rounded once, from the value that the
+ * slots; slots, scales and FLUX_DEV_BAD_PAGE as in flux_kv_append_paged, total_new <= 2^27.  A key's code is rounded once, from the value that the
  * formula names.  positions: dev int32 [total_new] (rotary_dim 0: not used).  Every row of q_out is written, whatever its slot is. */
 int flux_qkv_append_paged(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_paged_kv* kv, const flux_qkv_rows* in,
                           const int32_t* slots, const int32_t* positions, int total_new, void* q_out, void* stream);
@@ -439,7 +439,7 @@ int flux_qkv_append_paged(flux_ctx* ctx, const flux_head_cfg* cfg, const flux_pa
  *   free_pages[n_free - 1 - j] (after those that went back were listed), and copies[j] = {page, its copy, n(b) % 64} (dev int32 [batch, 3]); *n_copies
  *   (dev int32) is their number, and entries behind them are left as they were.  flux_page_copy then copies them in each layer, before
  *   anything is appended.  Where the free pages do not suffice, such a sequence is cut to whole pages and FLUX_DEV_KV_OVERFLOW is raised.
- * Limits as in flux_page_release.  The partials of the workspace hold 4 bytes per page (FLUX_EWORKSPACE).  Parents outside the batch count as -1 and lengths
+ * Limits as in flux_page_release.  Of pools of more than 16384 pages the workspace holds 4 bytes per page beside what flux_create asks for at least (FLUX_EWORKSPACE; the default does).  Parents outside the batch count as -1 and lengths
  * outside the table are cut (FLUX_DEV_BAD_LENGTH); table entries outside the pool are not counted, are given on as -1 and raise FLUX_DEV_BAD_PAGE,
  * as does a page that more rows lost than had it by `shares` (it goes back all the same). */
 int flux_page_fork(flux_ctx* ctx, const flux_page_table* pt, int32_t* shares, const int32_t* parent, const int32_t* keep_len,
@@ -449,8 +449,8 @@ int flux_page_fork(flux_ctx* ctx, const flux_page_table* pt, int32_t* shares, co
  * the former, at most max_moves times.  moves[j] = {from, to, 64} (dev int32 [max_moves, 3]), *n_moves (dev int32) their number, entries behind
  * them left as they were.  Tables and shares (NULL: nobody shares pages) follow; the free pages are listed again, the highest number first, so that
  * the lowest is taken first.  flux_page_copy then moves the codes in each layer (no page is both moved from and to), before the next attention or append call.  After a call with
- * enough moves the pages in use are 0 .. n_pages - n_free - 1.  n_pages <= 2^20, batch <= FLUX_MAX_PAGED_BATCH; the partials of the workspace hold 4 bytes per page
- * (FLUX_EWORKSPACE).  Numbers in the list outside the pool, or listed twice, are dropped from it and raise FLUX_DEV_BAD_PAGE, as do table entries outside the
+ * enough moves the pages in use are 0 .. n_pages - n_free - 1.  n_pages <= 2^20, batch <= FLUX_MAX_PAGED_BATCH; the workspace holds 36 bytes per 256 pages
+ * beside what flux_create asks for at least (FLUX_EWORKSPACE; the default does).  Numbers in the list outside the pool, or listed twice, are dropped from it and raise FLUX_DEV_BAD_PAGE, as do table entries outside the
  * pool (left as they were). */
 int flux_page_compact(flux_ctx* ctx, const flux_page_table* pt, int32_t* shares, int32_t* moves, int max_moves, int32_t* n_moves,
                       void* stream);
@@ -466,10 +466,11 @@ int flux_page_copy(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int h
  * (dev int32 [batch+1]); cu_q NULL: max_q_len rows each, one sequence behind the other.  out dev [T, n_q_heads, head_dim] in cfg->out_dtype; cfg->n_sink, window and
  * sa_block are not used.  max_q_len, max_kv_len: host upper bounds (rows and keys beyond them are left out and raise FLUX_DEV_BAD_LENGTH; looser ones cost idle
  * workgroups).  Rows without any key are zero; rows of no sequence are left as they were.  With cu_q NULL and max_q_len 1 (a decode step) the
- * call is worked on like flux_attn_decode and needs the workspace that flux_workspace_needed names; any other call takes what there is.
+ * call is worked on like flux_attn_decode and needs the workspace that flux_workspace_needed names (a length above the capacity counts as the capacity there,
+ * and is not reported); any other call takes what there is.
  * Weights are rounded to bf16 as in flux_attn_prefill (a decode step: as in flux_attn_decode), cached rows below kv_len[b] must be finite, those of V up to 2^64.
  * Keys of a tile of rows may be shared out over workgroups, in a way that depends on the bounds and lengths of up to 64 sequences side by side.
- * batch * max_q_len < 2^31 where cu_q is NULL; 64 * n_kv_heads * ceil(max_q_len * group / 64) <= 2^28 (FLUX_EINVAL). */
+ * batch * max_q_len < 2^31 where cu_q is NULL; min(batch, 64) * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^23 is always enough (FLUX_EINVAL). */
 int flux_attn_cross(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
                     const flux_kv_cache* cache, void* out, void* stream);
 

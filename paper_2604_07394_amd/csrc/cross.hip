@@ -81,7 +81,8 @@ __device__ __forceinline__ CrossUnit cross_plan(const CrossArgs& a, int wg, int 
   if (a.part_units > 0) {
     const int t_all = wave_total(tiles) * a.hkv;
     if (t_all < resident) {
-      const float work = (float)wave_total(tiles * nb) * (float)a.hkv, share = work / (float)resident;
+      // (blocks of all tiles pass 32 bits in caches of 10^8 rows: their low 12 bits and the rest apart)
+      const float work = ((float)wave_total(tiles * (nb & 4095)) + 4096.0f * (float)wave_total(tiles * (nb >> 12))) * (float)a.hkv, share = work / (float)resident;
       float best = 1e30f;
 #pragma unroll
       for (int i = 0; i < 9; ++i) {

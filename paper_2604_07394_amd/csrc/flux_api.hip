@@ -597,7 +597,7 @@ int flux_page_copy(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int h
                    void* stream) {
   if (!ctx || !copies || max_copies < 0 || max_copies > (1 << 24)) return FLUX_EINVAL;
   if (head_dim != 64 && head_dim != 128) return FLUX_EINVAL;
-  if (n_kv_heads <= 0) return FLUX_EINVAL;
+  if (n_kv_heads <= 0 || n_kv_heads > (1 << 20)) return FLUX_EINVAL;
   const int rc = check_paged_kv(kv, head_dim);
   if (rc != FLUX_OK) return rc;
   if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
@@ -618,9 +618,10 @@ int flux_attn_cross(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, cons
   if (max_q_len < 0 || max_kv_len < 0) return FLUX_EINVAL;
   if (max_kv_len > cache->capacity) return FLUX_ECAPACITY;
   if (!aligned16(q) || !aligned16(out)) return FLUX_EINVAL;
-  // rows and workgroups are counted in 32 bits
+  // rows and the threads of a launch are counted in 32 bits
   const long long rows = (long long)max_q_len * (cfg->n_q_heads / cfg->n_kv_heads);
-  if ((rows + 63) / 64 > (1 << 22) / cfg->n_kv_heads) return FLUX_EINVAL;
+  if ((rows + 63) / 64 > (1 << 23) / cfg->n_kv_heads) return FLUX_EINVAL;
+  if (plan_cross(*cfg, cache->batch, max_q_len, max_kv_len, ctx->c.partials_bytes).wgs > kCrossMostWgs) return FLUX_EINVAL;
   if (!cu_q && (long long)cache->batch * max_q_len > 0x7FFFFFFFll) return FLUX_EINVAL;
   if (!cu_q && max_q_len == 1) {
     // a decode step: a ring of all rows of the cache, which sees all that it holds

@@ -517,6 +517,7 @@ __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(Quant
       const int64_t t = u / a.h.waves;
       HeadArgs q = a.h;
       q.hkv = 0;
+      q.k_norm = nullptr;                                    // (its registers)
       token_rows<D, NEAR, false>(q, t, [&]() { return a.h.rot ? a.h.pos[t] : 0; }, (int)(u - t * a.h.waves), l, [&](int) { return (char*)nullptr; }, [&](int) { return (char*)nullptr; });
     }
     return;

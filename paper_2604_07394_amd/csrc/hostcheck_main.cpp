@@ -17,6 +17,9 @@ extern "C" int hostcheck_decode_in_partials(const flux_attn_cfg* cfg, int batch,
 extern "C" int hostcheck_decode_blocks_fit(const flux_attn_cfg* cfg, int batch, int max_kv_len);
 extern "C" int hostcheck_decode_rows_fit(const flux_attn_cfg* cfg, int batch, int max_kv_len);
 extern "C" int hostcheck_paged_rows_fit(const flux_attn_cfg* cfg, int batch, int max_q_len, int max_kv_len, int* wgs, int* waves);
+extern "C" int hostcheck_cross_fits(const flux_attn_cfg* cfg, int batch, int max_q_len, int max_kv_len, long long* wgs);
+extern "C" int hostcheck_quant(int total, int hkv, int* share);
+extern "C" int hostcheck_head_waves(int total, int passes);
 extern "C" int hostcheck_append(int batch, int hkv, int d, int total_new, int max_new, int ring, int window, unsigned* wgs);
 
 static int failures = 0;
@@ -227,6 +230,58 @@ int main() {
               EXPECT(hostcheck_paged_rows_fit(&c, batch, q, k, &wgs, &waves), 1);
               EXPECT(wgs >= 1 && wgs <= (waves == 8 ? 256 : 512), 1);
             }
+  }
+  // ---- heads, pages that change hands, cross attention
+  {
+    flux_head_cfg hc = {8, 2, 128, 128, 0, 1e-6f, p, p, (float*)buf};
+    flux_qkv_rows rows = {p, p, p, 12 * 128, 12 * 128, 12 * 128};
+    char* other = buf + 4096;
+    flux_page_table pt = {pi, pi, pi, pi, 2, 4, 8};
+    flux_paged_kv kv = {p, p, (float*)buf, (float*)buf, 2 * 64 * 128, 64 * 128, 128, 8};
+    EXPECT(flux_qk_norm_rope(ctx, &hc, &rows, pi, 5, other, other, nullptr), FLUX_EHIP);
+    EXPECT(flux_qk_norm_rope(ctx, &hc, &rows, pi, INT_MAX, other, other, nullptr), FLUX_EINVAL);
+    EXPECT(flux_qk_norm_rope(ctx, &hc, &rows, nullptr, 5, other, other, nullptr), FLUX_EINVAL);
+    EXPECT(flux_qk_norm_rope(ctx, &hc, &rows, pi, 5, p, other, nullptr), FLUX_EINVAL);
+    EXPECT(flux_qk_norm_rope(ctx, nullptr, &rows, pi, 5, other, other, nullptr), FLUX_EINVAL);
+    EXPECT(flux_qkv_append(ctx, &hc, &kc, &rows, pi, 5, 5, nullptr, other, nullptr), FLUX_EHIP);
+    EXPECT(flux_qkv_append(ctx, &hc, &kc, &rows, pi, 1 << 30, 1 << 30, nullptr, other, nullptr), FLUX_ECAPACITY);
+    EXPECT(flux_qkv_append(ctx, &hc, nullptr, &rows, pi, 5, 5, nullptr, other, nullptr), FLUX_EINVAL);
+    EXPECT(flux_qkv_append_paged(ctx, &hc, &kv, &rows, pi, pi, 5, other, nullptr), FLUX_EHIP);
+    EXPECT(flux_qkv_append_paged(ctx, &hc, &kv, &rows, pi, pi, INT_MAX, other, nullptr), FLUX_EINVAL);
+    EXPECT(flux_qkv_append_paged(ctx, &hc, nullptr, &rows, pi, pi, 5, other, nullptr), FLUX_EINVAL);
+    rows.stride_k = INT64_MAX;                               // (not a multiple of 8)
+    EXPECT(flux_qkv_append_paged(ctx, &hc, &kv, &rows, pi, pi, 5, other, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_fork(ctx, &pt, pi, pi, pi, pi, pi, nullptr), FLUX_EHIP);
+    EXPECT(flux_page_fork(ctx, &pt, pi, nullptr, nullptr, pi, pi, nullptr), FLUX_EHIP);
+    EXPECT(flux_page_fork(ctx, nullptr, pi, pi, pi, pi, pi, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_compact(ctx, &pt, nullptr, pi, INT_MAX, pi, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_compact(ctx, &pt, nullptr, pi, 1 << 24, pi, nullptr), FLUX_EHIP);
+    EXPECT(flux_page_copy(ctx, &kv, 2, 128, pi, pi, INT_MAX, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_copy(ctx, &kv, INT_MAX, 128, pi, pi, 1 << 24, nullptr), FLUX_EINVAL);
+    EXPECT(flux_page_copy(ctx, &kv, 2, 128, pi, pi, 1 << 24, nullptr), FLUX_EHIP);
+    EXPECT(flux_attn_cross(ctx, &cfg, p, pi, 64, 64, &kc, p, nullptr), FLUX_EHIP);
+    EXPECT(flux_attn_cross(ctx, &cfg, p, nullptr, 1, 64, &kc, p, nullptr), FLUX_EHIP);
+    EXPECT(flux_attn_cross(ctx, &cfg, p, nullptr, INT_MAX, 64, &kc, p, nullptr), FLUX_EINVAL);
+    EXPECT(flux_attn_cross(ctx, &cfg, p, pi, INT_MAX, 64, &kc, p, nullptr), FLUX_EINVAL);
+    EXPECT(flux_attn_cross(ctx, &cfg, p, pi, 64, INT_MAX, &kc, p, nullptr), FLUX_ECAPACITY);
+    long long wgs;
+    int share;
+    const int heads[][2] = {{32, 8}, {28, 4}, {8, 2}, {1, 1}, {16, 1}, {64, 64}, {96, 1}, {256, 2}, {4096, 4096}};
+    for (int d : {64, 128})
+      for (const auto& h : heads)
+        for (int batch : {1, 2, 13, 63, 64, 65, 500, 70000})
+          for (int k : {0, 1, 64, 129, 2001, 131072, 1 << 30})
+            for (int q : {1, 2, 5, 16, 17, 64, 300, 40000, 1 << 20}) {
+              flux_attn_cfg c = {h[0], h[1], d, 4, 16, 0.f, 0, 0};
+              if (((long long)q * (h[0] / h[1]) + 63) / 64 > (1 << 23) / h[1]) continue;
+              EXPECT(hostcheck_cross_fits(&c, batch, q, k, &wgs), 1);
+            }
+    for (int hkv : {1, 2, 8, 17, 1 << 20})
+      for (int total : {1, 63, 64, 65, 1000, 8192, 16384, 1 << 20, 1 << 27}) {
+        EXPECT(hostcheck_quant(total, hkv, &share), 1);
+        EXPECT(share >= 0 && share <= 7, 1);
+        for (int passes : {1, 2, 6, 100}) EXPECT(hostcheck_head_waves(total, passes) >= 1 && hostcheck_head_waves(total, passes) <= passes, 1);
+      }
   }
   EXPECT(flux_destroy(ctx), FLUX_OK);
   EXPECT(flux_destroy(nullptr), FLUX_EINVAL);

@@ -53,6 +53,26 @@ int hostcheck_paged_rows_fit(const flux_attn_cfg* cfg, int batch, int max_q_len,
   }
   return fits;
 }
+// a call of cross attention: whether the rows of its parts end within the partials, and its launches stay below 2^32 threads where they are
+// not refused; workgroups
+int hostcheck_cross_fits(const flux_attn_cfg* cfg, int batch, int max_q_len, int max_kv_len, long long* wgs) {
+  bool fits = true;
+  for (size_t room = 4096; room <= (size_t)1 << 28; room *= 4) {
+    const flux::CrossPlan p = flux::plan_cross(*cfg, batch, max_q_len, max_kv_len, room);
+    *wgs = p.wgs;
+    const long long rows = (long long)max_q_len * (cfg->n_q_heads / cfg->n_kv_heads);
+    fits = fits && p.info_bytes % 16 == 0 && (long long)p.tiles * p.bm >= rows && p.wgs >= p.part_units && (p.bm > 32 || p.tiles <= 1);
+    if (p.part_units > 0) fits = fits && p.info_bytes + (size_t)p.part_units * p.bm * (cfg->head_dim + 2) * sizeof(float) <= room && (long long)cfg->n_kv_heads * p.tiles <= 65535;
+  }
+  return fits;
+}
+// an append into pages: workgroups for K and V, and whether all that such a launch has stays below 2^32 threads
+int hostcheck_quant(int total, int hkv, int* share) {
+  const long long tiles = ((long long)total + 63) / 64;
+  *share = flux::quant_share(tiles, hkv);
+  return ((tiles << (*share + 1)) + flux::kHeadMost) * 512 < 1ll << 32;
+}
+int hostcheck_head_waves(int total, int passes) { return flux::head_waves(total, passes); }
 int hostcheck_decode_rows_fit(const flux_attn_cfg* cfg, int batch, int max_kv_len) {
   const flux::DecodePlan p = flux::plan_decode(*cfg, batch, max_kv_len);
   const size_t rows = (size_t)2 * p.wgs * p.rpu * (cfg->head_dim + 2) * sizeof(float);
