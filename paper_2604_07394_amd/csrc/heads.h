@@ -20,9 +20,8 @@ hipError_t launch_qkv_append_paged(const Ctx& c, const HeadRows& r, const flux_p
 
 constexpr int kHeadWaves = 8192;            // waves that a launch takes where a token's heads can be shared out over so many
 constexpr int kHeadMost = 1 << 20;          // workgroups for queries that such a launch takes at most
-// Workgroups for K, and for V, up to which a tile of 64 rows has several of them: one per head at most, and more where that leaves few.  us with up to 128 / 256 /
-// 512 of either kind, 8 heads of 128: 512 rows of one sequence 7.9 / 10.7 / 12.3, 2048 19.8 / 19.3 / 26, 4096 33 / 28 / 31, 16384 91 / 91 / 93; 256
-// sequences with a row each 11.5 / 10.3 / 10.6, 1024 37 / 32 / 28.
+// Workgroups for K, and for V, up to which a tile of 64 rows has several of them: one per head at most, and up to kQuantFewWgs also more.  us with 256 and 128
+// / 512 and 256, 8 heads of 128: 512 rows of one sequence 7.4 / 9.1, 1024 12.0 / 11.6, 1500 12.5 / 15.8, 4096 22 / 24, 16384 79 / 82.
 constexpr int kQuantWgs = 256, kQuantFewWgs = 128;
 inline int quant_share(long long tiles, int hkv) {
   int share = 0;

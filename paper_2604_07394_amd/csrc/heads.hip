@@ -352,10 +352,16 @@ typedef __attribute__((__vector_size__(2 * sizeof(uint16_t)))) uint16_t u16x2;
 __device__ __forceinline__ uint32_t pair_max(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
+// Largest of a wave's: within rows of 16 lanes, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t max_moved(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false)); }
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, off));
-  return x;
+  x = max_moved<0x111, 0xf>(x);
+  x = max_moved<0x112, 0xf>(x);
+  x = max_moved<0x114, 0xf>(x);
+  x = max_moved<0x118, 0xf>(x);
+  x = max_moved<0x142, 0xa>(x);
+  return (uint32_t)__builtin_amdgcn_readlane((int)max_moved<0x143, 0xc>(x), 63);
 }
 // 16 codes of a page that takes a larger scale.
 __device__ __forceinline__ void scale_down(char* at, float down) {
@@ -465,45 +471,78 @@ __device__ __forceinline__ int nth_set(uint64_t x, int n) {
   return at;
 }
 
-// What a workgroup of W waves has of its tile's (block, head) pairs, which 2^share workgroups look after: pairs of up to 64 / W rows, what
-// a wave holds at a time, go to single waves, the others to a whole workgroup.  one(at, slot, rows, head, alone)
-template <int W, typename F>
-__device__ __forceinline__ void for_blocks(const QuantArgs& a, int tile, int turn, int l, int w, F one) {
+// What a workgroup of W waves has of its tile's (block, head) pairs, which 2^share workgroups look after: a wave holds 64 / W rows at a time, so blocks of
+// one row go to a wave for as many heads at once (kSingle), other blocks of up to 64 / W rows to a wave per head (kAlone), the rest to a whole workgroup per
+// head (kShared).  one(pair, rows, how): while it is worked on, what fetch(pair, how) asks for of the next pair is on its way.
+enum { kSingle, kAlone, kShared };
+struct Pair {
+  int at, slot, rows, head;       // row of the tile where the block begins, its slot; rows of the block; head, or first of them
+};
+struct Rows {                     // of a lane
+  u32x4 x[2];
+  int pos;
+  float old;                      // scale that the page has
+};
+template <int W, typename G, typename F>
+__device__ __forceinline__ void for_blocks(const QuantArgs& a, int tile, int turn, int l, int w, G fetch, F one) {
   const Tile x = load_tile(a, tile * 64, l);
   const int mine = block_rows(x, l), hkv = a.h.hkv;
   const bool begins = (x.begins >> l) & 1, in_pool = (x.slot >> 6) < a.n_pages;
   if (turn == 0 && w == 0 && __builtin_amdgcn_ballot_w64(begins && !in_pool) != 0 && l == 0) atomicOr(a.h.status, (uint32_t)FLUX_DEV_BAD_PAGE);
-  const uint64_t short_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine <= 64 / W);
+  const uint64_t single_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine == 1);
+  const uint64_t short_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine > 1 && mine <= 64 / W);
   const uint64_t long_ones = __builtin_amdgcn_ballot_w64(begins && in_pool && mine > 64 / W);
 #pragma unroll 1
-  for (int phase = 0; phase < 2; ++phase) {
-    const bool alone = phase == 0;
-    const uint64_t set = alone ? short_ones : long_ones;
+  for (int how = kSingle; how <= kShared; ++how) {
+    const bool alone = how != kShared;
+    const uint64_t set = how == kSingle ? single_ones : (alone ? short_ones : long_ones);
     const int sharers = (alone ? W : 1) << a.share, me = alone ? W * turn + w : turn;
-    const int64_t pairs = (int64_t)__builtin_popcountll(set) * hkv;
+    const int per = how == kSingle ? (hkv + 64 / W - 1) / (64 / W) : hkv;          // of a block
+    const int64_t pairs = (int64_t)__builtin_popcountll(set) * per;
+    auto nth = [&](int64_t pair) __attribute__((always_inline)) {
+      const int block = (int)((uint32_t)pair / (uint32_t)per), at = __builtin_amdgcn_readfirstlane(nth_set(set, block)), head = (int)pair - block * per;
+      return Pair{at, __builtin_amdgcn_readlane(x.slot, at), __builtin_amdgcn_readlane(mine, at), how == kSingle ? head * (64 / W) : head};
+    };
+    if (me >= pairs) continue;
+    Pair now = nth(me);
+    Rows rows = fetch(now, how);
 #pragma unroll 1
     for (int64_t pair = me; pair < pairs; pair += sharers) {
-      const int block = (int)((uint32_t)pair / (uint32_t)hkv), at = __builtin_amdgcn_readfirstlane(nth_set(set, block));
-      one(at, __builtin_amdgcn_readlane(x.slot, at), __builtin_amdgcn_readlane(mine, at), (int)pair - block * hkv, alone);
+      Pair next = now;
+      Rows next_rows = rows;
+      if (pair + sharers < pairs) {
+        next = nth(pair + sharers);
+        next_rows = fetch(next, how);
+      }
+      one(now, rows, how);
+      now = next;
+      rows = next_rows;
     }
   }
 }
-// Largest of what the lanes of a wave (alone), or of the workgroup, have.
-template <int W>
-__device__ __forceinline__ uint32_t block_max(uint32_t y, bool alone, uint32_t* words, int l, int w) {
+// Largest of what the lanes of a row (kSingle), of a wave (kAlone) or of the workgroup have.
+template <int W, int LPR>
+__device__ __forceinline__ uint32_t block_max(uint32_t y, int how, uint32_t* words, int l, int w) {
+  if (how == kSingle) {
+    y = max(y, (uint32_t)__builtin_amdgcn_mov_dpp((int)y, 0xB1, 0xf, 0xf, true));  // as in row_sum
+    y = max(y, (uint32_t)__builtin_amdgcn_mov_dpp((int)y, 0x4E, 0xf, 0xf, true));
+    if constexpr (LPR == 8) y = max(y, (uint32_t)__builtin_amdgcn_mov_dpp((int)y, 0x141, 0xf, 0xf, true));
+    return y;
+  }
   y = wave_max(y);
-  if (!alone) {
+  if (how == kShared) {
     if (l == 0) words[w] = y;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < W; ++i) y = max(y, words[i]);
   }
-  return (uint32_t)__builtin_amdgcn_readfirstlane(y);
+  return y;
 }
 
-// One launch: K and V, then the queries.  What bounds it: a decode step its latencies (slots, rows, the arithmetic of 64 bits), a long prompt the
+// One launch: K, V, then the queries.  What bounds it: a decode step its latencies (slots, rows, the arithmetic of 64 bits), a long prompt the
 // memory and that arithmetic together.  A workgroup with several heads of a block works their angles out once and keeps them in LDS.  us, 32/8 heads of 128:
-// 64 sequences with a row each 6.9, 256 10.5, 1024 rows of one 13, 4096 28, 16384 91 (4.1 TB/s; 118 with angles for every head).  Keys from 32 bits,
+// 64 sequences with a row each 6.5, 256 6.7, 1024 8.6 (a wave per head of each row: 35), 1024 rows of one 12.3, 4096 24, 16384 80 (369 MB, 4.6 TB/s; 118 with
+// angles for every head, 89 with rows that are asked for when they are needed and K and V in turn).  Keys from 32 bits,
 // worked out again in 64 where 32 do not settle a code, took 108 for the 16384 rows in launches of their own for queries, keys and values.
 constexpr int quant_waves(int head_dim) { return head_dim == 128 ? 8 : 4; }   // of a workgroup: a row per D / 16 lanes, 64 rows in all
 template <int D, bool NEAR>
@@ -527,25 +566,38 @@ __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(Quant
   int turn_of = 0;                                           // (blocks take turns with the words: a barrier each)
   int angles_of = -1;                                        // the block whose angles this wave has in LDS
   const int i = l % LPR;
-  const int tile = (int)(blockIdx.x >> (a.share + 1));
-  const bool is_v = (blockIdx.x >> a.share) & 1, norm = !is_v && a.h.k_norm != nullptr;
+  // K first, which takes longer (K and V in turn give all of K to every other XCD: 16384 rows 85 us for 79)
+  const unsigned half = a.kv_wgs >> 1;
+  const bool is_v = blockIdx.x >= half;
+  const unsigned wg = blockIdx.x - (is_v ? half : 0);
+  const int tile = (int)(wg >> a.share);
+  const bool norm = !is_v && a.h.k_norm != nullptr;
   int c0 = 16 * i, c1 = 16 * i + 8;
   bool turns = false;
   if (!is_v) lane_places<NEAR>(i, a.h.rot, c0, c1, turns);
   const int64_t src_step = is_v ? a.h.stride_v : a.h.stride_k;
-  for_blocks<W>(a, tile, blockIdx.x & ((1 << a.share) - 1), l, w, [&](int at, int slot, int rows, int h, bool alone) __attribute__((always_inline)) {
-    const int t0 = tile * 64 + at, page = slot >> 6, held = slot & 63, part = alone ? 0 : w, parts = alone ? 1 : W, r = RPW * part + l / LPR;
-    const char* src = (is_v ? a.h.v : a.h.k) + (int64_t)(t0 + r) * src_step + (int64_t)h * D * 2;
+  auto fetch = [&](const Pair b, int how) __attribute__((always_inline)) {
+    const int r = how == kSingle ? 0 : RPW * (how == kShared ? w : 0) + l / LPR, h = b.head + (how == kSingle ? l / LPR : 0);
+    const int t = tile * 64 + b.at;
+    Rows y = {{{0, 0, 0, 0}, {0, 0, 0, 0}}, 0, 0.f};         // (rows that the block does not have count as zeros)
+    if (r < b.rows && h < a.h.hkv) {
+      const char* src = (is_v ? a.h.v : a.h.k) + (int64_t)(t + r) * src_step + (int64_t)h * D * 2;
+      y.x[0] = *(const u32x4*)(src + 2 * c0);
+      y.x[1] = *(const u32x4*)(src + 2 * c1);
+      if (turns) y.pos = a.h.pos[t + r];
+    }
+    if ((b.slot & 63) != 0 && h < a.h.hkv) y.old = (is_v ? a.v_scale : a.k_scale)[(int64_t)(b.slot >> 6) * a.h.hkv + h];
+    return y;
+  };
+  for_blocks<W>(a, tile, (int)(wg & ((1u << a.share) - 1)), l, w, fetch, [&](const Pair b, const Rows& y, int how) __attribute__((always_inline)) {
+    const bool single = how == kSingle, alone = how != kShared;
+    const int at = b.at, page = b.slot >> 6, held = b.slot & 63, h = b.head + (single ? l / LPR : 0), pos = y.pos;
+    const int part = alone ? 0 : w, r = single ? 0 : RPW * part + l / LPR;
+    const bool has = r < b.rows && h < a.h.hkv;              // a row of its own
     float* const scale_at = (is_v ? a.v_scale : a.k_scale) + (int64_t)page * a.h.hkv + h;
     char* const dst = (is_v ? a.v : a.k) + (int64_t)page * a.stride_p + (int64_t)h * a.stride_h;
-    u32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};               // (rows that the block does not have count as zeros)
-    int pos = 0;
-    if (r < rows) {
-      x[0] = *(const u32x4*)(src + 2 * c0);
-      x[1] = *(const u32x4*)(src + 2 * c1);
-      if (turns) pos = a.h.pos[t0 + r];
-    }
-    const float old = held != 0 ? *scale_at : 0.f;
+    const u32x4 (&x)[2] = y.x;
+    const float old = y.old;
     float scale, inv;                                        // (inv: exact, a power of two)
     turn_of ^= alone ? 0 : 1;
     if (is_v) {
@@ -562,7 +614,7 @@ __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(Quant
           most = pair_max(most, (lo < 0x7F80u ? lo : 0u) | (hi < 0x7F80u ? hi << 16 : 0u));
         }
       }
-      most = block_max<W>(max(most & 0xFFFFu, most >> 16), alone, tops[turn_of], l, w);
+      most = block_max<W, LPR>(max(most & 0xFFFFu, most >> 16), how, tops[turn_of], l, w);
       // most = (1 + f / 128) 2^(E - 127): see block_scale
       const int e = max((int)(most >> 7) - 135 + ((most & 127) > 96 ? 1 : 0), kMinScaleExp);
       scale = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
@@ -578,12 +630,12 @@ __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(Quant
       u32x4 codes;
 #pragma unroll
       for (int j = 0; j < 4; ++j) codes[j] = codes4(f[4 * j] * inv, f[4 * j + 1] * inv, f[4 * j + 2] * inv, f[4 * j + 3] * inv);
-      if (r < rows) *(u32x4*)(dst + (int64_t)(held + r) * a.stride_t + c0) = codes;
+      if (has) *(u32x4*)(dst + (int64_t)(held + r) * a.stride_t + c0) = codes;
     } else {
       uint32_t val[16], top = 0;
 #pragma unroll
       for (int j = 0; j < 16; ++j) val[j] = 0;
-      if (RPW * part < rows) {                               // (uniform)
+      if (RPW * part < b.rows) {                             // (uniform)
         u32x4 wp[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
         if (norm) {
           wp[0] = *(const u32x4*)(a.h.k_norm + 2 * c0);
@@ -594,14 +646,16 @@ __global__ __launch_bounds__(64 * quant_waves(D), 4) void qkv_quant_kernel(Quant
 #pragma unroll
         for (int j = 0; j < 16; ++j) top = max(top, finite_or_zero(val[j]));
       }
-      top = block_max<W>(top, alone, tops[turn_of], l, w);
+      top = block_max<W, LPR>(top, how, tops[turn_of], l, w);
       scale = block_scale(top, old);
       inv = 1.0f / scale;
-      if (r < rows) put_codes(dst + (int64_t)(held + r) * a.stride_t, c0, c1, codes16(val, (double)inv));
+      if (has) put_codes(dst + (int64_t)(held + r) * a.stride_t, c0, c1, codes16(val, (double)inv));
     }
-    if (held != 0 && scale > old)                            // the rows that the page holds take the new scale too
-      for (int y = RPW * part + l / LPR; y < held; y += parts * RPW) scale_down(dst + (int64_t)y * a.stride_t + 16 * i, old * inv);
-    if (l == 0 && part == 0 && (held == 0 || scale > old)) *scale_at = scale;
+    if (held != 0 && scale > old && h < a.h.hkv) {           // the rows that the page holds take the new scale too
+      const int step = single ? 1 : (alone ? RPW : RPW * W);
+      for (int y = r; y < held; y += step) scale_down(dst + (int64_t)y * a.stride_t + 16 * i, old * inv);
+    }
+    if (i == 0 && r == 0 && has && (held == 0 || scale > old)) *scale_at = scale;
   });
 }
 

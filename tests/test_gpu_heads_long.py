@@ -52,6 +52,9 @@ def paged_case(F, ctx, t, new, first, hq, hkv, d, rot, near, norm, seed=0, check
     ([8, 9] * 40, [0] * 80, 3, 17, 64, 64, 0, False),                    # blocks about as long as one wave takes alone, an odd number of heads
     ([16, 17, 7] * 12, [50] * 36, 3, 17, 128, 48, 1, True),
     ([70], [3], 1, 40, 64, 0, 0, True),
+    ([1] * 130, [(i * 5) % 64 for i in range(130)], 2, 17, 64, 64, 0, True),      # single rows, heads that do not fill the last wave
+    ([1, 2, 1, 9, 1, 1] * 9, [(i * 7) % 64 for i in range(54)], 1, 11, 128, 64, 1, True),
+    ([1] * 40, [63, 0] * 20, 3, 24, 128, 0, 0, False),
     ([8192 + 31], [17], 1, 1, 64, 64, 0, True),                          # as many tiles as workgroups side by side, and more
     ([8100, 8300], [0, 40], 1, 2, 128, 128, 0, True),
     ([1] * 64 + [16500], list(range(64)) + [9], 1, 3, 64, 64, 0, False),
