@@ -190,6 +190,8 @@ __device__ __forceinline__ void fetch_tile(const char* kt, const char* vt, const
   }
 }
 
+// Bound by the matrix pipe (two thirds of the cycles of the CUs' SIMDs) and the vector instructions beside it: four sequences of 1000 to 5000 rows on 4001 to
+// 9000 keys, 32 and 8 heads of 128 (986 GFLOP), 767 to 814 us from box to box, 1.21 to 1.29 PFLOP/s.
 template <int D, int QB>
 __global__ __launch_bounds__(256, 2) void cross_tile_kernel(CrossArgs a) {
   constexpr int WR = 16 * QB, BM = 4 * WR, BN = 64;
@@ -462,7 +464,8 @@ __global__ __launch_bounds__(256, 2) void cross_tile_kernel(CrossArgs a) {
 
 // Short runs: the rows of a KV head fit one or two blocks of 16 columns (a decode step of several beams, say), and a call is bound by the
 // bytes of K and V.  The four waves of a workgroup take blocks of 32 keys in turn, K from memory into the MFMA's operand, V through
-// LDS of their own, each block asked for while the one before is worked on, and join their rows in the end.
+// LDS of their own, each block asked for while the one before is worked on, and join their rows in the end.  16 sequences of five rows on 1500 keys, 8
+// heads of 64 (49 MB): 13.4 us of which the streaming is about 9, and 2.5 for the joining launch.
 template <int D, int QB>
 __global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
   constexpr int BM = 16 * QB, KC = D / 32, DB = D / 16, CPR = D / 8, ROWB = 2 * D, VL = 32 * CPR / 64;

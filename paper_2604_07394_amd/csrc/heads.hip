@@ -222,6 +222,8 @@ __device__ __forceinline__ void token_rows(const HeadArgs& a, int64_t t, PP posi
   }
 }
 
+// A wave per token, or several where tokens are few.  Bound by the memory: 32768 tokens of 32 and 8 heads of 128 (671 MB) 124 us, 5.4 TB/s; 16 of 8 and 2 of 64
+// 2.8, which is a launch and its two waits.
 template <int D, bool NEAR>
 __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -248,7 +250,8 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int t, 
 }
 
 // The contiguous cache: row r of sequence b goes to position kv_len[b] + r.  All waves read the lengths; the last workgroup to have read
-// them moves them on (see kv_append.hip).
+// them moves them on (see kv_append.hip).  Five chunks of 129 to 3001 tokens, 28 and 4 heads of 128 (120 MB): 25 us, 4.8 TB/s; a step of 16
+// sequences 4.8, in which the sequence of a row, its length and the arrivals wait for each other.
 template <int D, bool NEAR>
 __global__ __launch_bounds__(256) void qkv_rows_kernel(HeadArgs a) {
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
