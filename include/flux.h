@@ -464,7 +464,7 @@ int flux_page_copy(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int h
 /* ---- Cross attention: every query row of sequence b sees all kv_len[b] keys of its cache (the states of an encoder, written by flux_kv_append or
  * flux_qkv_append), whatever the number of queries.  q dev bf16 [T, n_q_heads, head_dim], rows of sequence b are cu_q[b] .. cu_q[b+1]-1
  * (dev int32 [batch+1]); cu_q NULL: max_q_len rows each, one sequence behind the other.  out dev [T, n_q_heads, head_dim] in cfg->out_dtype; cfg->n_sink, window and
- * sa_block are not used.  max_q_len, max_kv_len: host upper bounds (rows and keys beyond them are left out and raise FLUX_DEV_BAD_LENGTH; looser ones cost idle
+ * sa_block have to be valid and are not used.  max_q_len, max_kv_len: host upper bounds (rows and keys beyond them are left out and raise FLUX_DEV_BAD_LENGTH; looser ones cost idle
  * workgroups).  Rows without any key are zero; rows of no sequence are left as they were.  With cu_q NULL and max_q_len 1 (a decode step) the
  * call is worked on like flux_attn_decode and needs the workspace that flux_workspace_needed names (a length above the capacity counts as the capacity there,
  * and is not reported); any other call takes what there is.

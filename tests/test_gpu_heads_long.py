@@ -145,3 +145,21 @@ def test_captured_appends(F, ctx):
         at = at + 1
         assert lens.tolist() == at.tolist()
     assert F.flux_last_device_status(ctx) == 0
+
+
+def test_single_rows_without_norm_as_the_plain_call(F, ctx):
+    """One row of many sequences, values that are not finite among them, pages that take a larger scale: the pages of flux_kv_append_paged, bit for bit."""
+    t, hkv = 70, 11
+    for d in (64, 128):
+        _, x, _, _ = rows(d, t, 1, hkv, d)
+        x[3, 1, 7], x[40, 2, 9], x[66, 13, 0], x[69, 22, 1], x[5, 12, :] = np.inf, np.nan, -np.inf, 1e30, 300.0
+        dev, _ = bf16(x)
+        k, v = dev[:, 1:1 + hkv], dev[:, 1 + hkv:]
+        slots = i32([64 * i + (i * 11) % 64 for i in range(t)])
+        a, _, _ = pool_of(F, 1, t, hkv, d)
+        b, _, _ = pool_of(F, 1, t, hkv, d)
+        F.flux_qkv_append_paged(ctx, F.head_cfg(1, hkv, d), a, None, k, v, slots, None, t, None)
+        F.flux_kv_append_paged(ctx, b, hkv, d, k.contiguous(), v.contiguous(), slots, t)
+        for p, q in ((a.k, b.k), (a.v, b.v)):
+            assert bool(((p == q) | (((p & 0x7F) == 0x7F) & ((q & 0x7F) == 0x7F))).all())     # (the sign of NaN is nobody's)
+        assert torch.equal(a.k_scale, b.k_scale) and torch.equal(a.v_scale, b.v_scale)
