@@ -465,7 +465,7 @@ __global__ __launch_bounds__(256, 2) void cross_tile_kernel(CrossArgs a) {
 // Short runs: the rows of a KV head fit one or two blocks of 16 columns (a decode step of several beams, say), and a call is bound by the
 // bytes of K and V.  The four waves of a workgroup take blocks of 32 keys in turn, K from memory into the MFMA's operand, V through
 // LDS of their own, each block asked for while the one before is worked on, and join their rows in the end.  16 sequences of five rows on 1500 keys, 8
-// heads of 64 (49 MB): 13.4 us of which the streaming is about 9, and 2.5 for the joining launch.
+// heads of 64 (49 MB): 13.2 us of which the streaming is about 9, and 2.3 for the joining launch.
 template <int D, int QB>
 __global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
   constexpr int BM = 16 * QB, KC = D / 32, DB = D / 16, CPR = D / 8, ROWB = 2 * D, VL = 32 * CPR / 64;
@@ -644,13 +644,16 @@ __global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
 template <int D, int BM>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   constexpr int RPW = 1024 / D;
-  if (a.info[-1][0] == 0) return;                            // no tile was
   const int b = blockIdx.z, d = 4 * (threadIdx.x % (D / 4));
+  const int kvh = blockIdx.y / a.n_tiles, tile = blockIdx.y - kvh * a.n_tiles, x = (int)blockIdx.x * RPW + threadIdx.x / (D / 4);
+  // (asked for together; what stands in a tile's entry counts only if it has rows)
+  const int any = a.info[-1][0];
+  const i32x4 info = a.info[((int64_t)b * a.hkv + kvh) * a.n_tiles + tile];
   const int q_begin = a.cu ? a.cu[b] : (a.first + b) * a.q_len, n_q = a.cu ? min(a.cu[b + 1] - q_begin, a.q_len) : a.q_len;
   const int64_t n_rows = (int64_t)n_q * a.group;
-  const int kvh = blockIdx.y / a.n_tiles, tile = blockIdx.y - kvh * a.n_tiles, x = (int)blockIdx.x * RPW + threadIdx.x / (D / 4);
+  asm volatile("" : : "v"(any), "v"(info));
+  if (any == 0) return;                                      // no tile was
   if ((int64_t)tile * BM + (int64_t)blockIdx.x * RPW >= n_rows) return;
-  const i32x4 info = a.info[((int64_t)b * a.hkv + kvh) * a.n_tiles + tile];
   const int parts = info[2];
   const int64_t row = (int64_t)tile * BM + x;
   if (parts < 2 || row >= n_rows) return;
