@@ -9,6 +9,7 @@ constexpr int kCrossBatch = 64;             // sequences of a launch: a lane loo
 constexpr int kCrossMaxUnits = 1024;        // units of a launch whose tiles may be shared out (or one per tile, where those are more)
 constexpr int kCrossMostWgs = 1 << 23;      // workgroups of a launch: fewer than 2^32 threads
 constexpr int kCrossRunWgs = 512;           // workgroups of short runs that the chip holds at once
+constexpr int kCrossJoinWgs = 4096;         // workgroups that join at most (24576 that find nothing to do take 11 us, 4096 take 3)
 constexpr int cross_resident(int head_dim) { return 256 * (head_dim == 128 ? 2 : 3); }   // workgroups that the chip holds at once
 
 struct CrossPlan {

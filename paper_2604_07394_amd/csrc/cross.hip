@@ -644,49 +644,52 @@ __global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
 template <int D, int BM>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   constexpr int RPW = 1024 / D;
-  const int b = blockIdx.z, d = 4 * (threadIdx.x % (D / 4));
-  const int kvh = blockIdx.y / a.n_tiles, tile = blockIdx.y - kvh * a.n_tiles, x = (int)blockIdx.x * RPW + threadIdx.x / (D / 4);
-  // (asked for together; what stands in a tile's entry counts only if it has rows)
-  const int any = a.info[-1][0];
-  const i32x4 info = a.info[((int64_t)b * a.hkv + kvh) * a.n_tiles + tile];
-  const int q_begin = a.cu ? a.cu[b] : (a.first + b) * a.q_len, n_q = a.cu ? min(a.cu[b + 1] - q_begin, a.q_len) : a.q_len;
-  const int64_t n_rows = (int64_t)n_q * a.group;
-  asm volatile("" : : "v"(any), "v"(info));
-  if (any == 0) return;                                      // no tile was
-  if ((int64_t)tile * BM + (int64_t)blockIdx.x * RPW >= n_rows) return;
-  const int parts = info[2];
-  const int64_t row = (int64_t)tile * BM + x;
-  if (parts < 2 || row >= n_rows) return;
-  const int64_t r0 = (int64_t)info[0] * BM + x, step = (int64_t)info[1] * BM;
-  float m = -INFINITY, den = 0.f;
-  f32x4 num = {0.f, 0.f, 0.f, 0.f};
-  for (int c0 = 0; c0 < parts; c0 += 4) {                    // four at a time, their loads together (the last one again where there are fewer)
-    float mc[4], lc[4];
-    f32x4 oc[4];
+  constexpr int CHUNKS = BM < RPW ? 1 : BM / RPW;            // of a tile
+  const int d = 4 * (threadIdx.x % (D / 4)), tiles = a.hkv * a.n_tiles, any = a.info[-1][0];
+  for (int unit = blockIdx.x; unit < CHUNKS * tiles * a.batch; unit += gridDim.x) {
+    const int at = unit / CHUNKS, b = at / tiles, kvh = (at - b * tiles) / a.n_tiles, tile = at - b * tiles - kvh * a.n_tiles;
+    const int x0 = (unit - at * CHUNKS) * RPW, x = x0 + threadIdx.x / (D / 4);
+    // (asked for together; what stands in a tile's entry counts only if it has rows)
+    const i32x4 info = a.info[at];
+    const int q_begin = a.cu ? a.cu[b] : (a.first + b) * a.q_len, n_q = a.cu ? min(a.cu[b + 1] - q_begin, a.q_len) : a.q_len;
+    const int64_t n_rows = (int64_t)n_q * a.group;
+    asm volatile("" : : "v"(any), "v"(info));
+    if (any == 0) return;                                    // no tile was
+    if ((int64_t)tile * BM + x0 >= n_rows) continue;
+    const int parts = info[2];
+    const int64_t row = (int64_t)tile * BM + x;
+    if (parts < 2 || row >= n_rows) continue;
+    const int64_t r0 = (int64_t)info[0] * BM + x, step = (int64_t)info[1] * BM;
+    float m = -INFINITY, den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = 0; c0 < parts; c0 += 4) {                  // four at a time, their loads together (the last one again where there are fewer)
+      float mc[4], lc[4];
+      f32x4 oc[4];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int64_t r = r0 + min(c0 + v, parts - 1) * step;
-      mc[v] = c0 + v < parts ? a.part_ml[2 * r] : -INFINITY;
-      lc[v] = a.part_ml[2 * r + 1];
-      oc[v] = *(const f32x4*)(a.part_o + r * D + d);
-    }
-    const float top = fmaxf(fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])), m);
-    if (top == -INFINITY) continue;
-    const float al = fast_exp2((m - top) * a.scale_log2);
-    den *= al;
-    num *= al;
-    m = top;
+      for (int v = 0; v < 4; ++v) {
+        const int64_t r = r0 + min(c0 + v, parts - 1) * step;
+        mc[v] = c0 + v < parts ? a.part_ml[2 * r] : -INFINITY;
+        lc[v] = a.part_ml[2 * r + 1];
+        oc[v] = *(const f32x4*)(a.part_o + r * D + d);
+      }
+      const float top = fmaxf(fmaxf(fmaxf(mc[0], mc[1]), fmaxf(mc[2], mc[3])), m);
+      if (top == -INFINITY) continue;
+      const float al = fast_exp2((m - top) * a.scale_log2);
+      den *= al;
+      num *= al;
+      m = top;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const float p = fast_exp2((mc[v] - m) * a.scale_log2);
-      den += p * lc[v];
-      num += p * oc[v];
+      for (int v = 0; v < 4; ++v) {
+        const float p = fast_exp2((mc[v] - m) * a.scale_log2);
+        den += p * lc[v];
+        num += p * oc[v];
+      }
     }
+    const float inv = 1.0f / den;
+    const int64_t off = ((int64_t)(q_begin + row / a.group) * a.hq + (int64_t)kvh * a.group + row % a.group) * D + d;
+    if (a.out_fp32) *(f32x4*)((float*)a.out + off) = num * inv;
+    else *(u32x2*)((__bf16*)a.out + off) = u32x2{pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv)};
   }
-  const float inv = 1.0f / den;
-  const int64_t off = ((int64_t)(q_begin + row / a.group) * a.hq + (int64_t)kvh * a.group + row % a.group) * D + d;
-  if (a.out_fp32) *(f32x4*)((float*)a.out + off) = num * inv;
-  else *(u32x2*)((__bf16*)a.out + off) = u32x2{pack_bf16(num[0] * inv, num[1] * inv), pack_bf16(num[2] * inv, num[3] * inv)};
 }
 
 namespace {
@@ -697,8 +700,9 @@ hipError_t launch_one(const CrossArgs& a, hipStream_t s) {
   if (a.part_units == 0) return hipGetLastError();
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int RPW = 1024 / D, rows = BM < RPW ? RPW : BM;
-  hipLaunchKernelGGL((cross_join_kernel<D, BM>), dim3(rows / RPW, a.hkv * a.n_tiles, a.batch), dim3(256), 0, s, a);
+  constexpr int RPW = 1024 / D, chunks = BM < RPW ? 1 : BM / RPW;
+  const int units = chunks * a.hkv * a.n_tiles * a.batch;    // (below 2^31: see kCrossMostWgs)
+  hipLaunchKernelGGL((cross_join_kernel<D, BM>), dim3(units < kCrossJoinWgs ? units : kCrossJoinWgs), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <int D>
