@@ -191,7 +191,7 @@ __device__ __forceinline__ void fetch_tile(const char* kt, const char* vt, const
 }
 
 // Bound by the matrix pipe (two thirds of the cycles of the CUs' SIMDs) and the vector instructions beside it: four sequences of 1000 to 5000 rows on 4001 to
-// 9000 keys, 32 and 8 heads of 128 (986 GFLOP), 767 to 814 us from box to box, 1.21 to 1.29 PFLOP/s.
+// 9000 keys, 32 and 8 heads of 128 (986 GFLOP), 767 to 858 us from box to box, 1.15 to 1.29 PFLOP/s.
 template <int D, int QB>
 __global__ __launch_bounds__(256, 2) void cross_tile_kernel(CrossArgs a) {
   constexpr int WR = 16 * QB, BM = 4 * WR, BN = 64;
