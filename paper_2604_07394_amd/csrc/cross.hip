@@ -8,8 +8,9 @@
 //                                for its maximum first
 //     O^T[d][row]  += V^T . p    the accumulators of two blocks of 16 keys are this product's operand as they are; V^T comes
 //                                from row-major LDS through the transposing read
-// K and V go to LDS without passing through registers, one block ahead.  Weights are rounded to bf16 (2^-9 of one at most), and the
-// denominator sums the rounded ones.  Where the tiles are few, the keys of a tile are shared out over several workgroups, and
+// K and V go to LDS without passing through registers, one block ahead.  The tiles' weights are rounded to bf16 (by 2^-8 of one at most), and the
+// denominator sums the rounded ones, as in prefill.hip: a second term each would be half as many MFMAs again, in a kernel that the matrix pipe bounds.
+// Where the tiles are few, the keys of a tile are shared out over several workgroups, and
 // their unnormalised rows joined by a second launch.  Every workgroup finds out from the lengths which unit it is.
 #include "cross.h"
 
@@ -552,7 +553,10 @@ __global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     if (j0 < k1) load_block(j0);                             // (its registers have been read by now)
     __builtin_amdgcn_sched_barrier(0);
-    bf16x8 pf[QB];
+    // A weight is the sum of two bf16 values, its upper bits and what they leave of it, to 2^-16 of it as in decode.hip: rows of several beams are scored as a
+    // decode step scores one, and the matrix pipe is idle while a block arrives.  (2-norm of the error with fp32 outputs 1.2e-3 with one bf16 value, below 1.2e-5
+    // with two; the call of the 49 MB above 16.0 us with either.)
+    bf16x8 pf[QB], pr[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       if (left < 32) {
@@ -571,18 +575,20 @@ __global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
       // (a row whose scores are all -inf so far refers to 0)
       const float ref = top == -INFINITY ? 0.f : top, al = fast_exp2((m[qb] - ref) * a.scale_log2), mneg = -ref * a.scale_log2;
       m[qb] = top;
-      const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-      uint32_t pk[4];
+      uint32_t pk[4], rest[4];
       float add = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        pk[t] = pack_bf16(fast_exp2(__builtin_fmaf(s[t >> 1][qb][2 * (t & 1)], a.scale_log2, mneg)), fast_exp2(__builtin_fmaf(s[t >> 1][qb][2 * (t & 1) + 1], a.scale_log2, mneg)));
-        add = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk[t]), ones, add, false);
+        const float p0 = fast_exp2(__builtin_fmaf(s[t >> 1][qb][2 * (t & 1)], a.scale_log2, mneg)), p1 = fast_exp2(__builtin_fmaf(s[t >> 1][qb][2 * (t & 1) + 1], a.scale_log2, mneg));
+        pk[t] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, p1), __builtin_bit_cast(uint32_t, p0), 0x07060302u);
+        rest[t] = pack_bf16(p0 - bf16_lo(pk[t]), p1 - bf16_hi(pk[t]));
+        add += p0 + p1;
       }
       sum[qb] = __builtin_fmaf(sum[qb], al, add);
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db][qb] *= al;
       pf[qb] = __builtin_bit_cast(bf16x8, u32x4{pk[0], pk[1], pk[2], pk[3]});
+      pr[qb] = __builtin_bit_cast(bf16x8, u32x4{rest[0], rest[1], rest[2], rest[3]});
     }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -590,7 +596,10 @@ __global__ __launch_bounds__(256, 2) void cross_run_kernel(CrossArgs a) {
       const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FLUX_LDS bf16x4*)(vs + v_rd[db] + 16 * ROWB));
       const bf16x8 vf = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-      for (int qb = 0; qb < QB; ++qb) o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qb], o[db][qb], 0, 0, 0);
+      for (int qb = 0; qb < QB; ++qb) {
+        o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qb], o[db][qb], 0, 0, 0);
+        o[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pr[qb], o[db][qb], 0, 0, 0);
+      }
     }
   }
   // the waves' rows: references and sums first
