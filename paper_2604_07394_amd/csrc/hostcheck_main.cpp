@@ -20,6 +20,7 @@ extern "C" int hostcheck_paged_rows_fit(const flux_attn_cfg* cfg, int batch, int
 extern "C" int hostcheck_cross_fits(const flux_attn_cfg* cfg, int batch, int max_q_len, int max_kv_len, long long* wgs);
 extern "C" int hostcheck_quant(int total, int hkv, int* share);
 extern "C" int hostcheck_head_waves(int total, int passes);
+extern "C" int hostcheck_fork_last(int entry, int n_pages, int own, int* left);
 extern "C" int hostcheck_append(int batch, int hkv, int d, int total_new, int max_new, int ring, int window, unsigned* wgs);
 
 static int failures = 0;
@@ -276,6 +277,13 @@ int main() {
               if (((long long)q * (h[0] / h[1]) + 63) / 64 > (1 << 23) / h[1]) continue;
               EXPECT(hostcheck_cross_fits(&c, batch, q, k, &wgs), 1);
             }
+    for (int n_pages : {1, 16, 16384, 16385, 1 << 24})
+      for (int own : {0, 1})
+        for (int entry : {0, n_pages - 1, n_pages, n_pages + 1, INT_MAX, -1, -7, INT_MIN}) {
+          int left;
+          EXPECT(hostcheck_fork_last(entry, n_pages, own, &left), 1);
+          EXPECT(left, entry >= 0 && entry < n_pages ? entry : -1);
+        }
     for (int hkv : {1, 2, 8, 17, 1 << 20})
       for (int total : {1, 63, 64, 65, 1000, 8192, 16384, 1 << 20, 1 << 27}) {
         EXPECT(hostcheck_quant(total, hkv, &share), 1);

@@ -73,6 +73,14 @@ int hostcheck_quant(int total, int hkv, int* share) {
   return ((tiles << (*share + 1)) + flux::kHeadMost) * 512 < 1ll << 32;
 }
 int hostcheck_head_waves(int total, int passes) { return flux::head_waves(total, passes); }
+// a fork's last place of a row that keeps two places, the second of them partly filled, with `entry` there, which nobody else has: what the table holds
+// then, and whether the holders that are looked up for it are those of a page of the pool, or none are
+int hostcheck_fork_last(int entry, int n_pages, int own, int* left) {
+  const int before = (uint32_t)entry < (uint32_t)n_pages ? entry : -1;             // (what the first part holds of it)
+  *left = flux::fork_writes(1, own ? 2 : 0, 2, own != 0, before) ? before : entry;
+  const int page = flux::page_of_entry(*left, n_pages);
+  return page < n_pages;                                     // (below 0: not looked up)
+}
 int hostcheck_decode_rows_fit(const flux_attn_cfg* cfg, int batch, int max_kv_len) {
   const flux::DecodePlan p = flux::plan_decode(*cfg, batch, max_kv_len);
   const size_t rows = (size_t)2 * p.wgs * p.rpu * (cfg->head_dim + 2) * sizeof(float);

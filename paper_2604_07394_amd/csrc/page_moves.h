@@ -12,6 +12,12 @@ constexpr int kCompactPages = 1 << 20;      // pages of a pool that one workgrou
 constexpr int kCopyWgs = 8192;              // workgroups that copy at most
 static_assert(kForkEntries >= 4 * FLUX_MAX_PAGED_BATCH, "four columns of the table fit");
 
+// An entry of a table as a page of the pool; -1: none.
+constexpr int page_of_entry(int entry, int n_pages) { return (uint32_t)entry < (uint32_t)n_pages ? entry : -1; }
+// Whether a fork writes a place of a row that had `had` places and goes on with `has`, of its own (`own`) or another row's; `before`: the page there, -1:
+// none.  A page that a row keeps of its own stays as it is; a number outside the pool there becomes -1 like any other.
+constexpr bool fork_writes(int place, int had, int has, bool own, int before) { return place < (had > has ? had : has) && (!own || place >= has || before < 0); }
+
 // Bytes of the partials that the calls take: what every workgroup found and how much, or a bit per page and a count per 256.
 inline size_t fork_bytes(int n_pages) {
   if (n_pages <= kForkAlone) return 0;

@@ -181,11 +181,9 @@ __global__ __launch_bounds__(1024) void page_fork_kernel(MoveArgs a) {
       for (int u = 0; u < 4; ++u) {
         const int i = i0 + 1024 * u;
         if (i >= entries) continue;
-        if ((uint32_t)page[u] >= (uint32_t)a.n_pages) {
-          if ((int)c0 + (i & (cols - 1)) < s_old[i >> shift]) bad_page = FLUX_DEV_BAD_PAGE;
-          page[u] = -1;
-        }
-        s_work[i] = page[u];
+        const int in_pool = page_of_entry(page[u], a.n_pages);
+        if (in_pool < 0 && (int)c0 + (i & (cols - 1)) < s_old[i >> shift]) bad_page = FLUX_DEV_BAD_PAGE;
+        s_work[i] = in_pool;
       }
     }
     __syncthreads();
@@ -196,7 +194,7 @@ __global__ __launch_bounds__(1024) void page_fork_kernel(MoveArgs a) {
         if (before >= 0) atomicSub(a.shares + before, 1);
         if (now >= 0) atomicAdd(a.shares + now, 1);
       }
-      if (c < max(s_old[b], has) && (p != b || c >= has)) put(a.table + (int64_t)b * a.table_pages + c, now);
+      if (fork_writes(c, s_old[b], has, p == b, before)) put(a.table + (int64_t)b * a.table_pages + c, now);
     }
     __syncthreads();
   }
@@ -229,7 +227,7 @@ __global__ __launch_bounds__(1024) void page_fork_kernel(MoveArgs a) {
 #pragma unroll
   for (int i = 0; i < kMine; ++i) {
     const int b = tid + 1024 * i;
-    page[i] = b < a.batch && (s_len[b] & 63) != 0 ? get(a.table + (int64_t)b * a.table_pages + (s_len[b] >> 6)) : -1;
+    page[i] = b < a.batch && (s_len[b] & 63) != 0 ? page_of_entry(get(a.table + (int64_t)b * a.table_pages + (s_len[b] >> 6)), a.n_pages) : -1;
   }
   const int n_free = *a.n_free, avail = clampi(n_free, 0, a.n_pages);
   if (n_free != avail) bad |= FLUX_DEV_BAD_LENGTH;
@@ -329,7 +327,7 @@ __global__ __launch_bounds__(1024) void page_fork_end_kernel(MoveArgs a) {
 #pragma unroll
   for (int i = 0; i < kMine; ++i) {
     const int b = tid + 1024 * i;
-    page[i] = b < a.batch && (s_len[b] & 63) != 0 ? a.table[(int64_t)b * a.table_pages + (s_len[b] >> 6)] : -1;
+    page[i] = b < a.batch && (s_len[b] & 63) != 0 ? page_of_entry(a.table[(int64_t)b * a.table_pages + (s_len[b] >> 6)], a.n_pages) : -1;
   }
 #pragma unroll
   for (int i = 0; i < kMine; ++i) shares[i] = page[i] >= 0 ? get(a.shares + page[i]) : 0;
