@@ -158,7 +158,8 @@ __global__ __launch_bounds__(1024) void page_fork_kernel(MoveArgs a) {
   int most = 0;
   for (int b = tid; b < a.batch; b += 1024) {
     int p;
-    const int n = goes_on(a, b, p, bad), had = (clampi(a.kv_len[b], 0, a.table_pages << 6) + 63) >> 6;
+    const int n = goes_on(a, b, p, bad), got = a.kv_len[b], len = clampi(got, 0, a.table_pages << 6), had = (len + 63) >> 6;
+    if (got != len) bad |= FLUX_DEV_BAD_LENGTH;              // (whoever goes on with it)
     s_old[b] = had;
     s_len[b] = n;
     s_parent[b] = p;

@@ -1,4 +1,5 @@
-"""Forks of tables that hold numbers outside the pool: such an entry counts as no page, whoever goes on with it, and is never looked up."""
+"""Forks and compactions of tables that hold numbers outside the pool, or lengths outside the table: such an entry counts as no page, whoever goes on with
+it, and is never looked up; the status says so."""
 import pytest
 import torch
 
@@ -58,3 +59,20 @@ def test_fork_with_an_entry_outside_the_pool(F, ctx, n_pages, which, parent, pla
     gone = sorted((first[b] for b in range(4) if b not in who and b != 1), reverse=True)
     free = free + gone
     assert pt.free_pages.tolist()[:int(pt.n_free)] == (free[:-1] if copied else free)
+
+
+@pytest.mark.parametrize("n_pages", [16, 20000])
+@pytest.mark.parametrize("length", [257, 1 << 30, -1])
+@pytest.mark.parametrize("parent", [[0, 0, 2, 3], [0, -1, 2, 3], [0, 1, 2, 3], [1, 0, 2, 3]])
+def test_fork_with_a_length_outside_the_table(F, ctx, n_pages, length, parent):
+    """Sequence 1 has it: reported whether or not anybody goes on with what it holds."""
+    pt, shares, o, _ = state(F, [(0, [10, 256, 64, 5])], 4, n_pages, 5)
+    had = [int(pt.table[b, 0]) for b in range(4)]
+    pt.kv_len[1] = length
+    cut = min(max(length, 0), 256)
+    copies, n = torch.full((4, 3), -9, dtype=torch.int32, device="cuda"), i32([-9])
+    F.flux_page_fork(ctx, pt, shares, i32(parent), None, copies, n)
+    assert F.flux_last_device_status(ctx) == F.FLUX_DEV_BAD_LENGTH
+    lens = [10, cut, 64, 5]
+    assert pt.kv_len.tolist() == [lens[p] if p >= 0 else 0 for p in parent]
+    assert [int(pt.table[b, 0]) for b in (2, 3)] == had[2:]
