@@ -521,8 +521,7 @@ __global__ __launch_bounds__(1024) void page_renumber_kernel(MoveArgs a) {
     else if ((bits >> l) & 1) nth = free_below(page) - moves;
     if (nth >= 0) a.free_pages[free_all - 1 - nth] = page;
   }
-  if (moves == 0) return;
-  uint32_t bad = 0;
+  uint32_t bad = 0;                                          // (entries are looked at where no page moves, too: an error in them is reported either way)
   for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
     if (b != (int)blockIdx.x) len = a.kv_len[b];
     const int pages = (clampi(len, 0, a.table_pages << 6) + 63) >> 6;

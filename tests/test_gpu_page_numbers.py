@@ -76,3 +76,21 @@ def test_fork_with_a_length_outside_the_table(F, ctx, n_pages, length, parent):
     lens = [10, cut, 64, 5]
     assert pt.kv_len.tolist() == [lens[p] if p >= 0 else 0 for p in parent]
     assert [int(pt.table[b, 0]) for b in (2, 3)] == had[2:]
+
+
+@pytest.mark.parametrize("n_pages", [5, 300, 70000])
+@pytest.mark.parametrize("which", range(5))
+def test_compact_with_an_entry_outside_the_pool_where_nothing_moves(F, ctx, n_pages, which):
+    pt, _, _, _ = state(F, [(0, [10, 200])], 5, n_pages, 3)
+    pt.table[:, :] = i32([[0, -1, -1, -1, -1], [1, 2, 3, 4, -1]])
+    pt.free_pages[:n_pages - 5] = torch.arange(5, n_pages, dtype=torch.int32, device="cuda")
+    pt.n_free[0] = n_pages - 5
+    moves, n = torch.full((16, 3), -9, dtype=torch.int32, device="cuda"), i32([-9])
+    for bad in (False, True):
+        if bad:
+            pt.table[1, 2] = numbers(n_pages)[which]
+        before = pt.table.clone()
+        F.flux_page_compact(ctx, pt, None, moves, n)
+        assert F.flux_last_device_status(ctx) == (F.FLUX_DEV_BAD_PAGE if bad else 0)
+        assert n.tolist() == [0] and bool((moves == -9).all()) and torch.equal(pt.table, before)
+        assert pt.free_pages.tolist()[:n_pages - 5] == list(range(n_pages - 1, 4, -1)) and int(pt.n_free) == n_pages - 5
