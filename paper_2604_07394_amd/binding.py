@@ -425,32 +425,45 @@ def _head_arg(hc):
     return hc.packed if type(hc) is HeadCfg else C.byref(hc)
 
 
-def _row_stride(x):
-    """Elements between the token rows of a tensor [T, heads, head_dim] whose heads lie next to each other."""
+def _row_stride(x, heads=None, head_dim=None, total=0):
+    """Elements between the token rows of a tensor [total or more, heads, head_dim] whose heads lie next to each other."""
     t, h, d = x.shape
     stride, between, one = x.stride()
     assert one == 1 and (between == d or h == 1) and x.dtype is _bf16
+    assert t >= total and (heads is None or (h == heads and d == head_dim))
     return stride if t > 1 else h * d                        # (of a single row torch may say anything)
 
 
-def _rows_arg(q, k, v):
-    """The bytes of a FluxQKVRows.  (Written out for each of the three: in a loop it took 3.2 us, of the 5.5 of a call, and takes 2.4.)"""
+def _rows_arg(q, k, v, hc=None, total=0):
+    """The bytes of a FluxQKVRows, of `total` rows of the heads that hc names (None: not looked at).  (Written out for each of the three: in a loop it took 0.8 us more,
+    of some 6 of a call; looking at the rows and heads takes 0.4.)"""
+    hq, hkv, d = (None, None, None) if hc is None else (hc.n_q_heads, hc.n_kv_heads, hc.head_dim)
     return _pack_rows(q.data_ptr() if q is not None else 0, k.data_ptr() if k is not None else 0, v.data_ptr() if v is not None else 0,
-                      _row_stride(q) if q is not None else 0, _row_stride(k) if k is not None else 0, _row_stride(v) if v is not None else 0)
+                      _row_stride(q, hq, d, total) if q is not None else 0, _row_stride(k, hkv, d, total) if k is not None else 0,
+                      _row_stride(v, hkv, d, total) if v is not None else 0)
+
+
+def _rows_out(x, elements):
+    """The address of a result that has room for so many elements."""
+    if x is None or type(x) is int:
+        return x
+    assert x.numel() >= elements
+    return x.data_ptr()
 
 
 def flux_qk_norm_rope(ctx, hc, q, k, positions, total, q_out, k_out, stream=None) -> None:
-    _check(_lib.flux_qk_norm_rope(ctx, _head_arg(hc), _rows_arg(q, k, None), _ptr(positions), total, _ptr(q_out), _ptr(k_out), _stream(stream)))
+    _check(_lib.flux_qk_norm_rope(ctx, _head_arg(hc), _rows_arg(q, k, None, hc, total), _ptr(positions), total, _rows_out(q_out, total * hc.n_q_heads * hc.head_dim),
+                                  _rows_out(k_out, total * hc.n_kv_heads * hc.head_dim), _stream(stream)))
 
 
 def flux_qkv_append(ctx, hc, cache, q, k, v, cu_new, total_new, max_new, positions, q_out, stream=None) -> None:
-    _check(_lib.flux_qkv_append(ctx, _head_arg(hc), _cache_arg(cache), _rows_arg(q, k, v), _ptr(cu_new), total_new, max_new, _ptr(positions),
-                                _ptr(q_out), _stream(stream)))
+    _check(_lib.flux_qkv_append(ctx, _head_arg(hc), _cache_arg(cache), _rows_arg(q, k, v, hc, total_new), _ptr(cu_new), total_new, max_new, _ptr(positions),
+                                _rows_out(q_out, total_new * hc.n_q_heads * hc.head_dim), _stream(stream)))
 
 
 def flux_qkv_append_paged(ctx, hc, kv, q, k, v, slots, positions, total_new, q_out, stream=None) -> None:
-    _check(_lib.flux_qkv_append_paged(ctx, _head_arg(hc), _handle_arg(kv), _rows_arg(q, k, v), _ptr(slots), _ptr(positions), total_new, _ptr(q_out),
-                                      _stream(stream)))
+    _check(_lib.flux_qkv_append_paged(ctx, _head_arg(hc), _handle_arg(kv), _rows_arg(q, k, v, hc, total_new), _ptr(slots), _ptr(positions), total_new,
+                                      _rows_out(q_out, total_new * hc.n_q_heads * hc.head_dim), _stream(stream)))
 
 
 def flux_page_fork(ctx, pt, shares, parent, keep_len, copies, n_copies, stream=None) -> None:
