@@ -470,7 +470,7 @@ int flux_page_copy(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int h
  * and is not reported); any other call takes what there is.
  * Weights are held to 2^-16 where max_q_len * group <= 32 (a decode step is such a call), and else rounded to bf16 as in flux_attn_prefill; cached rows below kv_len[b] must be finite, those of V up to 2^64.
  * Keys of a tile of rows may be shared out over workgroups, in a way that depends on the bounds and lengths of up to 64 sequences side by side.
- * batch * max_q_len < 2^31 where cu_q is NULL; min(batch, 64) * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^23 is always enough (FLUX_EINVAL). */
+ * n_q_heads / n_kv_heads <= 2^20, batch * max_q_len < 2^31 where cu_q is NULL; min(batch, 64) * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^23 is always enough (FLUX_EINVAL). */
 int flux_attn_cross(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, const int32_t* cu_q, int max_q_len, int max_kv_len,
                     const flux_kv_cache* cache, void* out, void* stream);
 

@@ -8,6 +8,7 @@ namespace flux {
 constexpr int kCrossBatch = 64;             // sequences of a launch: a lane looks after each; longer batches take several launches
 constexpr int kCrossMaxUnits = 1024;        // units of a launch whose tiles may be shared out (or one per tile, where those are more)
 constexpr int kCrossMostWgs = 1 << 23;      // workgroups of a launch: fewer than 2^32 threads
+constexpr int kCrossMostGroup = 1 << 20;    // query heads per KV head: (x + 1/2) / group in floats tells row x < 2 group of two tokens (from 2^22.5 on it does not)
 constexpr int kCrossRunWgs = 512;           // workgroups of short runs that the chip holds at once
 constexpr int kCrossJoinWgs = 4096;         // workgroups that join at most (24576 that find nothing to do take 11 us, 4096 take 3)
 constexpr int cross_resident(int head_dim) { return 256 * (head_dim == 128 ? 2 : 3); }   // workgroups that the chip holds at once

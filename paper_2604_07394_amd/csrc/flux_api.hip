@@ -618,9 +618,9 @@ int flux_attn_cross(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, cons
   if (max_q_len < 0 || max_kv_len < 0) return FLUX_EINVAL;
   if (max_kv_len > cache->capacity) return FLUX_ECAPACITY;
   if (!aligned16(q) || !aligned16(out)) return FLUX_EINVAL;
-  // rows and the threads of a launch are counted in 32 bits
+  // rows and the threads of a launch are counted in 32 bits; a row's token is a quotient of 24-bit floats
   const long long rows = (long long)max_q_len * (cfg->n_q_heads / cfg->n_kv_heads);
-  if ((rows + 63) / 64 > (1 << 23) / cfg->n_kv_heads) return FLUX_EINVAL;
+  if (cfg->n_q_heads / cfg->n_kv_heads > kCrossMostGroup || (rows + 63) / 64 > (1 << 23) / cfg->n_kv_heads) return FLUX_EINVAL;
   if (plan_cross(*cfg, cache->batch, max_q_len, max_kv_len, ctx->c.partials_bytes).wgs > kCrossMostWgs) return FLUX_EINVAL;
   if (!cu_q && (long long)cache->batch * max_q_len > 0x7FFFFFFFll) return FLUX_EINVAL;
   if (!cu_q && max_q_len == 1) {

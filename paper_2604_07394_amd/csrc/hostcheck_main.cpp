@@ -265,6 +265,17 @@ int main() {
     EXPECT(flux_attn_cross(ctx, &cfg, p, nullptr, INT_MAX, 64, &kc, p, nullptr), FLUX_EINVAL);
     EXPECT(flux_attn_cross(ctx, &cfg, p, pi, INT_MAX, 64, &kc, p, nullptr), FLUX_EINVAL);
     EXPECT(flux_attn_cross(ctx, &cfg, p, pi, 64, INT_MAX, &kc, p, nullptr), FLUX_ECAPACITY);
+    for (int hkv : {1, 2}) {
+      const int most = (1 << 20) * hkv;
+      flux_attn_cfg wide = {most, hkv, 64, 4, 16, 0.f, 0, 0};
+      EXPECT(flux_attn_cross(ctx, &wide, p, pi, 2, 64, &kc, p, nullptr), FLUX_EHIP);
+      EXPECT(flux_attn_cross(ctx, &wide, p, nullptr, 1, 64, &kc, p, nullptr), FLUX_EHIP);
+      for (int heads : {most + hkv, 6 * most}) {
+        wide.n_q_heads = heads;
+        EXPECT(flux_attn_cross(ctx, &wide, p, pi, 2, 64, &kc, p, nullptr), FLUX_EINVAL);
+        EXPECT(flux_attn_cross(ctx, &wide, p, nullptr, 1, 64, &kc, p, nullptr), FLUX_EINVAL);
+      }
+    }
     long long wgs;
     int share;
     const int heads[][2] = {{32, 8}, {28, 4}, {8, 2}, {1, 1}, {16, 1}, {64, 64}, {96, 1}, {256, 2}, {4096, 4096}};
