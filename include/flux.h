@@ -467,7 +467,7 @@ int flux_page_copy(flux_ctx* ctx, const flux_paged_kv* kv, int n_kv_heads, int h
  * sa_block have to be valid and are not used.  max_q_len, max_kv_len: host upper bounds (rows and keys beyond them are left out and raise FLUX_DEV_BAD_LENGTH; looser ones cost idle
  * workgroups).  Rows without any key are zero; rows of no sequence are left as they were.  With cu_q NULL and max_q_len 1 (a decode step) the
  * call is worked on like flux_attn_decode and needs the workspace that flux_workspace_needed names (a length above the capacity counts as the capacity there,
- * and is not reported); any other call takes what there is.
+ * and is reported only where max_kv_len is less); any other call takes what there is.
  * Weights are held to 2^-16 where max_q_len * group <= 32 (a decode step is such a call), and else rounded to bf16 as in flux_attn_prefill; cached rows below kv_len[b] must be finite, those of V up to 2^64.
  * Keys of a tile of rows may be shared out over workgroups, in a way that depends on the bounds and lengths of up to 64 sequences side by side.
  * n_q_heads / n_kv_heads <= 2^20, batch * max_q_len < 2^31 where cu_q is NULL; min(batch, 64) * (n_kv_heads * ceil(max_q_len * group / 64) + 8) <= 2^23 is always enough (FLUX_EINVAL). */

@@ -624,10 +624,11 @@ int flux_attn_cross(flux_ctx* ctx, const flux_attn_cfg* cfg, const void* q, cons
   if (plan_cross(*cfg, cache->batch, max_q_len, max_kv_len, ctx->c.partials_bytes).wgs > kCrossMostWgs) return FLUX_EINVAL;
   if (!cu_q && (long long)cache->batch * max_q_len > 0x7FFFFFFFll) return FLUX_EINVAL;
   if (!cu_q && max_q_len == 1) {
-    // a decode step: a ring of all rows of the cache, which sees all that it holds
+    // a decode step: a ring of all rows of the cache, which sees all that it holds; all but the last are sinks, so that the first rows come first whatever the length
     flux_attn_cfg ring = *cfg;
-    ring.n_sink = ring.sa_block = 0;
-    ring.window = cache->capacity;
+    ring.sa_block = 0;
+    ring.n_sink = cache->capacity - 1;
+    ring.window = 1;
     const DecodePlan p = plan_decode(ring, cache->batch, max_kv_len);
     if (ctx->c.device >= 0 && decode_partials_bytes(ring, p) > ctx->c.partials_bytes) return FLUX_EWORKSPACE;
     if (ctx->c.device < 0) return hip_fail(hipErrorNoDevice);
